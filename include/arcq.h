@@ -288,6 +288,73 @@ arcq_status arcq_mx_pack_weight_ex(const void* w, int64_t N, int64_t K, int64_t 
                                    const int32_t* perm, int64_t S, uint32_t flags,
                                    uint8_t* codes, uint8_t* scales, void* stream);
 
+/*
+ * 8-bit activations against the MXFP4 weights of arcq_mx_pack_weight.  MXFP8 is the 8-bit format whose worst case the paper's
+ * analysis compares its two 4-bit stages with (Section 3.4); gfx950 multiplies it with MXFP4 natively, so one set of packed weights
+ * serves both precisions of a layer's activations: the S columns that repeat the outliers' weights are passed over.
+ * Format (OCP Microscaling): 32 E4M3 elements (bias 7, max 448, finite flavour) per block, one E8M0 scale byte per block:
+ * shared exponent = floor(log2(block maximum)) - 8, elements round to nearest even and saturate at 448; an all-zero block gets byte 127.
+ *   codes  uint8 [rows, K]     one E4M3 byte per element, 16-byte aligned
+ *   scales uint8 [rows, K/32]
+ * K % 32 == 0, K <= ARCQ_MAX_K.  Rows are dense.
+ *
+ * arcq_mx8_quantize_act: Xp[m, j] = x[m, perm[j]], then blocks as above.  x, ldx as in arcq_quantize_act; perm as there (the order that
+ *   the weights were packed with), or NULL: channels stay in their order.  flags: 0 or ARCQ_SCALE_ROUND_UP, the smallest
+ *   power of two X with block maximum <= 448 X, so that no element saturates.
+ *
+ * arcq_mx8_add_rmsnorm_quantize_act: the same behind the residual's addition and RMSNorm, as one kernel:
+ *     hidden = fl16(x + residual);   y = RMSNorm(hidden) with weight gamma, the formula and roundings of arcq_rmsnorm_quantize_act;
+ *   then arcq_mx8_quantize_act of y.  residual and hidden are fp16 [M, K] with pitches of their own, 16-byte aligned, pitch % 8 == 0;
+ *   hidden may be x or residual (with that input's pitch: the addition in place); any other overlap of it with an input is not
+ *   allowed.  Both NULL: no addition, x itself is normalised (ldr and ldh are ignored).  flags: also ARCQ_RMSNORM_EXACT_SUM.
+ *   The sums x + residual must be finite in fp16.
+ *
+ * arcq_mx8_gemm: y[m, n] = sum_{b < K/32} 2^(sa[m,b]-127) 2^(sw[n,b]-127) sum_{i<32} a[m,32b+i] qw[n,32b+i],  fp32 accumulation.
+ *   a_*  MXFP8 activations [M, K];  w_*  weights of arcq_mx_pack_weight with this K and S in the plain layout (S = 0: plain MXFP4;
+ *   not ARCQ_LAYOUT_INTERLEAVED with S > 0); all codes 16-byte aligned.  y as in arcq_gemm.
+ *   workspace  256-byte aligned, at least arcq_mx8_gemm_workspace_size bytes: few-tile problems then split K into runs whose fp32 partial
+ *     results a second kernel adds in index order.  NULL: never split (the same result up to the order of the fp32 additions).
+ *     Calls that share a workspace must not overlap.
+ */
+arcq_status arcq_mx8_packed_sizes(int64_t rows, int64_t K, size_t* codes_bytes, size_t* scales_bytes);
+arcq_status arcq_mx8_quantize_act(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, uint32_t flags,
+                                  uint8_t* codes, uint8_t* scales, void* stream);
+arcq_status arcq_mx8_add_rmsnorm_quantize_act(const void* x, int64_t M, int64_t K, int64_t ldx,
+                                              const void* residual, int64_t ldr, void* hidden, int64_t ldh,
+                                              const void* gamma, float eps, const int32_t* perm, uint32_t flags,
+                                              uint8_t* codes, uint8_t* scales, void* stream);
+arcq_status arcq_mx8_gemm_workspace_size(int64_t M, int64_t N, int64_t K, size_t* bytes);
+arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales,
+                          const uint8_t* w_codes, const uint8_t* w_scales,
+                          int64_t M, int64_t N, int64_t K, int64_t S,
+                          void* y, int y_dtype, int64_t ldy,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A few fp16 rows times packed 4-bit weights: the decode step of a layer whose activations are not quantized, on the weights
+ * that arcq_pack_weight (arcq_gemv) or arcq_mx_pack_weight (arcq_mx_gemv) made for the 4-bit path:
+ *   y[m, n] = w_tensor_scale * sum_{b < K/16} sw[n,b] sum_{i<16} x[m, perm[16b+i]] qw[n,16b+i]           (MXFP4: blocks of 32, no tensor scale)
+ * with fp32 accumulation; the weights are used as they are packed, x is not rounded.
+ * x     fp16 [M, K], pitch ldx, 16-byte aligned, ldx % 8 == 0.  Any M; made for up to 64 rows (more take the weights once for every 64).
+ * perm  int32 [K], 16-byte aligned: the order that the weights were packed with, or NULL where they were packed in the channels' own.
+ *       With entries outside 0..K-1 the output is unspecified; no global memory outside the arguments is touched.
+ * w_*   packed weights [N, K + S] in the plain layout (not ARCQ_LAYOUT_INTERLEAVED with S > 0), codes 8-byte aligned; the S columns that
+ *       repeat the outliers' weights are passed over.  K, S as in the packer.
+ * y     as in arcq_gemm.
+ * workspace  256-byte aligned, at least arcq_gemv_workspace_size / arcq_mx_gemv_workspace_size bytes (may be NULL when that is 0).
+ *       Calls that share a workspace must not overlap.
+ */
+arcq_status arcq_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes);
+arcq_status arcq_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                      const uint8_t* w_codes, const uint8_t* w_scales, float w_tensor_scale,
+                      int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy,
+                      void* workspace, size_t workspace_bytes, void* stream);
+arcq_status arcq_mx_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes);
+arcq_status arcq_mx_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                         const uint8_t* w_codes, const uint8_t* w_scales,
+                         int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

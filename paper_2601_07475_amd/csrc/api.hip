@@ -477,4 +477,171 @@ arcq_status arcq_mx_gemm_ws(const uint8_t* a_codes, const uint8_t* a_scales, con
                          workspace_bytes, stream);
 }
 
+arcq_status arcq_mx8_packed_sizes(int64_t rows, int64_t K, size_t* codes_bytes, size_t* scales_bytes) {
+    clear_error();
+    if (arcq_status st = check_KS_mx(K, 0)) return st;
+    if (rows < 0) return fail(ARCQ_BAD_SHAPE, "rows = %lld < 0", (long long)rows);
+    if (!codes_bytes || !scales_bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    *codes_bytes = (size_t)rows * (size_t)K;
+    *scales_bytes = (size_t)rows * (size_t)K / 32;
+    return ARCQ_OK;
+}
+
+// Rows of fp16 that a kernel reads or writes in 16-byte pieces.
+static arcq_status check_rows(const char* who, const char* what, const void* p, int64_t ld) {
+    if (!p) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(p, 16) || (ld % 8) != 0)
+        return fail(ARCQ_BAD_ALIGN, "%s: %s must be 16-byte aligned with a leading dimension that is a multiple of 8", who, what);
+    return ARCQ_OK;
+}
+
+static arcq_status check_pitch(const char* who, const char* what, int64_t ld, int64_t K) {
+    if (ld < K) return fail(ARCQ_BAD_SHAPE, "%s: leading dimension of %s %lld < K = %lld", who, what, (long long)ld, (long long)K);
+    return ARCQ_OK;
+}
+
+static arcq_status check_mx8_outputs(const char* who, const int32_t* perm, const uint8_t* codes, const uint8_t* scales) {
+    if (!codes || !scales) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(codes, 16)) return fail(ARCQ_BAD_ALIGN, "%s: codes must be 16-byte aligned", who);
+    if (!aligned(perm, 16)) return fail(ARCQ_BAD_ALIGN, "%s: perm must be 16-byte aligned", who);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_mx8_quantize_act(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, uint32_t flags,
+                                  uint8_t* codes, uint8_t* scales, void* stream) {
+    const char* who = "arcq_mx8_quantize_act";
+    clear_error();
+    if (arcq_status st = check_KS_mx(K, 0)) return st;
+    if (flags & ~(uint32_t)ARCQ_SCALE_ROUND_UP) return fail(ARCQ_INVALID_ARG, "%s: unknown bits in flags = 0x%x", who, flags);
+    if (M < 0 || M > 0x7FFFFFFF) return fail(ARCQ_BAD_SHAPE, "%s: M = %lld out of range", who, (long long)M);
+    if (arcq_status st = check_pitch(who, "x", ldx, K)) return st;
+    if (M == 0) return ARCQ_OK;
+    if (arcq_status st = check_rows(who, "x", x, ldx)) return st;
+    if (arcq_status st = check_mx8_outputs(who, perm, codes, scales)) return st;
+    return launch_mx8_quantize(x, ldx, nullptr, 0, nullptr, 0, M, K, nullptr, 0.0f, perm, codes, scales, flags, static_cast<hipStream_t>(stream));
+}
+
+arcq_status arcq_mx8_add_rmsnorm_quantize_act(const void* x, int64_t M, int64_t K, int64_t ldx, const void* residual, int64_t ldr,
+                                              void* hidden, int64_t ldh, const void* gamma, float eps, const int32_t* perm, uint32_t flags,
+                                              uint8_t* codes, uint8_t* scales, void* stream) {
+    const char* who = "arcq_mx8_add_rmsnorm_quantize_act";
+    clear_error();
+    if (arcq_status st = check_KS_mx(K, 0)) return st;
+    if (flags & ~(uint32_t)(ARCQ_SCALE_ROUND_UP | ARCQ_RMSNORM_EXACT_SUM)) return fail(ARCQ_INVALID_ARG, "%s: unknown bits in flags = 0x%x", who, flags);
+    if (M < 0 || M > 0x7FFFFFFF) return fail(ARCQ_BAD_SHAPE, "%s: M = %lld out of range", who, (long long)M);
+    if (!std::isfinite(eps) || eps < 0.0f) return fail(ARCQ_INVALID_ARG, "%s: eps = %g must be finite and >= 0", who, (double)eps);
+    if (arcq_status st = check_pitch(who, "x", ldx, K)) return st;
+    if (M == 0) return ARCQ_OK;
+    if ((residual == nullptr) != (hidden == nullptr)) return fail(ARCQ_INVALID_ARG, "%s: residual and hidden go together", who);
+    if (arcq_status st = check_rows(who, "x", x, ldx)) return st;
+    if (residual) {
+        if (arcq_status st = check_pitch(who, "residual", ldr, K)) return st;
+        if (arcq_status st = check_pitch(who, "hidden", ldh, K)) return st;
+        if (arcq_status st = check_rows(who, "residual", residual, ldr)) return st;
+        if (arcq_status st = check_rows(who, "hidden", hidden, ldh)) return st;
+        // in place of an input is one row over the same row, not part of another
+        if (M > 1 && ((hidden == x && ldh != ldx) || (hidden == residual && ldh != ldr)))
+            return fail(ARCQ_BAD_SHAPE, "%s: hidden in place of an input needs that input's leading dimension", who);
+    }
+    if (!gamma) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(gamma, 16)) return fail(ARCQ_BAD_ALIGN, "%s: gamma must be 16-byte aligned", who);
+    if (arcq_status st = check_mx8_outputs(who, perm, codes, scales)) return st;
+    return launch_mx8_quantize(x, ldx, residual, ldr, hidden, ldh, M, K, gamma, eps, perm, codes, scales, flags, static_cast<hipStream_t>(stream));
+}
+
+static arcq_status check_mx8_gemm_shape(int64_t M, int64_t N, int64_t K, int64_t S) {
+    if (arcq_status st = check_KS_mx(K, S)) return st;
+    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x7FFFFFFF)
+        return fail(ARCQ_BAD_SHAPE, "M = %lld, N = %lld out of range", (long long)M, (long long)N);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_mx8_gemm_workspace_size(int64_t M, int64_t N, int64_t K, size_t* bytes) {
+    clear_error();
+    if (arcq_status st = check_mx8_gemm_shape(M, N, K, 0)) return st;
+    if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    *bytes = (M == 0 || N == 0) ? 0 : mx8_gemm_workspace_bytes(M, N, K);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                          int64_t M, int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "arcq_mx8_gemm";
+    clear_error();
+    if (arcq_status st = check_mx8_gemm_shape(M, N, K, S)) return st;
+    if (y_dtype != ARCQ_DTYPE_F16 && y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", y_dtype);
+    if (ldy < N) return fail(ARCQ_BAD_SHAPE, "ldy = %lld < N = %lld", (long long)ldy, (long long)N);
+    if (M == 0 || N == 0) return ARCQ_OK;
+    if (!a_codes || !a_scales || !w_codes || !w_scales || !y) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(a_codes, 16) || !aligned(w_codes, 16)) return fail(ARCQ_BAD_ALIGN, "%s: codes must be 16-byte aligned", who);
+    if (!aligned(y, 4)) return fail(ARCQ_BAD_ALIGN, "%s: y must be 4-byte aligned", who);
+    if (workspace) {
+        const size_t need = mx8_gemm_workspace_bytes(M, N, K);
+        if (workspace_bytes < need)
+            return fail(ARCQ_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace_bytes);
+        if (!aligned(workspace, 256)) return fail(ARCQ_BAD_ALIGN, "%s: workspace must be 256-byte aligned", who);
+    }
+    return launch_mx8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, S, y, y_dtype, ldy, workspace, static_cast<hipStream_t>(stream));
+}
+
+static arcq_status check_gemv_shape(int block, int64_t M, int64_t N, int64_t K, int64_t S) {
+    if (arcq_status st = block == 16 ? check_KS(K, S) : check_KS_mx(K, S)) return st;
+    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x7FFFFFFF)
+        return fail(ARCQ_BAD_SHAPE, "M = %lld, N = %lld out of range", (long long)M, (long long)N);
+    return ARCQ_OK;
+}
+
+static arcq_status gemv_entry(const char* who, int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                              const uint8_t* w_codes, const uint8_t* w_scales, float w_tensor_scale, int64_t N, int64_t S,
+                              void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    clear_error();
+    if (arcq_status st = check_gemv_shape(block, M, N, K, S)) return st;
+    if (y_dtype != ARCQ_DTYPE_F16 && y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", y_dtype);
+    if (arcq_status st = check_pitch(who, "x", ldx, K)) return st;
+    if (ldy < N) return fail(ARCQ_BAD_SHAPE, "ldy = %lld < N = %lld", (long long)ldy, (long long)N);
+    if (arcq_status st = check_scale(w_tensor_scale, "w_tensor_scale")) return st;
+    if (M == 0 || N == 0) return ARCQ_OK;
+    if (arcq_status st = check_rows(who, "x", x, ldx)) return st;
+    if (!w_codes || !w_scales || !y) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(w_codes, 8)) return fail(ARCQ_BAD_ALIGN, "%s: codes must be 8-byte aligned", who);
+    if (!aligned(perm, 16)) return fail(ARCQ_BAD_ALIGN, "%s: perm must be 16-byte aligned", who);
+    if (!aligned(y, 4)) return fail(ARCQ_BAD_ALIGN, "%s: y must be 4-byte aligned", who);
+    const size_t need = gemv_workspace_bytes(M, K, perm != nullptr);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need)
+            return fail(ARCQ_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace_bytes);
+        if (!aligned(workspace, 256)) return fail(ARCQ_BAD_ALIGN, "%s: workspace must be 256-byte aligned", who);
+    }
+    return launch_gemv(block, x, M, K, ldx, perm, w_codes, w_scales, N, S, w_tensor_scale, y, y_dtype, ldy, workspace,
+                       static_cast<hipStream_t>(stream));
+}
+
+arcq_status arcq_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes) {
+    clear_error();
+    if (arcq_status st = check_gemv_shape(16, M, N, K, 0)) return st;
+    if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    *bytes = (M == 0 || N == 0) ? 0 : gemv_workspace_bytes(M, K, with_perm != 0);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes, const uint8_t* w_scales,
+                      float w_tensor_scale, int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+    return gemv_entry("arcq_gemv", 16, x, M, K, ldx, perm, w_codes, w_scales, w_tensor_scale, N, S, y, y_dtype, ldy, workspace, workspace_bytes, stream);
+}
+
+arcq_status arcq_mx_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes) {
+    clear_error();
+    if (arcq_status st = check_gemv_shape(32, M, N, K, 0)) return st;
+    if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    *bytes = (M == 0 || N == 0) ? 0 : gemv_workspace_bytes(M, K, with_perm != 0);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_mx_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes, const uint8_t* w_scales,
+                         int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    return gemv_entry("arcq_mx_gemv", 32, x, M, K, ldx, perm, w_codes, w_scales, 1.0f, N, S, y, y_dtype, ldy, workspace, workspace_bytes, stream);
+}
+
 }  // extern "C"

@@ -96,6 +96,18 @@ arcq_status launch_mx_gemm(const uint8_t* a_codes, const uint8_t* a_scales, cons
                            const uint8_t* w_scales, int64_t M, int64_t N, int64_t Kp, void* y, int y_dtype, int64_t ldy,
                            void* workspace, hipStream_t stream);
 size_t mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t Kp);
+// MXFP8 activations (residual and hidden: both or neither; gamma null: no norm; perm null: channels stay in order) times MXFP4 weights
+arcq_status launch_mx8_quantize(const void* x, int64_t ldx, const void* residual, int64_t ldr, void* hidden, int64_t ldh, int64_t rows, int64_t K,
+                                const void* gamma, float eps, const int32_t* perm, uint8_t* codes, uint8_t* scales, uint32_t flags, hipStream_t stream);
+size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
+// workspace: fp32 partial results of a split reduction dimension, or null (never splits)
+arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
+                            int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream);
+// fp16 rows times packed weights (block 16: NVFP4, 32: MXFP4)
+size_t gemv_workspace_bytes(int64_t M, int64_t K, bool reorder);
+arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
+                        const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
+                        hipStream_t stream);
 // y = alpha * (partial[0] + partial[1] + ... in index order), partial results fp32 [splits][M][N]
 arcq_status launch_splitk_reduce(const float* partial, int splits, int M, int N, float alpha, void* y, int y_dtype,
                                  int64_t ldy, hipStream_t stream);

@@ -15,6 +15,7 @@
 #include "internal.h"
 #include "lds_dma.h"
 #include "nvfp4_device.h"
+#include "row_stats.h"
 
 #include <hip/hip_fp16.h>
 
@@ -57,22 +58,6 @@ typedef __attribute__((address_space(1))) const void global_void_t;
 //       (Appendix D), instead of at K/16 + i; ARCQ_SCALE_ROUND_UP rounds every block scale up.
 // lds_stride = 32 * BPT * blockDim.x >= 2K: bytes of one row buffer, so that the lanes past
 // the end of a row (which re-read its last 16 bytes) land in padding.
-// Sum of v over each row of 16 lanes, in every lane of the row (data-parallel-primitive moves within
-// quads, half rows and rows; the additions must be exact for the order not to matter).
-template <int CTRL>
-__device__ __forceinline__ double dpp_move(double v) {
-    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, true);
-    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, true);
-    return __hiloint2double(hi, lo);
-}
-__device__ __forceinline__ double row16_sum(double v) {
-    v += dpp_move<0xB1>(v);     // quad_perm [1,0,3,2]
-    v += dpp_move<0x4E>(v);     // quad_perm [2,3,0,1]
-    v += dpp_move<0x141>(v);    // row_half_mirror
-    v += dpp_move<0x140>(v);    // row_mirror
-    return v;
-}
-
 template <int BPT, int MODE, bool DB, bool STREAM, int NORM>
 __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(BPT == 1 ? (NORM ? 6 : 8) : 4)))
 void quantize_rows_kernel(
@@ -306,21 +291,7 @@ void quantize_rows_kernel(
                 if (tid < 64) {
                     const uint64_t s_aa = lds_read_u64(red), s_ab = lds_read_u64(red + 8), s_bb = lds_read_u64(red + 16);
                     if (tid < 3) lds_write_u64(red + 8u * tid, 0);      // ready for the next such row
-                    // N = s_aa 2^40 + s_ab 2^21 + s_bb (< 2^97) as six exact doubles, added without error
-                    // into (hi, lo); hi + lo then rounds the exact integer once.
-                    const double term[6] = {(double)(uint32_t)(s_aa >> 32) * 0x1p72, (double)(uint32_t)s_aa * 0x1p40,
-                                            (double)(uint32_t)(s_ab >> 32) * 0x1p53, (double)(uint32_t)s_ab * 0x1p21,
-                                            (double)(uint32_t)(s_bb >> 32) * 0x1p32, (double)(uint32_t)s_bb};
-                    double hi = term[0], lo = 0.0;
-#pragma unroll
-                    for (int k = 1; k < 6; ++k) {
-                        const double sum = hi + term[k];
-                        const double bb = sum - hi;
-                        const double err = (hi - (sum - bb)) + (term[k] - bb);   // hi + term = sum + err exactly
-                        hi = sum;
-                        lo += err;           // integers below 2^53: exact
-                    }
-                    const double sumsq = (hi + lo) * 0x1p-48;
+                    const double sumsq = join_exact_sums(s_aa, s_ab, s_bb);
                     const float ms = (float)(sumsq / (double)K);
                     const float r = 1.0f / __builtin_sqrtf(ms + eps);
                     if (tid == 0) lds_write_f32(red + 24, r);

@@ -1,0 +1,130 @@
+"""The operators with 8- and 16-bit activations together, as a program uses them: a layer's projections behind their norms, a decode
+step on the same packed weights, on other streams and in captured graphs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import arcquant as A
+from oracle import mxfp4 as MX
+from oracle import mxfp8 as M8
+from paper_2601_07475_amd import binding as B
+from paper_2601_07475_amd import workloads as wk
+
+from test_gpu_graph import _replays_match
+from test_gpu_mx8 import assert_product
+from test_gpu_parity import assert_same_bytes, dev, say
+
+pytestmark = pytest.mark.gpu
+
+D, FF, S = 512, 1376, 32        # hidden and inner size of a small model, outlier columns
+
+
+def model(seed):
+    rng = np.random.default_rng(seed)
+    up, down = ((rng.standard_normal(s) * 0.05).astype(np.float16) for s in ((FF, D), (D, FF)))
+    p_up, p_down = (rng.permutation(n).astype(np.int32) for n in (D, FF))
+    gamma = (1 + 0.1 * rng.standard_normal(D)).astype(np.float16)
+    return dict(gamma=gamma, p_up=p_up, p_down=p_down, up=MX.pack_weight(up, p_up, S), down=MX.pack_weight(down, p_down, S),
+                up_nv=A.pack_weight(up, p_up, S, wk.tensor_scale(up)), ts=wk.tensor_scale(up))
+
+
+@pytest.mark.parametrize("M", [1, 19, 300])
+def test_mlp_with_8_bit_activations(M):
+    """hidden -> norm -> up -> quantize -> down -> next layer's addition and norm, in place; each step against the oracle on what it got."""
+    say(f"MLP with MXFP8 activations, M={M}")
+    m = model(1)
+    rng = np.random.default_rng(2)
+    x, r = (dev((rng.standard_normal((M, D)) * 2).astype(np.float16)) for _ in range(2))
+    g, pu, pd = dev(m["gamma"]), dev(m["p_up"]), dev(m["p_down"])
+    up, down = [dev(t) for t in m["up"]], [dev(t) for t in m["down"]]
+    rn = r.cpu().numpy()
+    c, s, h = B.arcq_mx8_add_rmsnorm_quantize_act(x, r, g, 1e-5, pu, hidden=r)
+    wc, wsc, wh = M8.add_rmsnorm_quantize_act(x.cpu().numpy(), rn, m["gamma"], 1e-5, m["p_up"])
+    assert_same_bytes(c.cpu().numpy(), wc, "codes")
+    assert_same_bytes(s.cpu().numpy(), wsc, "scales")
+    assert np.array_equal(r.cpu().numpy(), wh)
+    y = B.arcq_mx8_gemm(c, s, *up)
+    assert_product(y, *M8.gemm(wc, wsc, *m["up"]), D)
+    c, s = B.arcq_mx8_quantize_act(y, pd)
+    wc, wsc = M8.quantize_act(y.cpu().numpy(), m["p_down"])
+    assert_same_bytes(c.cpu().numpy(), wc, "codes")
+    assert_same_bytes(s.cpu().numpy(), wsc, "scales")
+    z = B.arcq_mx8_gemm(c, s, *down)
+    assert_product(z, *M8.gemm(wc, wsc, *m["down"]), FF)
+    zn = z.cpu().numpy()
+    c, s, h = B.arcq_mx8_add_rmsnorm_quantize_act(z, r, g, 1e-5, pu, hidden=z)
+    wc, wsc, wh = M8.add_rmsnorm_quantize_act(zn, wh, m["gamma"], 1e-5, m["p_up"])
+    assert_same_bytes(c.cpu().numpy(), wc, "codes")
+    assert_same_bytes(s.cpu().numpy(), wsc, "scales")
+    assert np.array_equal(z.cpu().numpy(), wh)
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
+def test_decode_step_on_the_weights_of_the_4_bit_path(fmt):
+    """A prompt through the 4-bit GEMM and the next token through fp16 rows, on the same packed weights."""
+    say(f"4-bit prompt, fp16 decode, {fmt}")
+    m = model(3)
+    X = wk.activations(wk.Workload("t", 40, D, FF, S, 5, "loguniform20_100", 0.05, 5))
+    x, pu = dev(X), dev(m["p_up"])
+    if fmt == "mx":
+        w = [dev(t) for t in m["up"]]
+        prompt = B.arcq_mx_gemm(*B.arcq_mx_quantize_act(x, pu, S), *w, out_dtype=torch.float32)
+        token = B.arcq_mx_gemv(x[-1:], pu, *w, out_dtype=torch.float32)
+        want, mag = M8.gemv(X[-1:], m["p_up"], *m["up"])
+    else:
+        w, ts = [dev(t) for t in m["up_nv"]], float(m["ts"])
+        sx = float(wk.tensor_scale(X))
+        prompt = B.arcq_gemm(*B.arcq_quantize_act(x, pu, S, sx), sx, *w, ts, out_dtype=torch.float32)
+        token = B.arcq_gemv(x[-1:], pu, *w, ts, out_dtype=torch.float32)
+        want, mag = M8.gemv(X[-1:], m["p_up"], *m["up_nv"], m["ts"])
+    assert_product(token, want, mag, D)
+    # the prompt's last row is the same product with quantized activations
+    a, b = prompt[-1].double(), token[0].double()
+    assert float((a - b).norm() / b.norm()) < 0.25
+
+
+def test_steps_in_a_captured_graph():
+    say("graph capture of the 8-bit layer and the fp16 decode step")
+    m, M = model(4), 150
+    g, pu, pd = dev(m["gamma"]), dev(m["p_up"]), dev(m["p_down"])
+    up, down, nv = ([dev(t) for t in m[k]] for k in ("up", "down", "up_nv"))
+    ins = [(torch.randn((M, D), device="cuda") * 2).half() for _ in range(4)]
+    x, r = ins[0].clone(), ins[1].clone()
+    h, y, z = (torch.empty(s, dtype=torch.float16, device="cuda") for s in ((M, D), (M, FF), (M, D)))
+    v, v2 = (torch.empty((7, FF), dtype=torch.float32, device="cuda") for _ in range(2))
+    c1, s1, c2, s2 = (torch.empty(s, dtype=torch.uint8, device="cuda") for s in ((M, D), (M, D // 32), (M, FF), (M, FF // 32)))
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+
+    def step():
+        B.arcq_mx8_add_rmsnorm_quantize_act(x, r, g, 1e-5, pu, hidden=h, codes=c1, scales=s1)
+        B.arcq_mx8_gemm(c1, s1, *up, y=y, workspace=ws)
+        B.arcq_mx8_quantize_act(y, pd, codes=c2, scales=s2)
+        B.arcq_mx8_gemm(c2, s2, *down, y=z, workspace=ws)
+        B.arcq_mx_gemv(x[:7], pu, *up, y=v, workspace=ws)
+        B.arcq_gemv(x[:7], pu, *nv, float(m["ts"]), y=v2, workspace=ws)
+
+    _replays_match(step, step, [h, y, z, v, v2, c1, s1, c2, s2], lambda i: x.copy_(ins[i]))
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams, each with a workspace of its own, give what one after the other gives."""
+    say("two streams")
+    m = model(6)
+    pu, up = dev(m["p_up"]), [dev(t) for t in m["up"]]
+    xs = [(torch.randn((33, D), device="cuda") * 2).half() for _ in range(2)]
+
+    def step(x, ws):
+        c, s = B.arcq_mx8_quantize_act(x, pu)
+        return B.arcq_mx8_gemm(c, s, *up, workspace=ws), B.arcq_mx_gemv(x, pu, *up, workspace=ws)
+
+    spaces = [torch.empty(1 << 22, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    want = [step(x, w) for x, w in zip(xs, spaces)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        got = []
+        for x, w, st in zip(xs, spaces, streams):
+            with torch.cuda.stream(st):
+                got.append(step(x, w))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for p, q in zip(got, want) for a, b in zip(p, q))
