@@ -158,10 +158,15 @@ def test_rows_of_zeros():
 
 # ------------------------------------------------------------------------------------------------------------------ products
 
-def assert_product(y, want, mag, K):
+# fp16 products of more than a few rows line up eight products at the largest and drop what is more than 13 bits below its exponent: less than
+# 2^-13 of the largest for each of seven others, 2^-10 of the eight magnitudes' sum
+NATIVE = 2.0 ** -10
+
+
+def assert_product(y, want, mag, K, dropped=0.0):
     got = y.double().cpu().numpy()
     # each of the K / 32 block sums and each addition to the accumulator loses less than a step, 2^-23 of at most mag; joining waves and runs: 64 more
-    bound = mag * (K / 16 + 64) * 2.0 ** -23
+    bound = mag * ((K / 16 + 64) * 2.0 ** -23 + dropped)
     if y.dtype is torch.float16:
         bound = bound + (np.abs(want) + bound) * 2.0 ** -11 + 2.0 ** -25        # half a step, of a subnormal too
     over = np.abs(got - want) - bound
@@ -192,7 +197,7 @@ def run_gemm(M, N, K, S, dtype, seed, extra=0, workspace=True):
     raw, y = output(M, N, dtype, extra)
     B.arcq_mx8_gemm(dev(ac), dev(asc), dev(wc), dev(wsc), y=y, workspace=ws)
     torch.cuda.synchronize()
-    assert_product(y, want, mag, K)
+    assert_product(y, want, mag, K, NATIVE if dtype is torch.float16 else 0.0)
     y.fill_(12345.0)
     assert bool((raw == 12345.0).all())                                 # nothing beside the output
     return need
