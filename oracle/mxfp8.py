@@ -92,3 +92,23 @@ def gemv(X, perm, w_codes, w_scales, w_tensor_scale=None):
     w = MX.dequantize(w_codes, w_scales) if w_tensor_scale is None else A.dequantize(w_codes, w_scales, w_tensor_scale)
     w = w[:, :x.shape[1]].astype(np.float64)
     return x @ w.T, np.abs(x) @ np.abs(w).T
+
+
+def aligned_loss(a_codes, a_scales, w_codes, w_scales):
+    """Largest error, element by element, of products whose eight products of eight consecutive k are lined up at the largest of their
+    exponent sums (an element's exponent, that of the smallest normal below it) and cut 13 bits below it: less than a unit there for each of
+    seven others.  float64 [M, N]; for a few rows of activations (it looks at every product)."""
+    K = a_codes.shape[1]
+    mag = a_codes & 0x7F
+    ea = np.where(mag == 0, -1000, np.maximum(mag >> 3, 1).astype(np.int64) - 7)
+    ea = ea + np.repeat(a_scales.astype(np.int64) - 127, G, axis=1)
+    c = MX.unpack_nibbles(w_codes)[:, :K] & 7
+    ew = np.where(c == 0, -1000, np.maximum(c >> 1, 1).astype(np.int64) - 1)
+    ew = ew + np.repeat(w_scales[:, :K // G].astype(np.int64) - 127, G, axis=1)
+    out = np.zeros((a_codes.shape[0], w_codes.shape[0]))
+    for k in range(0, K, 8):
+        top = np.full(out.shape, -2000, dtype=np.int64)
+        for i in range(k, k + 8):
+            np.maximum(top, ea[:, i, None] + ew[None, :, i], out=top)
+        out += np.where(top > -500, 7.0 * np.exp2(np.maximum(top, -500) - 13.0), 0.0)
+    return out

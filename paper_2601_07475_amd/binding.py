@@ -71,6 +71,7 @@ SIGNATURES = {
     "arcq_mx8_add_rmsnorm_quantize_act": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _f32, _vp, _u32, _vp, _vp, _vp]),
     "arcq_mx8_gemm_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, ctypes.POINTER(_sz)]),
     "arcq_mx8_gemm": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "arcq_mx8_gemm_route": (ctypes.c_int, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(Route)]),
     "arcq_gemv_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, ctypes.POINTER(_sz)]),
     "arcq_gemv": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _f32, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
     "arcq_mx_gemv_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, ctypes.POINTER(_sz)]),
@@ -448,6 +449,14 @@ def _scratch(workspace):
         return None, 0
     assert workspace.is_cuda and workspace.is_contiguous()
     return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def arcq_mx8_gemm_route(M, N, K, S=0, out_dtype=torch.float16, with_workspace=False):
+    """(kernel, tile rows, tile columns, runs of K) that arcq_mx8_gemm takes for these sizes; no GPU needed."""
+    r = Route()
+    dt = DTYPE_F16 if out_dtype is torch.float16 else DTYPE_F32
+    _check(lib().arcq_mx8_gemm_route(M, N, K, S, dt, int(with_workspace), ctypes.byref(r)))
+    return r.kernel, r.tile_rows, r.tile_cols, r.runs
 
 
 def arcq_gemv_workspace_size(M, N, K, with_perm):

@@ -585,6 +585,15 @@ arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const
     return launch_mx8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, S, y, y_dtype, ldy, workspace, static_cast<hipStream_t>(stream));
 }
 
+arcq_status arcq_mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, int y_dtype, int with_workspace, arcq_route* route) {
+    clear_error();
+    if (arcq_status st = check_mx8_gemm_shape(M, N, K, S)) return st;
+    if (y_dtype != ARCQ_DTYPE_F16 && y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", y_dtype);
+    if (!route) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    mx8_gemm_route(M, N, K, S, y_dtype == ARCQ_DTYPE_F32, with_workspace != 0, route);
+    return ARCQ_OK;
+}
+
 static arcq_status check_gemv_shape(int block, int64_t M, int64_t N, int64_t K, int64_t S) {
     if (arcq_status st = block == 16 ? check_KS(K, S) : check_KS_mx(K, S)) return st;
     if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x7FFFFFFF)

@@ -13,6 +13,7 @@
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
+#include "lane_transpose.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -22,15 +23,6 @@ namespace arcq {
 namespace {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
-typedef unsigned uint2v __attribute__((ext_vector_type(2)));
-
-// w[j] of lane group q becomes word q of what lane group j held.
-__device__ __forceinline__ void transpose_words(uint4& w) {
-    const uint2v a = __builtin_amdgcn_permlane32_swap(w.x, w.z, false, false), b = __builtin_amdgcn_permlane32_swap(w.y, w.w, false, false);
-    const uint2v c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    w = make_uint4(c[0], c[1], d[0], d[1]);
-}
-
 typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
 __device__ __forceinline__ uint4 load16_a1(const uint8_t* p) {
     const u32x4 v = *reinterpret_cast<const u32x4_a1*>(p);

@@ -17,37 +17,43 @@
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
+#include "lane_transpose.h"
 #include "lds_dma.h"
 #include "tile_order.h"
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 namespace arcq {
 
 namespace {
 
+typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 // The codes with bit 6, and those without, zeros in the others' places.
+__device__ __forceinline__ void split_word(uint32_t v, int8v& large, int8v& small, int w) {
+    const uint32_t bit = v & 0x40404040u, l = v & ((bit << 2) - (bit >> 6));       // 0xFF for every byte that has the bit
+    large[w] = (int)l;
+    small[w] = (int)(v ^ l);
+}
 __device__ __forceinline__ void split_codes(const int8v& a, int8v& large, int8v& small) {
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        const uint32_t v = (uint32_t)a[w], bit = v & 0x40404040u;
-        const uint32_t l = v & ((bit << 2) - (bit >> 6));       // 0xFF for every byte that has the bit
-        large[w] = (int)l;
-        small[w] = (int)(v ^ l);
-    }
+    for (int w = 0; w < 8; ++w) split_word((uint32_t)a[w], large, small, w);
 }
 
 // Weight-streaming kernel: tiles of 16 MT rows by 16 NT weight rows, K split over the WAVES waves of a workgroup.  Bound by reading the
-// weights once (17/32 byte per weight) for a few rows; any sizes.
-template <int MT, int NT, int WAVES, typename OutT>
+// weights once (17/32 byte per weight) for a few rows; any sizes.  Whole chunks of 128 k go four at a time: every code of the four, and their scale
+// bytes, four to a load and transposed across the lane groups, are in flight at once.
+template <int MT, int NT, int WAVES, bool SPLIT, typename OutT>
 __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
     const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n) {
-    __shared__ float red[WAVES][MT * NT][4][64];
+    // the partial tiles of BATCH weight tiles fit the static LDS limit at a time
+    constexpr int BATCH = WAVES * MT * NT > 64 ? (NT + 1) / 2 : NT;
+    __shared__ float red[WAVES][MT * BATCH][4][64];
     static_assert(sizeof(red) <= 64 * 1024, "partial tiles must fit the static LDS limit");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int i = lane & 15, q = lane >> 4;
@@ -70,106 +76,132 @@ __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
     for (int r = 0; r < MT; ++r)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+    // one chunk; byte `at` of the scale registers
+    auto multiply = [&](const int4v (&lo)[MT], const int4v (&hi)[MT], const uint4 (&cw)[NT], const uint32_t (&sa)[MT], const uint32_t (&sw)[NT], auto at) {
+        constexpr int AT = decltype(at)::value;
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+            const int8v a = __builtin_shufflevector(lo[r], hi[r], 0, 1, 2, 3, 4, 5, 6, 7);
+            int8v large, small;
+            if constexpr (SPLIT) split_codes(a, large, small);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int8v w = {(int)cw[t].x, (int)cw[t].y, (int)cw[t].z, (int)cw[t].w, 0, 0, 0, 0};
+                // formats 0: E4M3, 4: E2M1
+                if constexpr (SPLIT) {
+                    acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(small, w, acc[r][t], 0, 4, AT, (int)sa[r], AT, (int)sw[t]);
+                    acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(large, w, acc[r][t], 0, 4, AT, (int)sa[r], AT, (int)sw[t]);
+                } else {
+                    acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, w, acc[r][t], 0, 4, AT, (int)sa[r], AT, (int)sw[t]);
+                }
+            }
+        }
+    };
 
-    const int chunks = (nb + 3) >> 2;               // of 128 k; the last one may hold fewer than four blocks
-    for (int c = wave; c < chunks; c += WAVES) {
+    const int groups = nb >> 4;
+    const uint32_t sel_half = half_selector(q), sel_byte = byte_selector(q);
+    // scale bytes first: they are needed first, and loads retire in order
+    auto load = [&](int g, int4v (&lo)[4][MT], int4v (&hi)[4][MT], uint4 (&cw)[4][NT], uint32_t (&sa)[MT], uint32_t (&sw)[NT]) {
+#pragma unroll
+        for (int r = 0; r < MT; ++r) sa[r] = load4_a1(as[r] + 16 * (int64_t)g + 4 * q);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sw[t] = load4_a1(ws[t] + 16 * (int64_t)g + 4 * q);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) cw[c][t] = *reinterpret_cast<const uint4*>(wc[t] + 256 * (int64_t)g + 64 * c + 16 * q);
+#pragma unroll
+            for (int r = 0; r < MT; ++r) {
+                lo[c][r] = *reinterpret_cast<const int4v*>(ac[r] + 512 * (int64_t)g + 128 * c + 16 * q);
+                hi[c][r] = *reinterpret_cast<const int4v*>(ac[r] + 512 * (int64_t)g + 128 * c + 64 + 16 * q);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);      // every load of the group ahead of the first use
+    };
+    auto compute = [&](const int4v (&lo)[4][MT], const int4v (&hi)[4][MT], const uint4 (&cw)[4][NT], uint32_t (&sa)[MT], uint32_t (&sw)[NT]) {
+#pragma unroll
+        for (int r = 0; r < MT; ++r) sa[r] = transpose_scale_bytes(sa[r], sel_half, sel_byte);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sw[t] = transpose_scale_bytes(sw[t], sel_half, sel_byte);
+        multiply(lo[0], hi[0], cw[0], sa, sw, std::integral_constant<int, 0>{});
+        multiply(lo[1], hi[1], cw[1], sa, sw, std::integral_constant<int, 1>{});
+        multiply(lo[2], hi[2], cw[2], sa, sw, std::integral_constant<int, 2>{});
+        multiply(lo[3], hi[3], cw[3], sa, sw, std::integral_constant<int, 3>{});
+    };
+    for (int g = wave; g < groups; g += WAVES) {
+        int4v lo[4][MT], hi[4][MT];
+        uint4 cw[4][NT];
+        uint32_t sa[MT], sw[NT];
+        load(g, lo, hi, cw, sa, sw);
+        compute(lo, hi, cw, sa, sw);
+    }
+    const int chunks = (nb + 3) >> 2;               // what is left, a chunk at a time; the last one may hold fewer than four blocks
+    for (int c = 4 * groups + (wave - groups % WAVES + WAVES) % WAVES; c < chunks; c += WAVES) {
         const int b = min(4 * c + q, nb - 1);       // blocks past the end: the last one's bytes, and weight codes of zero
         const bool ok = 4 * c + q < nb;
         const int a0 = min(128 * c + 16 * q, 32 * nb - 16), a1 = min(128 * c + 64 + 16 * q, 32 * nb - 16);
-        uint4 lo[MT], hi[MT], cw[NT];
+        int4v lo[MT], hi[MT];
+        uint4 cw[NT];
         uint32_t sa[MT], sw[NT];
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
-            lo[r] = *reinterpret_cast<const uint4*>(ac[r] + a0);
-            hi[r] = *reinterpret_cast<const uint4*>(ac[r] + a1);
+            lo[r] = *reinterpret_cast<const int4v*>(ac[r] + a0);
+            hi[r] = *reinterpret_cast<const int4v*>(ac[r] + a1);
             sa[r] = as[r][b];
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            cw[t] = *reinterpret_cast<const uint4*>(wc[t] + 16 * (int64_t)b);
+            const uint4 v = *reinterpret_cast<const uint4*>(wc[t] + 16 * (int64_t)b);
+            cw[t] = make_uint4(ok ? v.x : 0, ok ? v.y : 0, ok ? v.z : 0, ok ? v.w : 0);
             sw[t] = ws[t][b];
         }
-        int8v large[MT], small[MT];
-#pragma unroll
-        for (int r = 0; r < MT; ++r) {
-            const int8v a = {(int)lo[r].x, (int)lo[r].y, (int)lo[r].z, (int)lo[r].w, (int)hi[r].x, (int)hi[r].y, (int)hi[r].z, (int)hi[r].w};
-            split_codes(a, large[r], small[r]);
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int8v w = {ok ? (int)cw[t].x : 0, ok ? (int)cw[t].y : 0, ok ? (int)cw[t].z : 0, ok ? (int)cw[t].w : 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int r = 0; r < MT; ++r) {
-                // formats 0: E4M3, 4: E2M1
-                acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(small[r], w, acc[r][t], 0, 4, 0, (int)sa[r], 0, (int)sw[t]);
-                acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(large[r], w, acc[r][t], 0, 4, 0, (int)sa[r], 0, (int)sw[t]);
-            }
-        }
+        multiply(lo, hi, cw, sa, sw, std::integral_constant<int, 0>{});
     }
 #pragma unroll
-    for (int r = 0; r < MT; ++r)
+    for (int t0 = 0; t0 < NT; t0 += BATCH) {
+        if (t0 > 0) __syncthreads();
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int r = 0; r < MT; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][r * NT + t][e][lane] = acc[r][t][e];
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < MT * NT * 4 * 64; idx += WAVES * 64) {
-        const int rt = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
-        float sum = 0.f;
+            for (int t = t0; t < (t0 + BATCH < NT ? t0 + BATCH : NT); ++t)
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum += red[w][rt][e][l];
-        const int m = m0 + 16 * (rt / NT) + 4 * (l >> 4) + e, n = n0 + 16 * (rt % NT) + (l & 15);
-        if (m < M && n < N) store_out(y + (int64_t)m * ldy + n, sum);
+                for (int e = 0; e < 4; ++e) red[wave][r * BATCH + t - t0][e][lane] = acc[r][t][e];
+        __syncthreads();
+        for (int idx = threadIdx.x; idx < MT * BATCH * 4 * 64; idx += WAVES * 64) {
+            const int rt = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
+            if (NT % BATCH != 0 && t0 + rt % BATCH >= NT) continue;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) sum += red[w][rt][e][l];
+            const int m = m0 + 16 * (rt / BATCH) + 4 * (l >> 4) + e, n = n0 + 16 * (t0 + rt % BATCH) + (l & 15);
+            if (m < M && n < N) store_out(y + (int64_t)m * ldy + n, sum);
+        }
     }
 }
 
 // Tiled kernel: 32 WM GM by 32 WN GN outputs a workgroup of GM x GN waves, one tile of 32 WM by 32 WN a wave.  A unit is 128 k: per row 128 bytes
-// of A and 64 of W.  Units travel global -> LDS with buffer copies through a ring of three slots, two units ahead, one barrier a unit.
+// of A and 64 of W.  Units travel global -> LDS with buffer copies through a ring of NS slots, NS - 1 units ahead, one barrier a unit.
 // The 16-byte pieces of a row are stored XOR-swizzled, those of A with (row >> 1) & 7, those of W with (row >> 2) & 3, so that 16 consecutive rows, which a
 // 16-byte read is served in, lie on 16 different groups of banks; applied by choosing which piece a lane fetches.
-// Scale bytes come for four units at a time, 16 bytes a row, through registers into two buffers in front of the ring: their rows start at any
-// address.  Blocks past the end of a row count as zero weight codes.
-template <int WM, int WN, int GM, int GN>
+// Scale bytes: a row's four of a unit start at any address, copies at dwords.  A window of 16 bytes from the dword on that holds the first byte has
+// those of three units whatever the address; readers take two words of it and shift.  Windows have two buffers in front of the ring and are
+// asked for three units ahead.  (Through registers instead, the compiler's wait for them was one for every copy in flight.)
+// Blocks past the end of a row count as zero weight codes with a scale of 1.
+template <int WM, int WN, int GM, int GN, int NS_>
 struct Mx8Tile {
-    static constexpr int BM = 32 * WM * GM, BN = 32 * WN * GN, NT = 64 * GM * GN;
+    static constexpr int BM = 32 * WM * GM, BN = 32 * WN * GN, NT = 64 * GM * GN, NS = NS_;
     static constexpr int NA = BM * 8 / NT, NW = BN * 4 / NT;                // copies of a unit
     static constexpr int W_CODES = BM * 128, UNIT = W_CODES + BN * 64;
-    static constexpr int SCALES = (BM + BN) * 16, UNITS = 2 * SCALES;       // a buffer of scale bytes: rows of A, then of W; where the ring starts
-    static constexpr int LDS_BYTES = UNITS + 3 * UNIT;
-    static_assert(BM * 8 % NT == 0 && BN * 4 % NT == 0, "whole copies");
-    static_assert(BM <= NT && BN <= NT, "a thread fetches the scale bytes of one row of either operand");
+    static constexpr int GROUP = 3;                                         // units of a window
+    static constexpr int SCALES = (BM + BN) * 16, UNITS = 2 * SCALES;       // a buffer of windows: rows of A, then of W; where the ring starts
+    static constexpr int BLOCKS = (BM + BN) / 64, NSC = (BLOCKS + GM * GN - 1) / (GM * GN);      // copies of 64 windows, and of a wave
+    static constexpr int LDS_BYTES = UNITS + NS * UNIT;
+    static_assert(BM * 8 % NT == 0 && BN * 4 % NT == 0 && BM % 64 == 0 && BN % 64 == 0, "whole copies");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
+    static_assert(NS >= 3 && NS - 2 <= GROUP, "windows asked for at the start of a group are older than the copies that its last unit leaves in flight");
+    static_assert((NS - 2) * (NA + NW) < 64, "counted wait");
+    static_assert(WM * WN >= 2, "half a k-step behind the barrier");
 };
-
-typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
-// Scale bytes 16 g .. 16 g + 15 of a row of nb, zeros past its end.
-__device__ __forceinline__ uint4 scales_of_units(const uint8_t* row, int nb, int g) {
-    const int at = 16 * g;
-    if (at + 16 <= nb) {
-        const u32x4 v = *reinterpret_cast<const u32x4_a1*>(row + at);
-        return make_uint4(v[0], v[1], v[2], v[3]);
-    }
-    uint64_t lo = 0, hi = 0;
-    if (nb >= 16) {
-        const u32x4 v = *reinterpret_cast<const u32x4_a1*>(row + nb - 16);
-        lo = (uint64_t)v[1] << 32 | v[0];
-        hi = (uint64_t)v[3] << 32 | v[2];
-        const int shift = 8 * (at + 16 - nb);       // 8 .. 120
-        if (shift >= 64) {
-            lo = hi >> (shift - 64);
-            hi = 0;
-        } else {
-            lo = lo >> shift | hi << (64 - shift);
-            hi >>= shift;
-        }
-    } else {
-        for (int i = 0; i < nb; ++i) {
-            if (i < 8) lo |= (uint64_t)row[i] << (8 * i);
-            else hi |= (uint64_t)row[i] << (8 * (i - 8));
-        }
-    }
-    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
-}
 
 __device__ __forceinline__ float16v mfma_w4a8(const uint4& w, const int8v& a, const float16v& c, uint32_t sw, uint32_t sa, int t) {
     const int8v vw = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
@@ -178,12 +210,12 @@ __device__ __forceinline__ float16v mfma_w4a8(const uint4& w, const int8v& a, co
                   : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vw, a, c, 4, 0, 2, (int)sw, 2, (int)sa);
 }
 
-template <int WM, int WN, int GM, int GN, bool SPLIT, typename OutT>
+template <int WM, int WN, int GM, int GN, int NS, bool SPLIT, typename OutT>
 __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
     const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, int tiles_m, int tiles_n,
     int group_rows, int splits, int64_t split_stride) {
-    using C = Mx8Tile<WM, WN, GM, GN>;
+    using C = Mx8Tile<WM, WN, GM, GN, NS>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     // With splits > 1 workgroup split * num_tiles + tile adds up a run of K and stores an fp32 partial tile at y + split * split_stride
     const int num_tiles = tiles_m * tiles_n;
@@ -195,13 +227,11 @@ __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
     const int wg_m0 = tile.m * C::BM, wg_n0 = tile.n * C::BN;
     const int wrow0 = (wave / GN) * (32 * WM), wcol0 = (wave % GN) * (32 * WN);
 
-    // this workgroup's run of units [u0, u1), whole groups of four but for the last
     const int nunit = (nb + 3) >> 2;
-    int u0 = 0, u1 = nunit;
+    int u0 = 0, u1 = nunit;                     // this workgroup's run of units
     if (splits > 1) {
-        const int groups = (nunit + 3) >> 2;
-        u0 = 4 * (int)((uint32_t)(split * groups) / (uint32_t)splits);
-        u1 = min(4 * (int)((uint32_t)((split + 1) * groups) / (uint32_t)splits), nunit);
+        u0 = (int)((uint32_t)(split * nunit) / (uint32_t)splits);
+        u1 = (int)((uint32_t)((split + 1) * nunit) / (uint32_t)splits);
     }
     const bool ragged = (nb & 3) != 0;
 
@@ -222,19 +252,29 @@ __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
     auto lane_a = [&](int unit, bool last) { return row_a + 16u * (last ? min(8u * unit + pa, 2u * nb - 1u) : pa); };
     auto lane_w = [&](int unit, bool last) { return row_w + 16u * (last ? min(4u * unit + pw, (uint32_t)nb - 1u) : pw); };
 
-    // ---- scale bytes of four units: a row of A and one of W per thread
-    const uint8_t* sa_row = a_scales + (int64_t)min(wg_m0 + min(tid, C::BM - 1), M - 1) * nb;
-    const uint8_t* sw_row = w_scales + (int64_t)min(wg_n0 + min(tid, C::BN - 1), N - 1) * nbw;
-    uint4 next_sa, next_sw;
-    auto fetch_scales = [&](int g) {
-        next_sa = scales_of_units(sa_row, nb, g);
-        next_sw = scales_of_units(sw_row, nb, g);
+    // ---- windows of scale bytes: a wave copies those of 64 rows of one operand at a time (the last copies of some waves repeat others')
+    const uint32_t base_a = (uint32_t)(uintptr_t)a_scales & 3u, base_w = (uint32_t)(uintptr_t)w_scales & 3u;
+    // (whole words that hold a byte of the operand)
+    const buffer_t win_a = buffer_of(a_scales - base_a, (base_a + (uint32_t)M * (uint32_t)nb + 3u) & ~3u);
+    const buffer_t win_w = buffer_of(w_scales - base_w, (base_w + (uint32_t)N * (uint32_t)nbw + 3u) & ~3u);
+    uint32_t win_row[C::NSC];
+#pragma unroll
+    for (int e = 0; e < C::NSC; ++e) {
+        const int block = min((int)(wave_slot >> 6) + e * GM * GN, C::BLOCKS - 1), row = 64 * block + lane;
+        win_row[e] = (64 * block < C::BM ? base_a + (uint32_t)min(wg_m0 + row, M - 1) * (uint32_t)nb
+                                         : base_w + (uint32_t)min(wg_n0 + row - C::BM, N - 1) * (uint32_t)nbw) & ~3u;
+    }
+    auto issue_windows = [&](int group) {       // group of the run
+#pragma unroll
+        for (int e = 0; e < C::NSC; ++e) {
+            const int block = min((int)(wave_slot >> 6) + e * GM * GN, C::BLOCKS - 1);
+            const uint32_t to = lds_address(lds) + (group & 1) * C::SCALES + 1024u * (uint32_t)block, from = 4u * (uint32_t)(u0 + C::GROUP * group);
+            if (64 * block < C::BM) copy16(win_a, win_row[e], from, to);
+            else copy16(win_w, win_row[e], from, to);
+        }
     };
-    auto put_scales = [&](int g) {
-        uint8_t* to = lds + (g & 1) * C::SCALES;
-        if (C::BM == C::NT || tid < C::BM) *reinterpret_cast<uint4*>(to + 16 * tid) = next_sa;
-        if (C::BN == C::NT || tid < C::BN) *reinterpret_cast<uint4*>(to + 16 * (C::BM + tid)) = next_sw;
-    };
+    // a lane's bytes of a unit's word of its rows, shifted so that they are bytes 0 and 2 (rows 32 apart have the same place in a word)
+    const uint32_t shift_a = 8u * ((base_a + (uint32_t)r * (uint32_t)nb & 3u) + h), shift_w = 8u * ((base_w + (uint32_t)r * (uint32_t)nbw & 3u) + h);
 
     // ---- fragments: k-step t of a unit takes pieces 4t + h and 4t + 2 + h of a row of A, piece 2t + h of one of W
     const uint32_t rd_a = (wrow0 + r) * 128, rd_w = C::W_CODES + (wcol0 + r) * 64;
@@ -247,122 +287,177 @@ __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     uint4 fa[2][WM][2], fw[2][WN];
-    uint32_t sa[WM], sw[WN], sa_n[WM], sw_n[WN];        // shifted so that bytes 0 and 2 are this lane's
-    auto read_codes = [&](int t, const uint8_t* st) {
+    uint32_t sa[WM], sw[WN];
+    auto read_a = [&](int t, int i, const uint8_t* st) {
 #pragma unroll
-        for (int i = 0; i < WM; ++i)
-#pragma unroll
-            for (int p = 0; p < 2; ++p) fa[t][i][p] = *reinterpret_cast<const uint4*>(st + rd_a + i * 4096 + 16u * ((uint32_t)(4 * t + 2 * p + h) ^ swz_a));
-#pragma unroll
-        for (int j = 0; j < WN; ++j) fw[t][j] = *reinterpret_cast<const uint4*>(st + rd_w + j * 2048 + 16u * ((uint32_t)(2 * t + h) ^ swz_w));
+        for (int p = 0; p < 2; ++p) fa[t][i][p] = *reinterpret_cast<const uint4*>(st + rd_a + i * 4096 + 16u * ((uint32_t)(4 * t + 2 * p + h) ^ swz_a));
     };
-    auto read_scales = [&](int unit, uint32_t (&da)[WM], uint32_t (&dw)[WN]) {
-        const uint8_t* at = lds + (unit >> 2 & 1) * C::SCALES + 4 * (unit & 3);
+    auto read_w = [&](int t, int j, const uint8_t* st) {
+        fw[t][j] = *reinterpret_cast<const uint4*>(st + rd_w + j * 2048 + 16u * ((uint32_t)(2 * t + h) ^ swz_w));
+    };
+    // part k of `parts` of a k-step's fragments, in the order that the MFMAs want them
+    auto read_part = [&](int t, int k, int parts, const uint8_t* st) {
+        constexpr int ALL = WM + WN;
 #pragma unroll
-        for (int i = 0; i < WM; ++i) da[i] = *reinterpret_cast<const uint32_t*>(at + 16 * (wrow0 + 32 * i + r)) >> (8 * h);
+        for (int f = 0; f < ALL; ++f)
+            if (f * parts / ALL == k) {
+                if (f == 0) read_a(t, 0, st);
+                else if (f <= WN) read_w(t, f - 1, st);
+                else read_a(t, f - WN, st);
+            }
+    };
+    uint2 na[WM], nw[WN];
+    auto read_scales = [&](int group, int word) {
+        const uint8_t* at = lds + (group & 1) * C::SCALES + 4 * word;
+        auto two = [&](int row) {
+            const uint32_t* v = reinterpret_cast<const uint32_t*>(at + 16 * row);
+            return make_uint2(v[0], v[1]);
+        };
 #pragma unroll
-        for (int j = 0; j < WN; ++j) dw[j] = *reinterpret_cast<const uint32_t*>(at + 16 * (C::BM + wcol0 + 32 * j + r)) >> (8 * h);
+        for (int i = 0; i < WM; ++i) na[i] = two(wrow0 + 32 * i + r);
+#pragma unroll
+        for (int j = 0; j < WN; ++j) nw[j] = two(C::BM + wcol0 + 32 * j + r);
+    };
+    auto take_scales = [&]() {
+#pragma unroll
+        for (int i = 0; i < WM; ++i) sa[i] = (uint32_t)(((uint64_t)na[i].y << 32 | na[i].x) >> shift_a);
+#pragma unroll
+        for (int j = 0; j < WN; ++j) sw[j] = (uint32_t)(((uint64_t)nw[j].y << 32 | nw[j].x) >> shift_w);
     };
 
-    // ---- a unit, scheduled by hand: 2 WM WN MFMAs, or twice as many.  The copies of unit u + 2 go out between the first of them (its slot was last
-    // read in unit u - 1, which every wave left before the barrier inside unit u - 1), the fragments of k-step 1 are read while k-step 0 is computed,
-    // and the barrier that opens unit u + 1 and the reads of its first fragments come before the last half k-step.
-    // LEFT: units behind this one, up to 2.
+    // ---- a unit, scheduled by hand: 2 WM WN MFMAs, or twice as many.  Everything else goes between them, behind the first one, so that the
+    // matrix unit does not wait for it: the copies of unit u + NS - 1 (its slot was last read in unit u - 1, which every wave left before
+    // the barrier inside unit u - 1), the reads of k-step 1's fragments, and, behind the barrier that opens unit u + 1 before the last half
+    // k-step, the reads of that unit's first fragments and scale bytes.
+    // COPY: there is a unit u + NS - 1.  DRAIN: there is not, but more units follow.  LAST: none does.
+    enum { COPY, DRAIN, LAST };
     constexpr int NM = WM * WN, NDMA = C::NA + C::NW, LAST_Q = 2 * NM - NM / 2;
-    static_assert(NDMA <= LAST_Q, "copies are issued ahead of the wait that counts them");
-    int slot = 0;
-    auto run_unit = [&](int u, auto left_tag) {
-        constexpr int LEFT = decltype(left_tag)::value;
+    constexpr int FIRST = NM >= 8 ? 4 : NM >= 4 ? 2 : 1;        // MFMA slots that read the fragments of k-step 1
+    constexpr int NEXT = NM >= 16 ? 3 : 1;                      // and, from LAST_Q on, those of the next unit's k-step 0
+    constexpr int COPY0 = NM >= 4 ? 1 : 0;                      // first slot with a copy; all are ahead of the wait that counts them
+    constexpr int SPREAD = LAST_Q - COPY0;
+    int slot = 0, word = 0, group = 0;                          // of unit u
+    int8v large[2], small[2];                                   // SPLIT: of the fragment being multiplied and of the next
+    auto run_unit = [&](int u, auto phase_tag) {
+        constexpr int PHASE = decltype(phase_tag)::value;
         const uint8_t* st = lds + C::UNITS + slot * C::UNIT;
-        const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
-        const bool last = ragged && u + 2 == nunit - 1;
-        const uint32_t va = lane_a(u + 2, last), vw = lane_w(u + 2, last);
-        // scale bytes of the next four units: asked for in the third unit, stored in the fourth, ahead of that unit's copies each
-        // (the compiler waits for every copy in flight before it stores them: they are a unit old there)
-        const int g1 = (u >> 2) + 1;
-        const bool more = LEFT == 2 && 4 * g1 < u1 && (u & 3) == 2, store = LEFT > 0 && 4 * g1 < u1 && (u & 3) == 3;
-        if (more) fetch_scales(g1);
-        if (store) put_scales(g1);
+        const int slot1 = slot == NS - 1 ? 0 : slot + 1, fill = slot == 0 ? NS - 1 : slot - 1;
+        const int word1 = word == C::GROUP - 1 ? 0 : word + 1, group1 = word1 == 0 ? group + 1 : group;
+        bool last = false;
+        uint32_t va = 0, vw = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            if (LEFT == 0 && t == 1 && ragged && 4 * u + 2 >= nb) break;
-            if (t == 0) {
-                read_codes(1, st);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (LEFT == 0 && ragged && 4 * u + 2 * t + h >= nb) {
+            if (PHASE == LAST && t == 1 && ragged && 4 * u + 2 >= nb) break;
+            if (PHASE == LAST && ragged && 4 * u + 2 * t + h >= nb) {
 #pragma unroll
-                for (int j = 0; j < WN; ++j) fw[t][j] = make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < WM; ++i) sa[i] = 0x7F7F7F7Fu;
+#pragma unroll
+                for (int j = 0; j < WN; ++j) {
+                    fw[t][j] = make_uint4(0, 0, 0, 0);
+                    sw[j] = 0x7F7F7F7Fu;
+                }
             }
 #pragma unroll
             for (int i = 0; i < WM; ++i) {
                 const int8v a = {(int)fa[t][i][0].x, (int)fa[t][i][0].y, (int)fa[t][i][0].z, (int)fa[t][i][0].w,
                                  (int)fa[t][i][1].x, (int)fa[t][i][1].y, (int)fa[t][i][1].z, (int)fa[t][i][1].w};
-                int8v large, small;
-                if constexpr (SPLIT) split_codes(a, large, small);
+                constexpr int TURNS = 2 * WM;
+                const int turn = t * WM + i;
 #pragma unroll
                 for (int j = 0; j < WN; ++j) {
                     const int q = t * NM + i * WN + j;
-                    if (q == LAST_Q && LEFT > 0) {
-                        wait_vmcnt<LEFT == 2 ? NDMA : 0>();     // unit u + 1 has landed: the copies of unit u + 2 are younger
-                        wait_lgkmcnt0();                        // this wave's scale bytes are stored
+                    if (q == LAST_Q && PHASE != LAST) {
+                        // unit u + 1 has landed: the copies of later units are younger (and so are no windows that are read below)
+                        if constexpr (PHASE == COPY) {
+                            wait_vmcnt<(NS - 2) * NDMA>();
+                        } else {
+                            const int later = u1 - 2 - u;       // units in flight behind u + 1
+                            if (NS >= 5 && later == 2) wait_vmcnt<2 * NDMA>();
+                            else if (NS >= 4 && later == 1) wait_vmcnt<NDMA>();
+                            else wait_vmcnt<0>();
+                        }
+                        wait_lgkmcnt0();                        // (every fragment of unit u has arrived)
                         wg_barrier();
-                        read_codes(0, lds + C::UNITS + slot1 * C::UNIT);
-                        read_scales(u + 1, sa_n, sw_n);
+                    }
+                    if (PHASE != LAST && q >= LAST_Q && q < LAST_Q + NEXT) {
+                        read_part(0, q - LAST_Q, NEXT, lds + C::UNITS + slot1 * C::UNIT);
+                        if (q == LAST_Q + NEXT - 1) read_scales(group1, word1);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     // weights as the row operand: see store_tile_swapped
                     if constexpr (SPLIT) {
-                        acc[i][j] = mfma_w4a8(fw[t][j], small, acc[i][j], sw[j], sa[i], t);
-                        acc[i][j] = mfma_w4a8(fw[t][j], large, acc[i][j], sw[j], sa[i], t);
+                        acc[i][j] = mfma_w4a8(fw[t][j], small[turn & 1], acc[i][j], sw[j], sa[i], t);
+                        acc[i][j] = mfma_w4a8(fw[t][j], large[turn & 1], acc[i][j], sw[j], sa[i], t);
                     } else {
                         acc[i][j] = mfma_w4a8(fw[t][j], a, acc[i][j], sw[j], sa[i], t);
                     }
                     __builtin_amdgcn_sched_barrier(0);
-                    if (LEFT == 2 && q < NDMA) {
-                        issue_one(q, u + 2, slot2, va, vw, last);
-                        __builtin_amdgcn_sched_barrier(0);
+                    if (q == 0) {
+                        if (PHASE != LAST && word == 0 && u + C::GROUP < u1) issue_windows(group + 1);
+                        if constexpr (PHASE == COPY) {
+                            last = ragged && u + NS - 1 == nunit - 1;
+                            va = lane_a(u + NS - 1, last);
+                            vw = lane_w(u + NS - 1, last);
+                        }
                     }
+                    if (q < FIRST) read_part(1, q, FIRST, st);
+                    if (PHASE == COPY && q >= COPY0 && q < LAST_Q) {
+#pragma unroll
+                        for (int d = 0; d < NDMA; ++d)
+                            if (COPY0 + d * SPREAD / NDMA == q) issue_one(d, u + NS - 1, fill, va, vw, last);
+                    }
+                    // the next fragment's two kinds of codes, behind the second half of this one's MFMAs
+                    constexpr int HALF = WN / 2;
+                    if (SPLIT && j >= HALF && (turn + 1 < TURNS || PHASE != LAST)) {
+                        const int n = (turn + 1) % TURNS;
+                        const uint4(&f)[2] = fa[n / WM][n % WM];
+#pragma unroll
+                        for (int w = 0; w < 8; ++w)
+                            if (w * (WN - HALF) / 8 == j - HALF) {
+                                const uint4& v = f[w >> 2];
+                                split_word((w & 3) == 0 ? v.x : (w & 3) == 1 ? v.y : (w & 3) == 2 ? v.z : v.w, large[(turn + 1) & 1], small[(turn + 1) & 1], w);
+                            }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
-        if constexpr (LEFT > 0) {
-#pragma unroll
-            for (int i = 0; i < WM; ++i) sa[i] = sa_n[i];
-#pragma unroll
-            for (int j = 0; j < WN; ++j) sw[j] = sw_n[j];
-        }
+        if constexpr (PHASE != LAST) take_scales();
         slot = slot1;
+        word = word1;
+        group = group1;
     };
 
-    fetch_scales(u0 >> 2);
-    put_scales(u0 >> 2);
+    issue_windows(0);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int unit = min(u0 + k, nunit - 1);
+    for (int k = 0; k < NS - 1; ++k) {
+        const int unit = min(u0 + k, u1 - 1);       // (a run shorter than the ring copies its last unit again)
         const bool last = ragged && unit == nunit - 1;
 #pragma unroll
         for (int d = 0; d < NDMA; ++d) issue_one(d, unit, k, lane_a(unit, last), lane_w(unit, last), last);
     }
-    wait_vmcnt<NDMA>();
-    wait_lgkmcnt0();
+    wait_vmcnt<(NS - 2) * NDMA>();
     wg_barrier();
-    read_codes(0, lds + C::UNITS);
-    read_scales(u0, sa, sw);
-    using Left0 = std::integral_constant<int, 0>;
-    using Left1 = std::integral_constant<int, 1>;
-    using Left2 = std::integral_constant<int, 2>;
+    read_part(0, 0, 1, lds + C::UNITS);
+    read_scales(0, 0);
+    take_scales();
+    if constexpr (SPLIT) {
+        const uint4 f0 = fa[0][0][0], f1 = fa[0][0][1];
+        split_codes(int8v{(int)f0.x, (int)f0.y, (int)f0.z, (int)f0.w, (int)f1.x, (int)f1.y, (int)f1.z, (int)f1.w}, large[0], small[0]);
+    }
     int u = u0;
-    for (; u < u1 - 2; ++u) run_unit(u, Left2{});
-    if (u1 - u0 > 1) run_unit(u1 - 2, Left1{});
-    run_unit(u1 - 1, Left0{});
+    for (; u < u1 - (NS - 1); ++u) run_unit(u, std::integral_constant<int, COPY>{});
+    for (; u < u1 - 1; ++u) run_unit(u, std::integral_constant<int, DRAIN>{});
+    run_unit(u, std::integral_constant<int, LAST>{});
     wait_vmcnt<0>();                            // no copy may still be in flight when the LDS is released
 
     const int m0 = wg_m0 + wrow0, n0 = wg_n0 + wcol0;
     if constexpr (std::is_same<OutT, _Float16>::value) {
         static_assert(epilogue_lds_bytes(WN) * GM * GN <= C::LDS_BYTES, "one epilogue region per wave must fit");
         wg_barrier();                           // every wave has read its last operands: the ring is free
-        store_tile_f16_via_lds<WM, WN>(acc, lds + wave * epilogue_lds_bytes(WN), m0, n0, lane, M, N, 1.0f, y, ldy);
+        uint8_t* region = lds + wave * epilogue_lds_bytes(WN);
+        if constexpr (WM == 1) store_fragment_rows_f16_via_lds<WM, WN, 0, 1>(acc, region, m0, n0, lane, M, N, 1.0f, y, ldy);
+        else store_tile_f16_via_lds<WM, WN>(acc, region, m0, n0, lane, M, N, 1.0f, y, ldy);
     } else {
         store_tile_swapped<WM, WN>(acc, m0, n0, r, h, M, N, 1.0f, y + (int64_t)split * split_stride, ldy);
     }
@@ -375,19 +470,19 @@ struct Mx8Args {
     hipStream_t stream;
 };
 
-template <int MT, int NT, typename OutT>
+template <int MT, int NT, bool SPLIT, typename OutT>
 arcq_status launch_stream(const Mx8Args& a, OutT* y) {
     const unsigned tiles_n = ((unsigned)a.N + 16 * NT - 1) / (16 * NT), tiles_m = ((unsigned)a.M + 16 * MT - 1) / (16 * MT);
-    hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, OutT>), dim3(tiles_n * tiles_m), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
+    hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, SPLIT, OutT>), dim3(tiles_n * tiles_m), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
                        a.nb, a.nbw, y, a.ldy, tiles_n);
     return check_launch("mx8_stream_kernel");
 }
 
-template <int WM, int WN, bool SPLIT, typename OutT>
+template <int WM, int WN, int NS, bool SPLIT, typename OutT>
 arcq_status launch_tiles(const Mx8Args& a, OutT* y, int splits, int64_t split_stride) {
-    using C = Mx8Tile<WM, WN, 2, 2>;
+    using C = Mx8Tile<WM, WN, 2, 2, NS>;
     const int tiles_m = (a.M + C::BM - 1) / C::BM, tiles_n = (a.N + C::BN - 1) / C::BN;
-    auto kern = mx8_tile_kernel<WM, WN, 2, 2, SPLIT, OutT>;
+    auto kern = mx8_tile_kernel<WM, WN, 2, 2, NS, SPLIT, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     hipLaunchKernelGGL(kern, dim3(tiles_m * tiles_n * splits), dim3(C::NT), C::LDS_BYTES, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales,
@@ -395,28 +490,131 @@ arcq_status launch_tiles(const Mx8Args& a, OutT* y, int splits, int64_t split_st
     return check_launch("mx8_tile_kernel");
 }
 
-template <typename OutT>
-arcq_status launch_typed(const Mx8Args& a, OutT* y) {
-    constexpr bool SPLIT = !std::is_same<OutT, _Float16>::value;
-    const bool offsets_fit = (uint64_t)a.M * a.nb * 32 < 0xFFFF0000ull && (uint64_t)a.N * a.nbw * 16 < 0xFFFF0000ull;
-    if (a.M > 64 && offsets_fit) {
-        if ((int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256) >= 192) return launch_tiles<4, 4, SPLIT>(a, y, 1, 0);
-        return launch_tiles<2, 2, SPLIT>(a, y, 1, 0);
+// The tiles, by fragment rows and columns of a wave, and what a unit and the rest of a tile take (us, measured): with few workgroups, and with
+// every compute unit busy, where two smaller ones share one and large ones meet the power limit.  [0]: one pass, [1]: two.
+struct Tile {
+    int wm, wn;
+    double unit_few[2], unit_all[2], rest[2];
+};
+constexpr Tile kTiles[] = {
+    {4, 4, {1.20, 0.00}, {1.52, 0.00}, {4.0, 0.0}},      // (two passes: registers in scratch)
+    {3, 4, {1.03, 1.96}, {1.20, 2.17}, {3.2, 5.0}},
+    {2, 4, {0.75, 1.36}, {0.89, 1.56}, {2.2, 4.0}},
+    {3, 2, {0.65, 1.30}, {0.72, 1.45}, {2.0, 3.5}},
+    {2, 2, {0.48, 1.00}, {0.49, 0.81}, {1.5, 2.5}},
+    {1, 4, {0.58, 0.95}, {0.60, 0.89}, {1.3, 2.0}},
+    {1, 2, {0.37, 0.56}, {0.33, 0.46}, {1.0, 1.5}},
+};
+
+struct Mx8Plan {
+    int wm = 0, wn = 0, splits = 1;             // wm = 0: the streaming kernel, 16 mt rows by 16 nt weight rows
+    int mt = 0, nt = 0;
+};
+
+// As few weight tiles a wave as keep the launch at one workgroup per compute unit.
+Mx8Plan stream_plan(int64_t M, int64_t N) {
+    const int64_t tiles = (N + 15) / 16;
+    Mx8Plan p;
+    p.mt = M <= 16 ? 1 : 2;
+    p.nt = (int)std::min<int64_t>(tiles <= 1024 ? (tiles + 255) / 256 : p.mt == 1 ? (tiles + 255) / 256 : 4, 7);
+    return p;
+}
+
+// A function of the sizes, the passes and whether there is a workspace: whatever a model of their times, fitted to measurements over 32 to 3000 rows,
+// N = 1024 .. 27648 and K = 4096 .. 14336, puts first (120 problems: 1.02x the fastest of all on average, with one or two passes).
+// The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'.  With more than 128 rows
+// it has what the tiles cannot address.
+Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool two_passes, bool workspace) {
+    const bool offsets_fit = (uint64_t)M * nb * 32 < 0xFFFF0000ull && (uint64_t)N * nbw * 16 < 0xFFFF0000ull;
+    const Mx8Plan stream = stream_plan(M, N);
+    if (!offsets_fit) return stream;
+    const int64_t units = (nb + 3) >> 2;
+    Mx8Plan best;
+    double least = 0.0;
+    if (M <= 128) {
+        const int64_t wgs = ((N + 16 * stream.nt - 1) / (16 * stream.nt)) * ((M + 16 * stream.mt - 1) / (16 * stream.mt));
+        best = stream;
+        least = 4.0 + (double)((wgs + 255) / 256) * ((double)nb / 16.0) * (double)(5 * stream.nt + 9 * stream.mt) * 0.023;
     }
-    if (a.M <= 16) return a.N <= 4096 ? launch_stream<1, 1>(a, y) : launch_stream<1, 4>(a, y);
-    if (a.M <= 32) return a.N <= 4096 ? launch_stream<2, 1>(a, y) : launch_stream<2, 4>(a, y);
-    return launch_stream<4, 2>(a, y);
+    for (const Tile& t : kTiles) {
+        if (t.rest[two_passes] == 0.0) continue;
+        const int64_t tiles = ((M + 64 * t.wm - 1) / (64 * t.wm)) * ((N + 64 * t.wn - 1) / (64 * t.wn));
+        if (tiles > 0x7FFFFFFF / 8) continue;
+        // runs of at least four units; split only where tiles leave compute units idle
+        for (int64_t sp = 1; sp <= (workspace && tiles <= 256 ? std::min<int64_t>(8, units / 4) : 1) || sp == 1; ++sp) {
+            const int64_t work = tiles * sp;
+            const double unit = work >= 256 ? t.unit_all[two_passes] : t.unit_few[two_passes];
+            double us = 3.0 + (double)((work + 255) / 256) * ((double)((units + sp - 1) / sp) * unit + t.rest[two_passes]);
+            if (sp > 1) us += 3.5 + (double)sp * (double)M * (double)N * 8.0 / 4.0e6;      // fp32 partial results, written and read
+            if (least == 0.0 || us < least) {
+                least = us;
+                best = {t.wm, t.wn, (int)sp};
+            }
+        }
+    }
+    return best;
+}
+
+template <int WM, int WN, int NS, bool TWO, typename OutT>
+arcq_status launch_split_tiles(const Mx8Args& a, OutT* y, int splits, float* partial) {
+    if (splits == 1) return launch_tiles<WM, WN, NS, TWO>(a, y, 1, 0);
+    Mx8Args run = a;
+    run.ldy = a.N;
+    if (arcq_status st = launch_tiles<WM, WN, NS, TWO>(run, partial, splits, (int64_t)a.M * a.N)) return st;
+    return launch_splitk_reduce(partial, splits, a.M, a.N, 1.0f, y, std::is_same<OutT, _Float16>::value ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy, a.stream);
+}
+
+template <typename OutT>
+arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
+    constexpr bool TWO = !std::is_same<OutT, _Float16>::value;
+    const Mx8Plan plan = plan_mx8(a.M, a.N, a.nb, a.nbw, TWO, partial != nullptr);
+#define ARCQ_MX8_TILES(WM_, WN_, NS_) \
+    if (plan.wm == WM_ && plan.wn == WN_) return launch_split_tiles<WM_, WN_, NS_, TWO>(a, y, plan.splits, partial)
+    if constexpr (!TWO) {
+        if (plan.wm == 4 && plan.wn == 4 && plan.splits == 1) return launch_tiles<4, 4, 3, false>(a, y, 1, 0);
+    }
+    ARCQ_MX8_TILES(3, 4, 3);
+    ARCQ_MX8_TILES(2, 4, 4);
+    ARCQ_MX8_TILES(3, 2, 4);
+    ARCQ_MX8_TILES(2, 2, 3);
+    ARCQ_MX8_TILES(1, 4, 5);
+    ARCQ_MX8_TILES(1, 2, 4);
+#undef ARCQ_MX8_TILES
+#define ARCQ_MX8_STREAM(MT_, NT_) \
+    if (plan.wm == 0 && plan.mt == MT_ && plan.nt == NT_) return launch_stream<MT_, NT_, TWO>(a, y)
+    ARCQ_MX8_STREAM(1, 1);
+    ARCQ_MX8_STREAM(1, 2);
+    ARCQ_MX8_STREAM(1, 3);
+    ARCQ_MX8_STREAM(1, 4);
+    ARCQ_MX8_STREAM(1, 5);
+    ARCQ_MX8_STREAM(1, 6);
+    ARCQ_MX8_STREAM(1, 7);
+    ARCQ_MX8_STREAM(2, 1);
+    ARCQ_MX8_STREAM(2, 2);
+    ARCQ_MX8_STREAM(2, 3);
+    ARCQ_MX8_STREAM(2, 4);
+#undef ARCQ_MX8_STREAM
+    return fail(ARCQ_HIP_ERROR, "no MXFP8 kernel of %d x %d fragments, %d x %d tiles", plan.wm, plan.wn, plan.mt, plan.nt);
 }
 
 }  // namespace
 
-size_t mx8_gemm_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    const int one = plan_mx8(M, N, K >> 5, K >> 5, false, true).splits, two = plan_mx8(M, N, K >> 5, K >> 5, true, true).splits;
+    const int most = std::max(one, two);
+    return most > 1 ? (size_t)most * (size_t)M * (size_t)N * sizeof(float) : 0;
+}
+
+void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool two_passes, bool workspace, arcq_route* route) {
+    const Mx8Plan p = plan_mx8(M, N, K >> 5, (K + S) >> 5, two_passes, workspace);
+    *route = p.wm ? arcq_route{ARCQ_ROUTE_TILES, 64 * p.wm, 64 * p.wn, p.splits, 0} : arcq_route{ARCQ_ROUTE_STREAM, 16 * p.mt, 16 * p.nt, 1, 0};
+}
 
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
                             int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream) {
-    (void)workspace;
     const Mx8Args a = {a_codes, a_scales, w_codes, w_scales, (int)M, (int)N, (int)(K >> 5), (int)((K + S) >> 5), ldy, stream};
-    return y_dtype == ARCQ_DTYPE_F16 ? launch_typed(a, static_cast<_Float16*>(y)) : launch_typed(a, static_cast<float*>(y));
+    float* partial = static_cast<float*>(workspace);
+    return y_dtype == ARCQ_DTYPE_F16 ? launch_typed(a, static_cast<_Float16*>(y), partial) : launch_typed(a, static_cast<float*>(y), partial);
 }
 
 }  // namespace arcq

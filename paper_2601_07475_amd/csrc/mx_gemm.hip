@@ -11,6 +11,7 @@
 #include "internal.h"
 #include "code_rows.h"
 #include "gemm_decode.h"
+#include "lane_transpose.h"
 #include "lds_dma.h"
 #include "scale_chunks.h"
 #include "tile_order.h"
@@ -531,13 +532,6 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 // leaves every lane with the scale bytes of its block for the four chunks, which the matrix instruction
 // picks with its byte selector.  The address unit of a CU spends about two cycles per (row, 64-byte
 // segment) an instruction touches, so a four-byte scale load per chunk costs as much as the code load.
-typedef unsigned uint2v __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t transpose_scale_bytes(uint32_t s, uint32_t sel_half, uint32_t sel_byte) {
-    const uint2v x = __builtin_amdgcn_permlane32_swap(s, s, false, false);     // (q, q ^ 2): own and partner word
-    const uint32_t pair = __builtin_amdgcn_perm(x[1], x[0], sel_half);         // bytes {0,1} or {2,3} of chunks (q & 1), (q & 1) + 2
-    const uint2v t = __builtin_amdgcn_permlane16_swap(pair, pair, false, false);   // (q, q ^ 1)
-    return __builtin_amdgcn_perm(t[1], t[0], sel_byte);                        // byte q of chunks 0, 1, 2, 3
-}
 
 // weight tiles whose partial sums fit the static LDS limit at a time
 constexpr int mx_skinny_batch(int mt, int nt, int waves) { return waves * mt * nt > 64 ? (nt + 1) / 2 : nt; }
@@ -577,8 +571,7 @@ __device__ __forceinline__ void mx_skinny_tiles(
     int cbase = 0, first_wave = 0;              // first chunk and first wave of the chunk-at-a-time loop
     if constexpr (GRP) {
         const int ngroup = nb >> 4;             // groups of four whole chunks
-        const uint32_t sel_half = q < 2 ? 0x05040100u : 0x07060302u;
-        const uint32_t sel_byte = (q & 1) ? 0x07030501u : 0x06020400u;
+        const uint32_t sel_half = half_selector(q), sel_byte = byte_selector(q);
         for (int g = wave; g < ngroup; g += WAVES) {
             uint4 ca[4][MT], cw[4][NT];
             uint32_t sa[MT], sw[NT];

@@ -158,22 +158,28 @@ def test_rows_of_zeros():
 
 # ------------------------------------------------------------------------------------------------------------------ products
 
-# fp16 products of more than a few rows line up eight products at the largest and drop what is more than 13 bits below its exponent: less than
-# 2^-13 of the largest for each of seven others, 2^-10 of the eight magnitudes' sum
-NATIVE = 2.0 ** -10
-
-
 def assert_product(y, want, mag, K, dropped=0.0):
+    """dropped: what the kernel's summation may lose beside fp32 accumulation, an array like want."""
     got = y.double().cpu().numpy()
     # each of the K / 32 block sums and each addition to the accumulator loses less than a step, 2^-23 of at most mag; joining waves and runs: 64 more
-    bound = mag * ((K / 16 + 64) * 2.0 ** -23 + dropped)
+    bound = mag * (K / 16 + 64) * 2.0 ** -23 + dropped
     if y.dtype is torch.float16:
         bound = bound + (np.abs(want) + bound) * 2.0 ** -11 + 2.0 ** -25        # half a step, of a subnormal too
     over = np.abs(got - want) - bound
     assert np.isfinite(got).all() and over.max() <= 0, f"{over.max()} over the bound at {np.unravel_index(over.argmax(), over.shape)}"
-    rms = np.sqrt(np.mean(want ** 2))
-    err = np.max(np.abs(got - want) / np.maximum(np.abs(want), max(rms, 1e-300)))
-    assert err <= (2e-5 if y.dtype is torch.float32 else 1e-3), err
+    if y.dtype is torch.float32 or np.ndim(dropped) == 0:
+        rms = np.sqrt(np.mean(want ** 2))
+        err = np.max(np.abs(got - want) / np.maximum(np.abs(want), max(rms, 1e-300)))
+        assert err <= (2e-5 if y.dtype is torch.float32 else 1e-3), err
+
+
+def assert_fp16_product(y, ac, asc, wc, wsc, want, mag):
+    """fp16 results of arcq_mx8_gemm: the bits that the matrix unit drops looked up for some rows, bounded for all: less than 2^-13 of the
+    largest of eight products for each of seven others, 2^-10 of the sum of the eight magnitudes."""
+    M, K = ac.shape
+    rows = np.unique(np.linspace(0, M - 1, max(1, min(M, int(4e7) // (wc.shape[0] * K)))).astype(int))
+    assert_product(y[torch.from_numpy(rows).cuda()], want[rows], mag[rows], K, M8.aligned_loss(ac[rows], asc[rows], wc, wsc))
+    assert_product(y, want, mag, K, mag * 2.0 ** -10)
 
 
 def packed_weights(N, K, S, seed, perm=None):
@@ -197,7 +203,10 @@ def run_gemm(M, N, K, S, dtype, seed, extra=0, workspace=True):
     raw, y = output(M, N, dtype, extra)
     B.arcq_mx8_gemm(dev(ac), dev(asc), dev(wc), dev(wsc), y=y, workspace=ws)
     torch.cuda.synchronize()
-    assert_product(y, want, mag, K, NATIVE if dtype is torch.float16 else 0.0)
+    if dtype is torch.float16:
+        assert_fp16_product(y, ac, asc, wc, wsc, want, mag)
+    else:
+        assert_product(y, want, mag, K)
     y.fill_(12345.0)
     assert bool((raw == 12345.0).all())                                 # nothing beside the output
     return need
@@ -215,6 +224,45 @@ GEMM_SHAPES = [(1, 1, 32, 0), (1, 17, 64, 32), (3, 16, 96, 96), (16, 250, 512, 6
 def test_gemm(M, N, K, S, dtype):
     say(f"mx8_gemm M={M} N={N} K={K} S={S} {dtype}")
     run_gemm(M, N, K, S, dtype, seed=M + K, extra=(N * 7) % 5, workspace=(M + N) % 2 == 0)
+
+
+F16, F32 = torch.float16, torch.float32
+# M, N, K, S, type, workspace, (kernel, tile rows, tile columns, runs): every tile, K off its unit of 128 so that rows of scale bytes start at any address
+TILE_SHAPES = [(154, 66, 1888, 0, F16, True, (B.ROUTE_TILES, 64, 128, 3)), (149, 69, 2016, 96, F32, True, (B.ROUTE_TILES, 64, 128, 4)),
+               (1306, 2949, 544, 0, F16, False, (B.ROUTE_TILES, 64, 256, 1)), (6055, 261, 544, 0, F32, False, (B.ROUTE_TILES, 64, 256, 1)),
+               (6055, 261, 544, 0, F16, False, (B.ROUTE_TILES, 128, 128, 1)), (393, 8112, 608, 0, F32, False, (B.ROUTE_TILES, 128, 128, 1)),
+               (2113, 2756, 544, 96, F16, False, (B.ROUTE_TILES, 128, 256, 1)), (2113, 2756, 544, 96, F32, False, (B.ROUTE_TILES, 128, 256, 1)),
+               (6552, 555, 544, 0, F16, False, (B.ROUTE_TILES, 192, 128, 1)), (6552, 555, 544, 0, F32, False, (B.ROUTE_TILES, 192, 128, 1)),
+               (2965, 2695, 544, 96, F16, False, (B.ROUTE_TILES, 192, 256, 1)), (2965, 2695, 544, 96, F32, False, (B.ROUTE_TILES, 192, 256, 1)),
+               (7457, 1649, 544, 0, F16, False, (B.ROUTE_TILES, 256, 256, 1)),
+               (520, 2050, 8224, 0, F16, True, (B.ROUTE_TILES, 128, 128, 3)), (300, 4100, 8224, 0, F32, True, (B.ROUTE_TILES, 64, 256, 3)),
+               (520, 4100, 6176, 0, F32, True, (B.ROUTE_TILES, 128, 256, 3))]
+
+
+@pytest.mark.parametrize("M,N,K,S,dtype,workspace,route", TILE_SHAPES)
+def test_gemm_tiles(M, N, K, S, dtype, workspace, route):
+    say(f"mx8_gemm M={M} N={N} K={K} S={S} {dtype} on {route}")
+    assert B.arcq_mx8_gemm_route(M, N, K, S, dtype, workspace) == route
+    run_gemm(M, N, K, S, dtype, seed=M, extra=3, workspace=workspace)
+
+
+def test_gemm_scale_bytes_at_any_address():
+    """Scale bytes of both operands at odd addresses of their own, on tiles and streamed."""
+    say("mx8_gemm, scale bytes at odd addresses")
+    for M, N, K, S in ((200, 300, 1056, 32), (5, 300, 1056, 32), (129, 257, 2048, 0)):
+        X = wk.activations(wk.Workload("t", M, K, N, 0, 10, "loguniform20_100", 0.02, 5))
+        ac, asc = M8.quantize_act(X)
+        wc, wsc = packed_weights(N, K, S, 6)
+        want, mag = M8.gemm(ac, asc, wc, wsc)
+        buf = [torch.full((t.size + 8,), 0xFF, dtype=torch.uint8, device="cuda") for t in (asc, wsc)]      # 0xFF: NaN, beside the operands
+        for offs in ((1, 2), (3, 1), (2, 3)):
+            views = []
+            for b, o, t in zip(buf, offs, (asc, wsc)):
+                b.fill_(0xFF)
+                views.append(b[o:o + t.size].view(t.shape))
+                views[-1].copy_(dev(t))
+            y = B.arcq_mx8_gemm(dev(ac), views[0], dev(wc), views[1], out_dtype=torch.float32)
+            assert_product(y, want, mag, K)
 
 
 @pytest.mark.parametrize("up", [0, 1])

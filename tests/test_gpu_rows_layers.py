@@ -11,7 +11,7 @@ from paper_2601_07475_amd import binding as B
 from paper_2601_07475_amd import workloads as wk
 
 from test_gpu_graph import _replays_match
-from test_gpu_mx8 import NATIVE, assert_product
+from test_gpu_mx8 import assert_fp16_product, assert_product
 from test_gpu_parity import assert_same_bytes, dev, say
 
 pytestmark = pytest.mark.gpu
@@ -44,13 +44,13 @@ def test_mlp_with_8_bit_activations(M):
     assert_same_bytes(s.cpu().numpy(), wsc, "scales")
     assert np.array_equal(r.cpu().numpy(), wh)
     y = B.arcq_mx8_gemm(c, s, *up)
-    assert_product(y, *M8.gemm(wc, wsc, *m["up"]), D, NATIVE)
+    assert_fp16_product(y, wc, wsc, *m["up"], *M8.gemm(wc, wsc, *m["up"]))
     c, s = B.arcq_mx8_quantize_act(y, pd)
     wc, wsc = M8.quantize_act(y.cpu().numpy(), m["p_down"])
     assert_same_bytes(c.cpu().numpy(), wc, "codes")
     assert_same_bytes(s.cpu().numpy(), wsc, "scales")
     z = B.arcq_mx8_gemm(c, s, *down)
-    assert_product(z, *M8.gemm(wc, wsc, *m["down"]), FF, NATIVE)
+    assert_fp16_product(z, wc, wsc, *m["down"], *M8.gemm(wc, wsc, *m["down"]))
     zn = z.cpu().numpy()
     c, s, h = B.arcq_mx8_add_rmsnorm_quantize_act(z, r, g, 1e-5, pu, hidden=z)
     wc, wsc, wh = M8.add_rmsnorm_quantize_act(zn, wh, m["gamma"], 1e-5, m["p_up"])

@@ -94,3 +94,15 @@ def test_reorder_norm_and_products_as_identities():
     assert np.array_equal(M8.gemv(X, perm, gc, gs)[0], X.astype(np.float64) @ grid.T)
     nc, ns = A.pack_weight(grid.astype(np.float16), perm, S, np.float32(1.0))
     assert np.array_equal(M8.gemv(X, perm, nc, ns, np.float32(1.0))[0], X.astype(np.float64) @ grid.T)
+
+
+def test_aligned_loss_by_hand():
+    """One group: exponents of 448 (8) and 6 (2) on top, 2^(10 - 13) for each of seven others, times the blocks' scales."""
+    ac, asc = np.zeros((1, 32), np.uint8), np.array([[128]], np.uint8)
+    ac[0, 0], ac[0, 1] = 0x7E, 0x01                                         # 448, 2^-9
+    wc, wsc = np.zeros((2, 16), np.uint8), np.array([[127], [126]], np.uint8)
+    wc[:, 0] = 0x17                                                         # 6, 0.5
+    assert np.array_equal(M8.aligned_loss(ac, asc, wc, wsc), [[7 * 2.0 ** -3 * 2, 7 * 2.0 ** -3]])
+    ac[0, 0] = 0                                                            # what is left: the subnormal, exponents -6 and 0
+    assert np.array_equal(M8.aligned_loss(ac, asc, wc, wsc), [[7 * 2.0 ** -19 * 2, 7 * 2.0 ** -19]])
+    assert not M8.aligned_loss(np.zeros_like(ac), asc, wc, wsc).any()
