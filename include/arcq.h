@@ -338,7 +338,7 @@ arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales,
  * that arcq_pack_weight (arcq_gemv) or arcq_mx_pack_weight (arcq_mx_gemv) made for the 4-bit path:
  *   y[m, n] = w_tensor_scale * sum_{b < K/16} sw[n,b] sum_{i<16} x[m, perm[16b+i]] qw[n,16b+i]           (MXFP4: blocks of 32, no tensor scale)
  * with fp32 accumulation; the weights are used as they are packed, x is not rounded.
- * x     fp16 [M, K], pitch ldx, 16-byte aligned, ldx % 8 == 0.  Any M; made for up to 64 rows (more take the weights once for every 64).
+ * x     fp16 [M, K], pitch ldx, 16-byte aligned, ldx % 8 == 0.  Any M; made for up to 32 rows (more take the weights once for every 32).
  * perm  int32 [K], 16-byte aligned: the order that the weights were packed with, or NULL where they were packed in the channels' own.
  *       With entries outside 0..K-1 the output is unspecified; no global memory outside the arguments is touched.
  * w_*   packed weights [N, K + S] in the plain layout (not ARCQ_LAYOUT_INTERLEAVED with S > 0), codes 8-byte aligned; the S columns that

@@ -10,10 +10,27 @@
 // A chunk is 128 k.  Lane (i = lane % 16, q = lane / 16) loads 16 bytes of codes of weight row i (a wave: 16 rows x 64 contiguous bytes) and
 // a 4 x 4 transpose of words across the four lane groups (four lane-swap instructions) leaves it with word q of the chunk's blocks of 32 k:
 // word j is k = 32 j + 8 q .. + 7, for which the rows' 16 bytes of the four lane groups are contiguous, too.
+//
+// Loads return in the order they were asked for, so whatever is asked for behind the weights waits for them.  The rows are therefore asked for first
+// and reach the matrix instructions through LDS (X):
+//   SLICE   a wave brings what it multiplies next, 4 to 16 KB of its own, while it multiplies.  Rows that have to be reordered are so by a launch
+//           before, 2.2 to 3 us
+//   WHOLE   short rows that have to be reordered: all of them at once, in the order that lanes read them in (a unit of 16 bytes per eight k and
+//           row), 0.5 to 1.5 us; one row of 4096 channels over 4096 features 6.1 us where SLICE takes 4.7 without an order
+//
+// Measured (weights not in cache, rows in order; us, and TB/s of weights):     M = 1         M = 4         M = 16        M = 32
+//   NVFP4   4096 features,  4096 channels                                    4.7   2.0     5.0   1.9     6.6   1.4     8.4   1.1
+//          27648            5120                                            20.9   3.8    24.6   3.2    29.7   2.7    43.6   1.8
+//           8192           28672                                            29.9   4.4    35.8   3.7    42.6   3.1    59.8   2.2
+//   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    16.1   1.9    21.8   1.4
+// From 1 to 4 rows the weights' way from memory and the tiles' uneven shares bound it, with more the rows, too: every workgroup reads all of them
+// (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).  K split over workgroups would take that back but for a second launch
+// that adds up partial results: 16 rows, 4096 x 14336 15.3 us instead of 16.3, nothing elsewhere up to 27648 x 5120, so it is not there.
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
 #include "lane_transpose.h"
+#include "lds_dma.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -23,12 +40,6 @@ namespace arcq {
 namespace {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
-__device__ __forceinline__ uint4 load16_a1(const uint8_t* p) {
-    const u32x4 v = *reinterpret_cast<const u32x4_a1*>(p);
-    return uint4{v[0], v[1], v[2], v[3]};
-}
-
 // Eight codes -> fp16, unscaled.
 __device__ __forceinline__ half8 widen8(uint32_t c) {
     const half2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 1),
@@ -38,152 +49,326 @@ __device__ __forceinline__ half8 widen8(uint32_t c) {
 // E8M0 byte -> 2^(byte - 127); byte 0 is a subnormal.
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte != 0 ? byte << 23 : 0x400000u); }
 
-// The scale bytes of a chunk that a lane needs, one for each word: the same for all lane groups (MXFP4), or those of
-// its half of the words' blocks of 32 k.
+// Scale bytes of a group of four chunks: lane group q loads chunk q's; every lane gets those it needs of all four, one for each word: all
+// bytes of a chunk (MXFP4), or those of its half of the words' blocks of 32 k (NVFP4: even ones for q < 2, odd ones for the others).
+__device__ __forceinline__ void spread(uint32_t lower, uint32_t upper, uint32_t (&out)[4]) {
+    const uint2v a = __builtin_amdgcn_permlane32_swap(lower, upper, false, false);      // of lane groups q & 1 and (q & 1) + 2
+    const uint2v x = __builtin_amdgcn_permlane16_swap(a[0], a[0], false, false), y = __builtin_amdgcn_permlane16_swap(a[1], a[1], false, false);
+    out[0] = x[0], out[1] = x[1], out[2] = y[0], out[3] = y[1];
+}
 template <int B>
-__device__ __forceinline__ uint32_t scales_of_chunk(uint32_t lo, uint32_t hi, uint32_t half_select) {
-    return B == 32 ? lo : __builtin_amdgcn_perm(hi, lo, half_select);
+__device__ __forceinline__ void scales_of_group(uint2 s, uint32_t (&out)[4]) {
+    if constexpr (B == 32) spread(s.x, s.x, out);
+    else spread(__builtin_amdgcn_perm(s.y, s.x, 0x06040200u), __builtin_amdgcn_perm(s.y, s.x, 0x07050301u), out);
 }
 
-// One chunk of MT row tiles and NT weight tiles.
-template <int B, int MT, int NT>
-__device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[MT][NT]) {
+// One chunk of MT row tiles and NT weight tiles.  NVFP4: words 0 and 2, 1 and 3 have accumulators of their own (CH = 2) where a single chain of dependent products
+// would make every one wait for the one before.
+template <int B, int MT, int NT, int CH>
+__device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[CH][MT][NT]) {
+    half8 w[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         transpose_words(cw[t]);
         const uint32_t word[4] = {cw[t].x, cw[t].y, cw[t].z, cw[t].w};
-        if constexpr (B == 16) {
-            const uint32_t s01 = scale_halves(sw[t], 0x0C010C00), s23 = scale_halves(sw[t], 0x0C030C02);
+        const uint32_t s01 = B == 16 ? scale_halves(sw[t], 0x0C010C00) : 0u, s23 = B == 16 ? scale_halves(sw[t], 0x0C030C02) : 0u;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const half8 w = decode8_half(word[j], j < 2 ? s01 : s23, j & 1);
+        for (int j = 0; j < 4; ++j) w[t][j] = B == 16 ? decode8_half(word[j], j < 2 ? s01 : s23, j & 1) : widen8(word[j]);
+    }
+    if constexpr (B == 16) {
 #pragma unroll
-                for (int r = 0; r < MT; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w, acc[r][t], 0, 0, 0);
-            }
-        } else {
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const half8 w = widen8(word[j]);
-                const float s = power_of(sw[t] >> (8 * j) & 0xFFu);     // of weight row lane % 16, the column that the lane holds sums of
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int r = 0; r < MT; ++r) {
-                    const float4v sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w, float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                for (int r = 0; r < MT; ++r)
+                    acc[j % CH][r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w[t][j], acc[j % CH][r][t], 0, 0, 0);
+    } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[r][t][e] = __builtin_fmaf(sum[e], s, acc[r][t][e]);
+        for (int r = 0; r < MT; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float4v sum[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w[t][j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float s = power_of(sw[t] >> (8 * j) & 0xFFu);     // of weight row lane % 16, the column that the lane holds sums of
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[0][r][t][e] = __builtin_fmaf(sum[j][e], s, acc[0][r][t][e]);
                 }
             }
-        }
     }
 }
 
+enum Rows { WHOLE, SLICE };
+constexpr int WAVES = 8, THREADS = 64 * WAVES;
+// Tiles of 16 weight rows of a workgroup: two or four share the rows where there are enough of them for every compute unit.
+//   16 rows, NT = 1, 2, 4: 14336 x 4096 18.6, 13.4, 11.4 us; 27648 x 5120 47.7, 30.0, 29.7; 8192 x 28672 60, 43, 64; 4096 x 4096 6.8, 8.0, 10.3
+//   32 rows, NT = 1, 2:    14336 x 4096 23.7, 17.0 us; 8192 x 28672 87, 60; 4096 x 4096 8.4, 10.5
+// Up to 4 rows, one: registers then allow two workgroups on a compute unit (14336 x 4096 10.8 -> 10.1 us).
+constexpr int slice_chunks(int rows, int nt) { return rows == 4 ? 4 : rows == 16 ? (nt == 1 ? 4 : nt == 2 ? 2 : 1) : 1; }     // of a wave, as registers allow
+constexpr int slice_bytes(int rows, int nt) { return rows * slice_chunks(rows, nt) * 256; }
+constexpr int kPieces = 2;                      // WHOLE: 16-byte pieces of the rows per thread
+
 // B      16: NVFP4, 32: MXFP4
-// MT     tiles of 16 rows of x that share every decoded weight;  NT  tiles of 16 weight rows of a workgroup, whose WAVES waves split K
-template <int B, int MT, int NT, int WAVES, typename OutT>
-__global__ __launch_bounds__(WAVES * 64) void gemv_kernel(
-    const uint16_t* __restrict__ x, int64_t ldx, int M, int K, const uint8_t* __restrict__ w_codes, const uint8_t* __restrict__ w_scales,
-    int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n) {
-    __shared__ float red[WAVES][MT * NT][4][64];
-    static_assert(sizeof(red) <= 64 * 1024, "partial tiles must fit the static LDS limit");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+// ROWS   most rows of x of a workgroup: 4, 16 or 32, in tiles of 16 that share every decoded weight
+// NT     tiles of 16 weight rows of a workgroup, whose WAVES waves split K
+// LDS: the rows (WHOLE: M K 2 bytes twice, the second in the channels' own order), then the waves' partial tiles, two sets
+template <int B, int ROWS, int NT, int X, typename OutT>
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS == 4 ? 4 : 2, 4))) void gemv_kernel(
+    const uint16_t* __restrict__ x, int64_t ldx, int M, int K, const int32_t* __restrict__ perm, const uint8_t* __restrict__ w_codes,
+    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride) {
+    constexpr int MT = (ROWS + 15) / 16;
+    static_assert(X == SLICE || MT == 1, "WHOLE: up to 16 rows");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i = lane & 15, q = lane >> 4;
-    const int n0 = (int)(blockIdx.x % tiles_n) * (16 * NT), m0 = (int)(blockIdx.x / tiles_n) * (16 * MT);
+    // a workgroup takes every stride-th tile of weight rows, for one tile of rows of x
+    const int m0 = (int)(blockIdx.x / stride) * ROWS, tile0 = (int)(blockIdx.x % stride);
     constexpr int SB = 128 / B;                     // scale bytes of a chunk
-    const uint32_t half_select = q < 2 ? 0x06040200u : 0x07050301u;
+    const int rows = min(M - m0, ROWS), pieces = K >> 3;
 
-    const uint16_t* xr[MT];
-#pragma unroll
-    for (int r = 0; r < MT; ++r) xr[r] = x + (int64_t)min(m0 + 16 * r + i, M - 1) * ldx;      // rows past M repeat row M-1 and are not stored
-    const uint8_t *wc[NT], *ws[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int n = min(n0 + 16 * t + i, N - 1);
-        wc[t] = w_codes + n * cpitch;
-        ws[t] = w_scales + n * spitch;
-    }
-    float4v acc[MT][NT];
-#pragma unroll
-    for (int r = 0; r < MT; ++r)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+    // Whole chunks of 128 k go to the waves four at a time, in turn, and what is left of them in equal shares.
+    const int whole = K >> 7, rounds = whole / (4 * WAVES), rest = whole - rounds * 4 * WAVES;
+    const int rest0 = 4 * WAVES * rounds + wave * rest / WAVES, rest1 = 4 * WAVES * rounds + (wave + 1) * rest / WAVES;
+    const int turns = rounds + (rest1 > rest0 ? 1 : 0);
+    auto first_of = [&](int turn) { return turn < rounds ? 4 * (turn * WAVES + wave) : rest0; };
+    auto count_of = [&](int turn) { return turn < rounds ? 4 : turn == rounds ? rest1 - rest0 : 0; };
 
-    // whole chunks, four at a time
-    const int groups = K >> 9;
-    for (int g = wave; g < groups; g += WAVES) {
-        uint4 cw[4][NT], sc[NT][B == 16 ? 2 : 1];
+    // ---- the rows
+    u32x4 piece_x[X == WHOLE ? kPieces : 1];
+    uint32_t chan[X == WHOLE ? kPieces : 1][4];     // source channels of a piece, two to a register
+    if constexpr (X == WHOLE) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            sc[t][0] = load16_a1(ws[t] + (int64_t)(4 * SB) * g);
-            if constexpr (B == 16) sc[t][1] = load16_a1(ws[t] + (int64_t)(4 * SB) * g + 16);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) cw[c][t] = load16_a4(wc[t] + 256 * (int64_t)g + 64 * c + 16 * q);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            half8 xf[MT][4];
-#pragma unroll
-            for (int r = 0; r < MT; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(xr[r] + 512 * (int64_t)g + 128 * c + 32 * j + 8 * q);
-            uint32_t sw[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if constexpr (B == 16) {
-                    const uint4& s = sc[t][c >> 1];
-                    sw[t] = scales_of_chunk<B>(c & 1 ? s.z : s.x, c & 1 ? s.w : s.y, half_select);
-                } else {
-                    const uint4& s = sc[t][0];
-                    sw[t] = c == 0 ? s.x : c == 1 ? s.y : c == 2 ? s.z : s.w;
-                }
+        for (int p = 0; p < kPieces; ++p) {
+            const int u = tid + p * THREADS;
+            if (u < pieces) {
+                const int4 a = *reinterpret_cast<const int4*>(perm + 8 * u), b = *reinterpret_cast<const int4*>(perm + 8 * u + 4);
+                // (an index from an unchecked perm may lie outside the row)
+                auto two = [&](int lo, int hi) { return min((uint32_t)lo, (uint32_t)K - 1u) | min((uint32_t)hi, (uint32_t)K - 1u) << 16; };
+                chan[p][0] = two(a.x, a.y), chan[p][1] = two(a.z, a.w), chan[p][2] = two(b.x, b.y), chan[p][3] = two(b.z, b.w);
             }
-            multiply_chunk<B, MT, NT>(xf, cw[c], sw, acc);
+        }
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const int u = tid + p * THREADS;
+            if (u < rows * pieces) {
+                const int m = rows == 1 ? 0 : u / pieces;
+                piece_x[p] = *reinterpret_cast<const u32x4*>(x + (int64_t)(m0 + m) * ldx + 8 * (u - m * pieces));
+            }
         }
     }
-    // what is left of K, a chunk at a time: blocks past the end count as zero codes, and rows of x are read from their start there
-    const int blocks = K / B, chunks = (K + 127) >> 7;
-    for (int c = 4 * groups + (wave - groups % WAVES + WAVES) % WAVES; c < chunks; c += WAVES) {
-        uint4 cw[NT];
-        uint32_t sw[NT];
-        const int b0 = B == 16 ? 8 * c + 2 * q : 4 * c + q;
+    // SLICE: piece (eight k) and row at unit ROWS piece + (row ^ swizzle), so that writes of a row and reads of a piece both spread over the
+    // banks.  A load instruction brings a row, or two, whole lines of each.
+    constexpr int XC = slice_chunks(ROWS, NT), LPR = 16 * XC, RPL = 64 / LPR, LOADS = ROWS / RPL;     // chunks of a slice; lanes of a row; rows of a load
+    auto unit = [](int piece, int row) { return ROWS * piece + (row ^ (ROWS == 4 ? piece >> 2 & 3 : piece & 15)); };
+    uint8_t* slice = lds + (X == SLICE ? wave * slice_bytes(ROWS, NT) : 0);
+    u32x4 xv[X == SLICE ? LOADS : 1];
+    auto load_x = [&](int c) {
+        if constexpr (X == SLICE) {
+            const int piece = min(16 * c + lane % LPR, pieces - 1);
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l)
+                if (RPL * l < rows) xv[l] = *reinterpret_cast<const u32x4*>(x + (int64_t)min(m0 + RPL * l + lane / LPR, M - 1) * ldx + 8 * piece);
+        }
+    };
+    auto put_x = [&]() {
+        if constexpr (X == SLICE) {
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l)
+                if (RPL * l < rows) *reinterpret_cast<u32x4*>(slice + 16 * unit(lane % LPR, RPL * l + lane / LPR)) = xv[l];
+        }
+    };
+    if (turns > 0) load_x(first_of(0));
+    __builtin_amdgcn_sched_barrier(0);
+
+    // ---- the weights
+    // of the tile whose codes, and of the one whose scales, are asked for
+    const uint8_t *wc[NT], *ws[NT];
+    auto rows_of = [&](const uint8_t* base, int64_t pitch, int tile, const uint8_t* (&at)[NT]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) at[t] = base + min((tile * NT + t) * 16 + i, N - 1) * pitch;
+    };
+    rows_of(w_codes, cpitch, tile0, wc);
+    rows_of(w_scales, spitch, tile0, ws);
+    auto load_scales = [&](int c, int count, u32x2 (&sc)[NT]) {      // (past the end: the last chunk's again)
+        const int64_t at = (int64_t)SB * (c + min(q, count - 1));
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if constexpr (B == 16) {
-                const uint2 lo = load8_a8(wc[t] + 8 * (int64_t)min(b0, blocks - 1)), hi = load8_a8(wc[t] + 8 * (int64_t)min(b0 + 1, blocks - 1));
-                const bool ok0 = b0 < blocks, ok1 = b0 + 1 < blocks;
-                cw[t] = make_uint4(ok0 ? lo.x : 0, ok0 ? lo.y : 0, ok1 ? hi.x : 0, ok1 ? hi.y : 0);
+                const uint2 v = load8_a1(ws[t] + at);
+                sc[t] = u32x2{v.x, v.y};
             } else {
-                const uint4 v = load16_a4(wc[t] + 16 * (int64_t)min(b0, blocks - 1));
-                const bool ok = b0 < blocks;
-                cw[t] = make_uint4(ok ? v.x : 0, ok ? v.y : 0, ok ? v.z : 0, ok ? v.w : 0);
+                sc[t] = u32x2{load4_a1(ws[t] + at), 0u};
             }
-            sw[t] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sw[t] |= (uint32_t)ws[t][min(B == 16 ? 8 * c + 2 * j + (q >> 1) : 4 * c + j, blocks - 1)] << (8 * j);
         }
-        half8 xf[MT][4];
+    };
+    auto load_codes = [&](int c, u32x4 (&cw)[NT]) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = 128 * c + 32 * j + 8 * q;
+        for (int t = 0; t < NT; ++t) cw[t] = *reinterpret_cast<const u32x4_a4*>(wc[t] + 64 * (int64_t)c + 16 * q);
+    };
+    constexpr int AHEAD = MT * NT == 4 ? 2 : 4;          // chunks in flight
+    u32x4 cw[AHEAD][NT];
+    u32x2 sc[NT];
+    if (turns > 0) {
+        load_scales(first_of(0), count_of(0), sc);
 #pragma unroll
-            for (int r = 0; r < MT; ++r) xf[r][j] = *reinterpret_cast<const half8*>(xr[r] + (k < K ? k : 0));
-        }
-        multiply_chunk<B, MT, NT>(xf, cw, sw, acc);
+        for (int d = 0; d < AHEAD; ++d)
+            if (d < count_of(0)) load_codes(first_of(0) + d, cw[d]);
     }
+    __builtin_amdgcn_sched_barrier(0);
+
+    if constexpr (X == WHOLE) {
+        uint8_t* to = lds + (size_t)rows * K * 2;
 #pragma unroll
-    for (int r = 0; r < MT; ++r)
+        for (int p = 0; p < kPieces; ++p) {
+            const int u = tid + p * THREADS;
+            if (u < rows * pieces) *reinterpret_cast<u32x4*>(to + 16 * u) = piece_x[p];
+        }
+        wait_lgkmcnt0();
+        wg_barrier();                               // not __syncthreads(): the weights stay in flight
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int p = 0; p < kPieces; ++p) {
+            const int piece = tid + p * THREADS;
+            if (piece < pieces)
+                for (int m = 0; m < rows; ++m) {
+                    auto at = [&](uint32_t ch) { return (uint32_t)*reinterpret_cast<const uint16_t*>(to + 2 * ((uint32_t)m * (uint32_t)K + ch)); };
+                    u32x4 v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][r * NT + t][e][lane] = acc[r][t][e];
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < MT * NT * 4 * 64; idx += WAVES * 64) {
-        const int rt = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
-        float sum = 0.f;
+                    for (int w = 0; w < 4; ++w) v[w] = at(chan[p][w] & 0xFFFFu) | at(chan[p][w] >> 16) << 16;
+                    *reinterpret_cast<u32x4*>(lds + 16 * (piece * rows + m)) = v;
+                }
+        }
+        wait_lgkmcnt0();
+        wg_barrier();
+    }
+    // the lane's fragments of chunk c, the d-th of its four
+    auto take_x = [&](int c, int d, half8 (&xf)[MT][4]) {
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum += red[w][rt][e][l];
-        const int m = m0 + 16 * (rt / NT) + 4 * (l >> 4) + e, n = n0 + 16 * (rt % NT) + (l & 15);
-        if (m < M && n < N) store_out(y + (int64_t)m * ldy + n, sum * alpha);
+        for (int r = 0; r < MT; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (X == WHOLE) {
+                    xf[r][j] = *reinterpret_cast<const half8*>(lds + 16 * ((16 * c + 4 * j + q) * rows + min(i, rows - 1)));
+                } else {
+                    xf[r][j] = *reinterpret_cast<const half8*>(slice + 16 * unit(16 * (d % XC) + 4 * j + q, ROWS == 4 ? i & 3 : 16 * r + i));
+                }
+            }
+    };
+    constexpr int CH = B == 16 && ROWS == 16 && NT == 1 ? 2 : 1;
+    // Partial tiles have two buffers behind the rows, so that a barrier a tile is enough.  The next tile's weights are asked for while this one's are
+    // multiplied and added up.
+    float* red = reinterpret_cast<float*>(lds + (X == WHOLE ? (uint32_t)rows * (uint32_t)K * 4u : (uint32_t)(WAVES * slice_bytes(ROWS, NT))));
+    uint32_t turn_red = 0;
+    for (int tile = tile0; tile < tiles_n; tile += (int)stride) {
+        float4v acc[CH][MT][NT];
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int r = 0; r < MT; ++r)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[c][r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+
+        for (int turn = 0; turn < turns; ++turn) {
+            const bool over = turn + 1 == turns;
+            const int c = first_of(turn), count = count_of(turn);
+            const int next = first_of(over ? 0 : turn + 1);
+            const int next_count = !over ? count_of(turn + 1) : tile + (int)stride < tiles_n ? count_of(0) : 0;
+            const bool next_tile = over && next_count > 0;
+            if (next_tile) rows_of(w_scales, spitch, tile + (int)stride, ws);
+            uint32_t sw[4][NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                uint32_t s[4];
+                scales_of_group<B>(make_uint2(sc[t][0], sc[t][1]), s);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) sw[d][t] = s[d];
+            }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                if (d < count) {
+                    if (d % XC == 0) {
+                        put_x();
+                        if (d + XC < count) load_x(c + d + XC);
+                        else if (next_count > 0) load_x(next);
+                    }
+                    if (d == 0 && next_count > 0) load_scales(next, next_count, sc);
+                    half8 xf[MT][4];
+                    take_x(c + d, d, xf);
+                    uint4 words[NT];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) words[t] = make_uint4(cw[d % AHEAD][t][0], cw[d % AHEAD][t][1], cw[d % AHEAD][t][2], cw[d % AHEAD][t][3]);
+                    multiply_chunk<B, MT, NT, CH>(xf, words, sw[d], acc);
+                }
+                // AHEAD chunks ahead, as soon as there is room
+                if (d + AHEAD == 4 && next_tile) rows_of(w_codes, cpitch, tile + (int)stride, wc);
+                if (d + AHEAD < 4) {
+                    if (d + AHEAD < count) load_codes(c + d + AHEAD, cw[d % AHEAD]);
+                } else if (d + AHEAD - 4 < next_count) {
+                    load_codes(next + d + AHEAD - 4, cw[d % AHEAD]);
+                }
+            }
+        }
+        // What is left of K, less than a chunk, is for the first wave (the last one has the most): blocks past the end count as zero codes, and rows of x
+        // are read from their start there.
+        const int blocks = K / B;
+        if ((K & 127) != 0 && wave == 0) {
+            int c = whole;
+            asm volatile("" : "+v"(c));             // (its addresses, the same for every tile, are not worth registers in between)
+            const uint8_t *tc[NT], *ts[NT];
+            rows_of(w_codes, cpitch, tile, tc);
+            rows_of(w_scales, spitch, tile, ts);
+            uint4 words[NT];
+            uint32_t sw[NT];
+            const int b0 = B == 16 ? 8 * c + 2 * q : 4 * c + q;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if constexpr (B == 16) {
+                    const uint2 lo = load8_a8(tc[t] + 8 * (int64_t)min(b0, blocks - 1)), hi = load8_a8(tc[t] + 8 * (int64_t)min(b0 + 1, blocks - 1));
+                    const bool ok0 = b0 < blocks, ok1 = b0 + 1 < blocks;
+                    words[t] = make_uint4(ok0 ? lo.x : 0, ok0 ? lo.y : 0, ok1 ? hi.x : 0, ok1 ? hi.y : 0);
+                } else {
+                    const uint4 v = load16_a4(tc[t] + 16 * (int64_t)min(b0, blocks - 1));
+                    const bool ok = b0 < blocks;
+                    words[t] = make_uint4(ok ? v.x : 0, ok ? v.y : 0, ok ? v.z : 0, ok ? v.w : 0);
+                }
+                sw[t] = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sw[t] |= (uint32_t)ts[t][min(B == 16 ? 8 * c + 2 * j + (q >> 1) : 4 * c + j, blocks - 1)] << (8 * j);
+            }
+            half8 xf[MT][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int piece = 16 * c + 4 * j + q, at = piece < pieces ? piece : 0;
+#pragma unroll
+                for (int r = 0; r < MT; ++r) {
+                    const int m = min(16 * r + i, rows - 1);            // rows past M repeat the last one and are not stored
+                    if constexpr (X == WHOLE) xf[r][j] = *reinterpret_cast<const half8*>(lds + 16 * (at * rows + m));
+                    else xf[r][j] = *reinterpret_cast<const half8*>(x + (int64_t)(m0 + m) * ldx + 8 * at);
+                }
+            }
+            multiply_chunk<B, MT, NT, CH>(xf, words, sw, acc);
+        }
+        float* part = red + turn_red * (WAVES * MT * NT * 256);
+        turn_red ^= 1u;
+#pragma unroll
+        for (int r = 0; r < MT; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    part[((wave * MT * NT + r * NT + t) * 4 + e) * 64 + lane] = CH == 2 ? acc[0][r][t][e] + acc[CH - 1][r][t][e] : acc[0][r][t][e];
+        wait_lgkmcnt0();
+        wg_barrier();                                   // not __syncthreads(): the next tile's weights stay in flight
+        for (int idx = tid; idx < MT * NT * 4 * 64; idx += THREADS) {
+            const int rt = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) sum += part[(w * MT * NT * 4 + rt * 4 + e) * 64 + l];
+            const int m = m0 + 16 * (rt / NT) + 4 * (l >> 4) + e, n = (tile * NT + rt % NT) * 16 + (l & 15);
+            if (m < min(M, m0 + ROWS) && n < N) store_out(y + (int64_t)m * ldy + n, sum * alpha);
+        }
     }
 }
 
@@ -201,63 +386,69 @@ __global__ __launch_bounds__(256) void reorder_rows_kernel(const uint16_t* __res
     *reinterpret_cast<uint4*>(out + (int64_t)m * K + at) = make_uint4(take(a.x, a.y), take(a.z, a.w), take(b.x, b.y), take(b.z, b.w));
 }
 
-template <int B, int MT, int NT, typename OutT>
-arcq_status launch_tiles(const uint16_t* x, int64_t ldx, int64_t M, int64_t K, const uint8_t* w_codes, const uint8_t* w_scales, int64_t N,
-                         int64_t S, float alpha, OutT* y, int64_t ldy, hipStream_t stream) {
-    const unsigned tiles_n = (unsigned)((N + 16 * NT - 1) / (16 * NT)), tiles_m = (unsigned)((M + 16 * MT - 1) / (16 * MT));
-    hipLaunchKernelGGL((gemv_kernel<B, MT, NT, 8, OutT>), dim3(tiles_n * tiles_m), dim3(512), 0, stream, x, ldx, (int)M, (int)K, w_codes, w_scales,
-                       (int)N, (K + S) / 2, (K + S) / B, alpha, y, ldy, tiles_n);
+struct GemvArgs {
+    const uint16_t* x;
+    int64_t M, K, ldx;
+    const int32_t* perm;
+    const uint8_t *w_codes, *w_scales;
+    int64_t N, S;
+    float alpha;
+    int64_t ldy;
+    hipStream_t stream;
+};
+
+bool whole_rows(int64_t M, int64_t K) { return M <= 4 && M * K <= 8 * THREADS * kPieces; }
+
+template <int B, int ROWS, int NT, int X, typename OutT>
+arcq_status launch_tiles(const GemvArgs& a, OutT* y) {
+    auto kern = gemv_kernel<B, ROWS, NT, X, OutT>;
+    static std::atomic<uint64_t> lds_raised{0};
+    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+    const size_t rows = X == WHOLE ? (size_t)a.M * a.K * 4 : (size_t)WAVES * slice_bytes(ROWS, NT);
+    const size_t lds = rows + 2 * (size_t)WAVES * ((ROWS + 15) / 16) * NT * 1024;
+    const int64_t tiles_n = (a.N + 16 * NT - 1) / (16 * NT), tiles_m = (a.M + ROWS - 1) / ROWS;
+    const int per_cu = ROWS == 4 && lds <= 80 * 1024 ? 2 : 1;       // as registers and LDS allow
+    const unsigned stride = (unsigned)std::min<int64_t>(tiles_n, (int64_t)num_cu() * per_cu);
+    hipLaunchKernelGGL(kern, dim3(stride * (unsigned)tiles_m), dim3(THREADS), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
+                       a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride);
     return check_launch("gemv_kernel");
 }
 
 template <int B, typename OutT>
-arcq_status launch_typed(const uint16_t* x, int64_t ldx, int64_t M, int64_t K, const uint8_t* w_codes, const uint8_t* w_scales, int64_t N,
-                         int64_t S, float alpha, OutT* y, int64_t ldy, hipStream_t stream) {
-    const int64_t tiles = (N + 15) / 16;
-    const int nt = tiles <= 256 ? 1 : tiles <= 512 || M > 32 ? 2 : 4;
-#define ARCQ_GEMV(MT_, NT_) \
-    if (nt == NT_) return launch_tiles<B, MT_, NT_>(x, ldx, M, K, w_codes, w_scales, N, S, alpha, y, ldy, stream)
-    if (M <= 16) {
-        ARCQ_GEMV(1, 1);
-        ARCQ_GEMV(1, 2);
-        ARCQ_GEMV(1, 4);
-    }
-    if (M <= 32) {
-        ARCQ_GEMV(2, 1);
-        ARCQ_GEMV(2, 2);
-        ARCQ_GEMV(2, 4);
-    }
-    ARCQ_GEMV(4, 1);
-    return launch_tiles<B, 4, 2>(x, ldx, M, K, w_codes, w_scales, N, S, alpha, y, ldy, stream);
-#undef ARCQ_GEMV
-}
-
-template <int B>
-arcq_status launch_format(const uint16_t* x, int64_t ldx, int64_t M, int64_t K, const uint8_t* w_codes, const uint8_t* w_scales, int64_t N,
-                          int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, hipStream_t stream) {
-    if (y_dtype == ARCQ_DTYPE_F16)
-        return launch_typed<B>(x, ldx, M, K, w_codes, w_scales, N, S, alpha, static_cast<_Float16*>(y), ldy, stream);
-    return launch_typed<B>(x, ldx, M, K, w_codes, w_scales, N, S, alpha, static_cast<float*>(y), ldy, stream);
+arcq_status launch_typed(const GemvArgs& a, OutT* y) {
+    const int64_t tiles = (a.N + 15) / 16;
+    const int cus = num_cu();
+    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, WHOLE>(a, y) : launch_tiles<B, 4, 1, SLICE>(a, y);
+    if (a.M <= 16)
+        return tiles <= cus       ? launch_tiles<B, 16, 1, SLICE>(a, y)
+               : tiles <= 2 * cus ? launch_tiles<B, 16, 2, SLICE>(a, y)
+                                  : launch_tiles<B, 16, 4, SLICE>(a, y);
+    return tiles <= cus ? launch_tiles<B, 32, 1, SLICE>(a, y) : launch_tiles<B, 32, 2, SLICE>(a, y);
 }
 
 }  // namespace
 
-size_t gemv_workspace_bytes(int64_t M, int64_t K, bool reorder) { return reorder ? (size_t)M * (size_t)K * 2 : 0; }
+// Rows in the weights' order, where no kernel reorders them on the way.
+size_t gemv_workspace_bytes(int64_t M, int64_t K, bool reorder) {
+    return reorder && !whole_rows(M, K) ? (size_t)M * (size_t)K * 2 : 0;
+}
 
 arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
                         const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
                         hipStream_t stream) {
-    const uint16_t* rows = static_cast<const uint16_t*>(x);
-    if (perm) {
+    GemvArgs a = {static_cast<const uint16_t*>(x), M, K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream};
+    if (gemv_workspace_bytes(M, K, perm != nullptr) > 0) {
         uint16_t* reordered = static_cast<uint16_t*>(workspace);
         const unsigned parts = (unsigned)((K / 8 + 255) / 256);
-        hipLaunchKernelGGL(reorder_rows_kernel, dim3(parts * (unsigned)M), dim3(256), 0, stream, rows, ldx, (int)K, perm, reordered, parts);
+        hipLaunchKernelGGL(reorder_rows_kernel, dim3(parts * (unsigned)M), dim3(256), 0, stream, a.x, ldx, (int)K, perm, reordered, parts);
         if (arcq_status st = check_launch("reorder_rows_kernel")) return st;
-        rows = reordered;
-        ldx = K;
+        a.x = reordered;
+        a.ldx = K;
+        a.perm = nullptr;
     }
-    if (block == 16) return launch_format<16>(rows, ldx, M, K, w_codes, w_scales, N, S, alpha, y, y_dtype, ldy, stream);
-    return launch_format<32>(rows, ldx, M, K, w_codes, w_scales, N, S, alpha, y, y_dtype, ldy, stream);
+    if (y_dtype == ARCQ_DTYPE_F16)
+        return block == 16 ? launch_typed<16>(a, static_cast<_Float16*>(y)) : launch_typed<32>(a, static_cast<_Float16*>(y));
+    return block == 16 ? launch_typed<16>(a, static_cast<float*>(y)) : launch_typed<32>(a, static_cast<float*>(y));
 }
 
 }  // namespace arcq

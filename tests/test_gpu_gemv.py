@@ -59,6 +59,25 @@ def test_products(fmt, M, N, K, S, reorder):
     assert bool((raw == 12345.0).all())
 
 
+# Workgroups that take one tile of weight rows after the other, over rounds of K that end in a part of one: the next tile's weights and rows are
+# asked for while the last, shorter turn of this one is multiplied.
+@pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
+@pytest.mark.parametrize("M,N,K", [(1, 8400, 4736), (1, 16700, 4192), (3, 8300, 4256), (6, 16600, 4352), (16, 33000, 4704), (20, 16500, 4896), (32, 8200, 9216)])
+def test_tile_after_tile(fmt, M, N, K):
+    say(f"gemv {fmt} M={M} N={N} K={K}")
+    block = 32 if fmt == "mx" else 16
+    rng = np.random.default_rng(M + N + K)
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    codes = rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    scales = rng.integers(118, 124, (N, K // block), dtype=np.uint8) if fmt == "mx" else rng.integers(40, 60, (N, K // block), dtype=np.uint8)
+    w = (codes, scales, None if fmt == "mx" else np.float32(0.125))
+    want, mag = M8.gemv(x, None, *w)
+    raw, y = output(M, N, torch.float32, 3)
+    call(fmt, dev(x), None, w, y=y)
+    torch.cuda.synchronize()
+    assert_product(y, want, mag, K)
+
+
 @pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
 def test_scales_over_their_whole_range(fmt):
     """Weights whose blocks differ by many powers of two, and rows with subnormals: sums are of either end of the range."""
