@@ -117,6 +117,14 @@ def _stream():
         return torch.cuda.current_stream().cuda_stream
 
 
+def _device():
+    """Index of the current device (by torch's private function for it, as in _stream)."""
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
+
+
 def _ptr(t):
     """Address of a tensor's data; empty tensors and None are null.  (Every pointer argument is declared void*: plain integers do.)"""
     return t.data_ptr() or None if t is not None and t.numel() else None
@@ -339,31 +347,41 @@ def arcq_mx_gemm(a_codes, a_scales, w_codes, w_scales, out_dtype=torch.float16, 
     return y
 
 
-def _fp16_rows(t):
+# The calls from here to arcq_mx_gemv want every tensor on the current device, whose current stream they use.
+
+def _fp16_rows(t, device):
     """(rows, K, pitch) of fp16 rows, checked."""
-    assert t.is_cuda and t.dtype is torch.float16 and t.dim() == 2
+    assert t.get_device() == device and t.dtype is torch.float16
     rows, cols = t.shape
     pitch, step = t.stride()
     assert step == 1 or cols <= 1
     return rows, cols, pitch if rows > 1 else max(cols, pitch)
 
 
-def _perm(perm, K):
-    """perm, checked; None stays None."""
-    if perm is not None:
-        assert perm.is_cuda and perm.dtype is torch.int32 and perm.is_contiguous()
-        if perm.numel() != K:
-            raise ArcqError(BAD_SHAPE, "perm must have K entries")
-    return perm
+def _input_rows(x):
+    """(device, rows, K, pitch) of a call's fp16 rows, which have to be on the current device."""
+    assert x.is_cuda
+    device = _device()
+    return device, *_fp16_rows(x, device)
 
 
-def _mx8_outputs(x, rows, K, codes, scales):
+def _perm(perm, K, device):
+    """Address of perm, checked; none for None."""
+    if perm is None:
+        return None
+    assert perm.get_device() == device and perm.dtype is torch.int32 and perm.is_contiguous()
+    if perm.numel() != K:
+        raise ArcqError(BAD_SHAPE, "perm must have K entries")
+    return perm.data_ptr()
+
+
+def _mx8_outputs(x, rows, K, codes, scales, device):
     if codes is None:
         codes = x.new_empty((rows, K), dtype=torch.uint8)
     if scales is None:
         scales = x.new_empty((rows, K // 32), dtype=torch.uint8)
-    assert codes.dtype is torch.uint8 and scales.dtype is torch.uint8
-    assert codes.shape == (rows, K) and scales.shape == (rows, K // 32) and codes.is_contiguous() and scales.is_contiguous()
+    assert codes.get_device() == device and codes.dtype is torch.uint8 and codes.shape == (rows, K) and codes.is_contiguous()
+    assert scales.get_device() == device and scales.dtype is torch.uint8 and scales.shape == (rows, K // 32) and scales.is_contiguous()
     return codes, scales
 
 
@@ -375,51 +393,55 @@ def arcq_mx8_packed_sizes(rows, K):
 
 def arcq_mx8_quantize_act(x, perm=None, flags=0, codes=None, scales=None):
     """MXFP8: x fp16 [M, K] -> (codes uint8 [M, K], E4M3; scales uint8 [M, K/32], E8M0), channels in the order perm or their own."""
-    rows, K, ldx = _fp16_rows(x)
-    perm = _perm(perm, K)
-    codes, scales = _mx8_outputs(x, rows, K, codes, scales)
-    _check(lib().arcq_mx8_quantize_act(_ptr(x), rows, K, ldx, _ptr(perm), int(flags), _ptr(codes), _ptr(scales), _stream()))
+    device, rows, K, ldx = _input_rows(x)
+    codes, scales = _mx8_outputs(x, rows, K, codes, scales, device)
+    _check(lib().arcq_mx8_quantize_act(x.data_ptr(), rows, K, ldx, _perm(perm, K, device), flags, codes.data_ptr(), scales.data_ptr(), _stream()))
     return codes, scales
 
 
 def arcq_mx8_add_rmsnorm_quantize_act(x, residual, gamma, eps, perm=None, flags=0, hidden=None, codes=None, scales=None):
     """hidden = x + residual, RMSNorm (weight gamma fp16 [K], eps) and arcq_mx8_quantize_act as one kernel -> (codes, scales, hidden).
     hidden may be x or residual (in place).  residual None: the norm of x itself, hidden is None."""
-    rows, K, ldx = _fp16_rows(x)
-    perm = _perm(perm, K)
-    assert gamma.is_cuda and gamma.dtype is torch.float16 and gamma.is_contiguous() and gamma.numel() == K
-    codes, scales = _mx8_outputs(x, rows, K, codes, scales)
-    ldr = ldh = 0
-    if residual is not None:
-        assert residual.shape == x.shape
-        ldr = _fp16_rows(residual)[2]
+    device, rows, K, ldx = _input_rows(x)
+    assert gamma.get_device() == device and gamma.dtype is torch.float16 and gamma.is_contiguous() and gamma.numel() == K
+    codes, scales = _mx8_outputs(x, rows, K, codes, scales, device)
+    if residual is None:
+        assert hidden is None
+        r, ldr, h, ldh = None, 0, None, 0
+    else:
         if hidden is None:
             hidden = x.new_empty((rows, K))
-        assert hidden.shape == x.shape
-        ldh = _fp16_rows(hidden)[2]
-    else:
-        assert hidden is None
-    _check(lib().arcq_mx8_add_rmsnorm_quantize_act(_ptr(x), rows, K, ldx, _ptr(residual), ldr, _ptr(hidden), ldh, _ptr(gamma), float(eps),
-                                                   _ptr(perm), int(flags), _ptr(codes), _ptr(scales), _stream()))
+        ldr, ldh = _fp16_rows(residual, device)[2], _fp16_rows(hidden, device)[2]
+        assert residual.shape == x.shape == hidden.shape
+        r, h = residual.data_ptr(), hidden.data_ptr()
+    _check(lib().arcq_mx8_add_rmsnorm_quantize_act(x.data_ptr(), rows, K, ldx, r, ldr, h, ldh, gamma.data_ptr(), eps,
+                                                   _perm(perm, K, device), flags, codes.data_ptr(), scales.data_ptr(), _stream()))
     return codes, scales, hidden
 
 
-def _packed_weights(w_codes, w_scales, K, block):
+def _packed_weights(w_codes, w_scales, K, block, device):
     """(N, S) of packed weights [N, K + S], checked."""
-    for t in (w_codes, w_scales):
-        assert t.is_cuda and t.dtype is torch.uint8 and t.dim() == 2 and t.is_contiguous()
-    N, Kp = w_codes.shape[0], 2 * w_codes.shape[1]
-    if Kp < K or w_scales.shape != (N, Kp // block):
+    assert w_codes.get_device() == device and w_codes.dtype is torch.uint8 and w_codes.is_contiguous()
+    assert w_scales.get_device() == device and w_scales.dtype is torch.uint8 and w_scales.is_contiguous()
+    N, half = w_codes.shape
+    if 2 * half < K or w_scales.shape != (N, 2 * half // block):
         raise ArcqError(BAD_SHAPE, "operand shapes disagree on K and S")
-    return N, Kp - K
+    return N, 2 * half - K
 
 
-def _output(a, M, N, out_dtype, y):
+def _output(a, M, N, out_dtype, y, device):
     """(y, its type, its pitch): the caller's, checked, or a new one."""
     if y is None:
         y = a.new_empty((M, N), dtype=out_dtype)
-    assert y.is_cuda and y.shape == (M, N) and (y.stride(1) == 1 or N <= 1) and y.dtype in (torch.float16, torch.float32)
-    return y, DTYPE_F16 if y.dtype is torch.float16 else DTYPE_F32, y.stride(0) if M > 1 else max(N, y.stride(0))
+    assert y.get_device() == device and y.shape == (M, N)
+    pitch, step = y.stride()
+    assert step == 1 or N <= 1
+    if M <= 1:
+        pitch = max(N, pitch)
+    if y.dtype is torch.float16:
+        return y, DTYPE_F16, pitch
+    assert y.dtype is torch.float32
+    return y, DTYPE_F32, pitch
 
 
 def arcq_mx8_gemm_workspace_size(M, N, K):
@@ -431,24 +453,26 @@ def arcq_mx8_gemm_workspace_size(M, N, K):
 def arcq_mx8_gemm(a_codes, a_scales, w_codes, w_scales, out_dtype=torch.float16, y=None, workspace=None):
     """y[M, N] = MXFP8 activations [M, K] times MXFP4 weights packed [N, K + S] (the S repeated columns are passed over); returns y.
     workspace: a uint8 tensor of at least arcq_mx8_gemm_workspace_size bytes lets few-tile problems split K."""
-    assert a_codes.is_cuda and a_codes.dtype is torch.uint8 and a_codes.dim() == 2 and a_codes.is_contiguous()
-    assert a_scales.is_cuda and a_scales.dtype is torch.uint8 and a_scales.is_contiguous()
+    assert a_codes.is_cuda and a_codes.dtype is torch.uint8 and a_codes.is_contiguous()
+    device = _device()
+    assert a_codes.get_device() == device == a_scales.get_device() and a_scales.dtype is torch.uint8 and a_scales.is_contiguous()
     M, K = a_codes.shape
-    N, S = _packed_weights(w_codes, w_scales, K, 32)
+    N, S = _packed_weights(w_codes, w_scales, K, 32, device)
     if a_scales.shape != (M, K // 32):
         raise ArcqError(BAD_SHAPE, "activation shapes disagree on K")
-    y, dt, ldy = _output(a_codes, M, N, out_dtype, y)
-    ws, ws_bytes = _scratch(workspace)
-    _check(lib().arcq_mx8_gemm(_ptr(a_codes), _ptr(a_scales), _ptr(w_codes), _ptr(w_scales), M, N, K, S, _ptr(y), dt, ldy, ws, ws_bytes, _stream()))
+    y, dt, ldy = _output(a_codes, M, N, out_dtype, y, device)
+    ws, ws_bytes = _scratch(workspace, device)
+    _check(lib().arcq_mx8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, S, y.data_ptr(), dt, ldy,
+                               ws, ws_bytes, _stream()))
     return y
 
 
-def _scratch(workspace):
+def _scratch(workspace, device):
     """(address, bytes) of a workspace tensor, or of none."""
     if workspace is None:
         return None, 0
-    assert workspace.is_cuda and workspace.is_contiguous()
-    return _ptr(workspace), workspace.numel() * workspace.element_size()
+    assert workspace.get_device() == device and workspace.is_contiguous()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def arcq_mx8_gemm_route(M, N, K, S=0, out_dtype=torch.float16, with_workspace=False):
@@ -473,21 +497,21 @@ def arcq_mx_gemv_workspace_size(M, N, K, with_perm):
 
 def _gemv(size, block, x, perm, w_codes, w_scales, out_dtype, y, workspace):
     """Arguments of a product of fp16 rows with packed weights: what comes before the weights' scale, what comes behind it, and y."""
-    M, K, ldx = _fp16_rows(x)
-    perm = _perm(perm, K)
-    N, S = _packed_weights(w_codes, w_scales, K, block)
-    y, dt, ldy = _output(x, M, N, out_dtype, y)
+    device, M, K, ldx = _input_rows(x)
+    N, S = _packed_weights(w_codes, w_scales, K, block, device)
+    y, dt, ldy = _output(x, M, N, out_dtype, y, device)
     if workspace is None:
         need = size(M, N, K, perm is not None)
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    return (_ptr(x), M, K, ldx, _ptr(perm), _ptr(w_codes), _ptr(w_scales)), (N, S, _ptr(y), dt, ldy, *_scratch(workspace), _stream()), y
+    return ((x.data_ptr(), M, K, ldx, _perm(perm, K, device), w_codes.data_ptr(), w_scales.data_ptr()),
+            (N, S, y.data_ptr(), dt, ldy, *_scratch(workspace, device), _stream()), y)
 
 
 def arcq_gemv(x, perm, w_codes, w_scales, w_tensor_scale, out_dtype=torch.float16, y=None, workspace=None):
     """y[M, N] = x [M, K] fp16, channels in the order perm (None: their own), times NVFP4 weights packed [N, K + S]; returns y.
     workspace: a uint8 tensor of at least arcq_gemv_workspace_size bytes (one is made where none is given)."""
     head, tail, y = _gemv(arcq_gemv_workspace_size, 16, x, perm, w_codes, w_scales, out_dtype, y, workspace)
-    _check(lib().arcq_gemv(*head, float(w_tensor_scale), *tail))
+    _check(lib().arcq_gemv(*head, w_tensor_scale, *tail))
     return y
 
 

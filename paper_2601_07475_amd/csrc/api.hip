@@ -596,7 +596,7 @@ arcq_status arcq_mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, int 
 
 static arcq_status check_gemv_shape(int block, int64_t M, int64_t N, int64_t K, int64_t S) {
     if (arcq_status st = block == 16 ? check_KS(K, S) : check_KS_mx(K, S)) return st;
-    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x7FFFFFFF)
+    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x7FFFFF00)     // (whole tiles of features are counted in 32 bits)
         return fail(ARCQ_BAD_SHAPE, "M = %lld, N = %lld out of range", (long long)M, (long long)N);
     return ARCQ_OK;
 }

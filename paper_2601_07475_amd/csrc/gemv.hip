@@ -428,27 +428,40 @@ arcq_status launch_typed(const GemvArgs& a, OutT* y) {
 
 }  // namespace
 
+// Rows of a launch: grids and the reordered rows stay within bounds for any M.
+static constexpr int64_t kMostRows = 1 << 16;
+
 // Rows in the weights' order, where no kernel reorders them on the way.
 size_t gemv_workspace_bytes(int64_t M, int64_t K, bool reorder) {
-    return reorder && !whole_rows(M, K) ? (size_t)M * (size_t)K * 2 : 0;
+    return reorder && !whole_rows(M, K) ? (size_t)std::min(M, kMostRows) * (size_t)K * 2 : 0;
+}
+
+template <typename OutT>
+static arcq_status launch_rows(int block, const GemvArgs& a, OutT* y, uint16_t* reordered) {
+    GemvArgs run = a;
+    if (reordered) {
+        const unsigned parts = (unsigned)((a.K / 8 + 255) / 256);
+        hipLaunchKernelGGL(reorder_rows_kernel, dim3(parts * (unsigned)a.M), dim3(256), 0, a.stream, a.x, a.ldx, (int)a.K, a.perm, reordered, parts);
+        if (arcq_status st = check_launch("reorder_rows_kernel")) return st;
+        run.x = reordered;
+        run.ldx = a.K;
+        run.perm = nullptr;
+    }
+    return block == 16 ? launch_typed<16>(run, y) : launch_typed<32>(run, y);
 }
 
 arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
                         const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
                         hipStream_t stream) {
-    GemvArgs a = {static_cast<const uint16_t*>(x), M, K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream};
-    if (gemv_workspace_bytes(M, K, perm != nullptr) > 0) {
-        uint16_t* reordered = static_cast<uint16_t*>(workspace);
-        const unsigned parts = (unsigned)((K / 8 + 255) / 256);
-        hipLaunchKernelGGL(reorder_rows_kernel, dim3(parts * (unsigned)M), dim3(256), 0, stream, a.x, ldx, (int)K, perm, reordered, parts);
-        if (arcq_status st = check_launch("reorder_rows_kernel")) return st;
-        a.x = reordered;
-        a.ldx = K;
-        a.perm = nullptr;
+    uint16_t* reordered = gemv_workspace_bytes(M, K, perm != nullptr) > 0 ? static_cast<uint16_t*>(workspace) : nullptr;
+    for (int64_t m = 0; m < M; m += kMostRows) {
+        // (the last run of rows may be short enough to be reordered on the way: it goes like the others all the same)
+        const GemvArgs a = {static_cast<const uint16_t*>(x) + m * ldx, std::min(M - m, kMostRows), K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream};
+        const arcq_status st = y_dtype == ARCQ_DTYPE_F16 ? launch_rows(block, a, static_cast<_Float16*>(y) + m * ldy, reordered)
+                                                         : launch_rows(block, a, static_cast<float*>(y) + m * ldy, reordered);
+        if (st) return st;
     }
-    if (y_dtype == ARCQ_DTYPE_F16)
-        return block == 16 ? launch_typed<16>(a, static_cast<_Float16*>(y)) : launch_typed<32>(a, static_cast<_Float16*>(y));
-    return block == 16 ? launch_typed<16>(a, static_cast<float*>(y)) : launch_typed<32>(a, static_cast<float*>(y));
+    return ARCQ_OK;
 }
 
 }  // namespace arcq

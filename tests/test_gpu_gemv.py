@@ -138,3 +138,41 @@ def test_no_rows_and_no_features():
     one = torch.ones((1, 64), dtype=torch.float16, device="cuda")
     assert B.arcq_mx_gemv(one, None, w[:0], s[:0]).shape == (1, 0)
     assert B.arcq_gemv(one, None, w[:0], torch.zeros((0, 4), dtype=torch.uint8, device="cuda"), 1.0).shape == (1, 0)
+
+
+def test_more_rows_than_a_launch_takes():
+    """70000 rows go in two runs, which share the workspace for the reordered rows."""
+    say("gemv, 70000 rows")
+    M, N, K = 70000, 20, 64
+    rng = np.random.default_rng(8)
+    X = rng.standard_normal((M, K)).astype(np.float16)
+    perm = rng.permutation(K).astype(np.int32)
+    w = pack("mx", (rng.standard_normal((N, K)) * 0.02).astype(np.float16), perm, 0)
+    assert B.arcq_mx_gemv_workspace_size(M, N, K, True) == 65536 * K * 2
+    want, mag = M8.gemv(X, perm, *w)
+    assert_product(call("mx", dev(X), dev(perm), w, out_dtype=torch.float32), want, mag, K)
+
+
+def test_operands_in_host_memory():
+    """Refused before the library sees their addresses."""
+    x, w, s = torch.zeros((2, 64), dtype=torch.float16), torch.zeros((8, 32), dtype=torch.uint8), torch.zeros((8, 2), dtype=torch.uint8)
+    xd, wd, sd, codes, scales = x.cuda(), w.cuda(), s.cuda(), torch.zeros((2, 64), dtype=torch.uint8), torch.zeros((2, 2), dtype=torch.uint8)
+    y, perm = torch.zeros((2, 8), dtype=torch.float16), torch.arange(64, dtype=torch.int32)
+    for args in ((x, None, wd, sd), (xd, perm, wd, sd), (xd, None, w, sd), (xd, None, wd, s)):
+        with pytest.raises(AssertionError):
+            B.arcq_mx_gemv(*args)
+    with pytest.raises(AssertionError):
+        B.arcq_mx_gemv(xd, None, wd, sd, y=y)
+    with pytest.raises(AssertionError):
+        B.arcq_mx_gemv(xd, perm.cuda(), wd, sd, workspace=torch.zeros(4096, dtype=torch.uint8))
+    for kw in ({"codes": codes}, {"scales": scales}, {"perm": perm}):
+        with pytest.raises(AssertionError):
+            B.arcq_mx8_quantize_act(xd, **kw)
+        with pytest.raises(AssertionError):
+            B.arcq_mx8_add_rmsnorm_quantize_act(xd, None, xd[0], 1e-5, **kw)
+    for residual, gamma, hidden in ((x, xd[0], None), (xd, x[0], None), (xd, xd[0], x)):
+        with pytest.raises(AssertionError):
+            B.arcq_mx8_add_rmsnorm_quantize_act(xd, residual, gamma, 1e-5, hidden=hidden)
+    for args in ((codes, scales.cuda(), wd, sd), (codes.cuda(), scales, wd, sd), (codes.cuda(), scales.cuda(), w, sd)):
+        with pytest.raises(AssertionError):
+            B.arcq_mx8_gemm(*args)
