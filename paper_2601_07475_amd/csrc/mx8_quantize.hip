@@ -10,6 +10,15 @@
 // A workgroup owns whole rows.  A lane owns 16 consecutive channels at a time (32 bytes in, 16 out), the two lanes of a block are neighbours and
 // exchange their maxima by one data-parallel-primitive move.  A row is asked for while the one before it is being processed, in
 // registers: the addition, the new hidden state and the sum of squares want it in its own order; only the reordered values go through LDS.
+//
+// Measured (us, and TB/s of what is read and written, the order apart):    quantize        norm          addition and norm
+//        1 x 14336, reordered                                              3.6           4.9               5.4      (2.4 the launch of one row)
+//      333 x 5120                                                          2.7  1.9      4.8  1.1          4.8  2.5  (norm alone: reordered)
+//     2048 x 8192, reordered                                              10.3  4.9     14.2  3.6         21.3  5.5
+//     8192 x 8192, reordered                                              32.2  6.3     40.0  5.1         89.3  5.3
+//     8192 x 28672, reordered                                            124    5.8    174    4.1        357    4.6
+// Single rows are bound by one compute unit's way to memory and the launch, the others by memory; the norm's barriers and the reads of LDS in the
+// order of the weights take up to a quarter more, for rows of which only one or two workgroups fit a compute unit.
 #include "internal.h"
 #include "lds_dma.h"
 #include "row_stats.h"
@@ -48,9 +57,20 @@ __device__ __forceinline__ uint4 quantize_half(const float (&v)[16], bool scale_
     return make_uint4(c[0], c[1], c[2], c[3]);
 }
 
+// The channels' wider forms that came before are not kept for what comes behind, at two registers a channel and more.
+template <int HPT>
+__device__ __forceinline__ void pin(uint32_t (&h)[HPT][8]) {
+#pragma unroll
+    for (int j = 0; j < HPT; ++j)
+#pragma unroll
+        for (int w = 0; w < 8; ++w) asm volatile("" : "+v"(h[j][w]));
+}
+
 constexpr int kStatWords = 5 * 64;      // 64-bit words behind the row: two rows' partial sums, three exact ones
 
 // HPT     halves (16 channels) a lane owns: 1, 2, or 4 for rows of more than 32768 channels, which are not asked for ahead (registers)
+//         (HPT 2 with gamma kept in registers, too, spills: 4096 x 28672 with addition, norm and order 246 us, here 185.  HPT 4 with the norm does
+//         so by 36 or 88 bytes a lane, beside the 56 or 112 that it has in and out.)
 // ADD     the residual is added in front, and the sum stored as the new hidden state
 // NORM    RMSNorm in front of the quantizer: one more barrier, behind which the row in LDS is known to have been read
 // GATHER  channels are reordered, through LDS: two buffers without NORM, as far as they fit, so that one barrier a row is enough
@@ -69,8 +89,8 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
     const uint32_t row_bytes = 2u * (uint32_t)K;
     double* stats = reinterpret_cast<double*>(lds + (size_t)BUFFERS * row_bytes);
 
-    int row = blockIdx.x;
-    if (row >= rows) return;
+    uint32_t row = blockIdx.x;              // (32 bits of an unsigned number hold the last row and a grid behind it)
+    if (row >= (uint32_t)rows) return;
 
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     int at[HPT];
@@ -80,7 +100,7 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
         live[j] = tid + j * T < halves;
         at[j] = live[j] ? tid + j * T : halves - 1;
     }
-    auto fetch = [&](const uint16_t* base, int64_t ld, int r, u32x4 (&to)[HPT][2]) {
+    auto fetch = [&](const uint16_t* base, int64_t ld, uint32_t r, u32x4 (&to)[HPT][2]) {
 #pragma unroll
         for (int j = 0; j < HPT; ++j) {
             const u32x4* src = reinterpret_cast<const u32x4*>(base + (int64_t)r * ld) + 2 * at[j];
@@ -89,33 +109,42 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
         }
     };
     u32x4 in[HPT][2], in2[ADD ? HPT : 1][2];
-    auto ask = [&](int r) {
+    auto ask = [&](uint32_t r) {
         fetch(x, ldx, r, in);
         if constexpr (ADD) fetch(residual, ldr, r, in2);
     };
     if (AHEAD) ask(row);
 
-    uint32_t chan[GATHER ? HPT : 1][8], gam[NORM ? HPT : 1][8];     // source channels and gamma, two to a register
+    // Source channels and gamma, two to a register: kept, or gamma in LDS (HPT 2), or read again for every row (HPT 4).
+    auto channels_of = [&](int j, uint32_t (&to)[8]) {
+        const int4* pp = reinterpret_cast<const int4*>(perm + 16 * at[j]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int4 v4 = pp[q];
+            to[2 * q] = ((uint32_t)v4.x & 0xFFFFu) | ((uint32_t)v4.y << 16);
+            to[2 * q + 1] = ((uint32_t)v4.z & 0xFFFFu) | ((uint32_t)v4.w << 16);
+        }
+    };
+    constexpr bool KEEP_CHAN = GATHER && HPT <= 2, KEEP_GAMMA = NORM && HPT == 1, LDS_GAMMA = NORM && HPT == 2;
+    uint32_t chan[KEEP_CHAN ? HPT : 1][8], gam[KEEP_GAMMA ? HPT : 1][8];
+    uint4* lds_gamma = reinterpret_cast<uint4*>(lds + (size_t)BUFFERS * row_bytes + (NORM ? 8 * kStatWords : 0));
 #pragma unroll
     for (int j = 0; j < HPT; ++j) {
-        if constexpr (GATHER) {
-            const int4* pp = reinterpret_cast<const int4*>(perm + 16 * at[j]);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int4 v4 = pp[q];
-                chan[j][2 * q] = ((uint32_t)v4.x & 0xFFFFu) | ((uint32_t)v4.y << 16);
-                chan[j][2 * q + 1] = ((uint32_t)v4.z & 0xFFFFu) | ((uint32_t)v4.w << 16);
-            }
-        }
-        if constexpr (NORM) {
+        if constexpr (KEEP_CHAN) channels_of(j, chan[j]);
+        if constexpr (KEEP_GAMMA || LDS_GAMMA) {
             const uint4* gp = reinterpret_cast<const uint4*>(gamma + 16 * at[j]);
             const uint4 g0 = gp[0], g1 = gp[1];
-            gam[j][0] = g0.x, gam[j][1] = g0.y, gam[j][2] = g0.z, gam[j][3] = g0.w;
-            gam[j][4] = g1.x, gam[j][5] = g1.y, gam[j][6] = g1.z, gam[j][7] = g1.w;
+            if constexpr (KEEP_GAMMA) {
+                gam[j][0] = g0.x, gam[j][1] = g0.y, gam[j][2] = g0.z, gam[j][3] = g0.w;
+                gam[j][4] = g1.x, gam[j][5] = g1.y, gam[j][6] = g1.z, gam[j][7] = g1.w;
+            } else if (live[j]) {           // read by the lane that stores it
+                lds_gamma[2 * at[j]] = g0;
+                lds_gamma[2 * at[j] + 1] = g1;
+            }
         }
     }
     uint32_t turn = 0;
-    for (; row < rows; row += gridDim.x, turn ^= 1u) {
+    for (; row < (uint32_t)rows; row += gridDim.x, turn ^= 1u) {
         if (!AHEAD) ask(row);
         uint32_t h[HPT][8];                 // the lane's channels, two to a register
 #pragma unroll
@@ -128,8 +157,8 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
                     h[j][w] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, h[j][w]) + __builtin_bit_cast(half2v, r));
                 }
             }
-        const int next = row + gridDim.x;
-        if (AHEAD && next < rows) ask(next);
+        const uint32_t next = row + gridDim.x;
+        if (AHEAD && next < (uint32_t)rows) ask(next);
         if constexpr (ADD) {
 #pragma unroll
             for (int j = 0; j < HPT; ++j)
@@ -176,6 +205,7 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
                 decided = ms_lo == ms_hi;
                 rstd = 1.0f / __builtin_sqrtf(ms_lo + eps);             // IEEE square root and division
             }
+            pin(h);
             if (__builtin_amdgcn_readfirstlane(decided ? 1 : 0) == 0) {     // the same in every wave of the workgroup
                 uint64_t s[3] = {0, 0, 0};
 #pragma unroll
@@ -209,9 +239,19 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
                 }
                 const float ms = (float)(join_exact_sums(s[0], s[1], s[2]) / (double)K);
                 rstd = 1.0f / __builtin_sqrtf(ms + eps);
+                pin(h);
             }
 #pragma unroll
-            for (int j = 0; j < HPT; ++j)
+            for (int j = 0; j < HPT; ++j) {
+                uint32_t g[8];
+                if constexpr (KEEP_GAMMA) {
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) g[w] = gam[j][w];
+                } else {
+                    const uint4* gp = LDS_GAMMA ? lds_gamma + 2 * at[j] : reinterpret_cast<const uint4*>(gamma + 16 * at[j]);
+                    const uint4 g0 = gp[0], g1 = gp[1];
+                    g[0] = g0.x, g[1] = g0.y, g[2] = g0.z, g[3] = g0.w, g[4] = g1.x, g[5] = g1.y, g[6] = g1.z, g[7] = g1.w;
+                }
 #pragma unroll
                 for (int w = 0; w < 8; ++w) {
                     const half2v p = __builtin_bit_cast(half2v, h[j][w]);
@@ -220,9 +260,11 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
                     asm("" : "+v"(a));
                     asm("" : "+v"(b));
                     const half2v t = {(_Float16)a, (_Float16)b};
-                    h[j][w] = __builtin_bit_cast(uint32_t, t * __builtin_bit_cast(half2v, gam[j][w]));
+                    h[j][w] = __builtin_bit_cast(uint32_t, t * __builtin_bit_cast(half2v, g[w]));
                 }
+            }
         }
+        if constexpr (KEEP_CHAN && HPT == 2) pin(chan);     // (nor are two addresses for each of their pairs)
         const uint32_t base = BUFFERS == 2 ? turn * row_bytes : 0u;
         if constexpr (GATHER) {
 #pragma unroll
@@ -238,10 +280,12 @@ __global__ __launch_bounds__(1024) void mx8_rows_kernel(
 #pragma unroll
         for (int j = 0; j < HPT; ++j) {
             float v[16];
+            uint32_t from[8];
+            if constexpr (GATHER && !KEEP_CHAN) channels_of(j, from);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 if constexpr (GATHER) {
-                    const uint32_t ch = (chan[j][i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
+                    const uint32_t ch = ((KEEP_CHAN ? chan[j] : from)[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
                     v[i] = __half2float(*reinterpret_cast<const __half*>(lds + base + 2u * ch));
                 } else {
                     v[i] = (float)__builtin_bit_cast(half2v, h[j][i >> 1])[i & 1];
@@ -282,7 +326,7 @@ arcq_status launch_rows(const RowArgs& a) {
     auto kern = mx8_rows_kernel<HPT, ADD, NORM, GATHER, STREAM>;
     const int halves = (int)(a.K >> 4), threads = ((halves + HPT - 1) / HPT + 63) / 64 * 64;
     const int buffers = !GATHER ? 0 : NORM || HPT > 2 ? 1 : 2;
-    const size_t lds = (size_t)buffers * 2 * (size_t)a.K + (NORM ? 8 * kStatWords : 0);
+    const size_t lds = (size_t)buffers * 2 * (size_t)a.K + (NORM ? 8 * kStatWords : 0) + (NORM && HPT == 2 ? 2 * (size_t)a.K : 0);
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     // as many workgroups as the chip holds at once, never more than rows
