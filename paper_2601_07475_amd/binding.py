@@ -380,8 +380,8 @@ def _mx8_outputs(x, rows, K, codes, scales, device):
         codes = x.new_empty((rows, K), dtype=torch.uint8)
     if scales is None:
         scales = x.new_empty((rows, K // 32), dtype=torch.uint8)
-    assert codes.get_device() == device and codes.dtype is torch.uint8 and codes.shape == (rows, K) and codes.is_contiguous()
-    assert scales.get_device() == device and scales.dtype is torch.uint8 and scales.shape == (rows, K // 32) and scales.is_contiguous()
+    assert codes.get_device() == device and codes.dtype is torch.uint8 and codes.numel() == rows * K and codes.is_contiguous()
+    assert scales.get_device() == device and scales.dtype is torch.uint8 and scales.numel() == rows * (K // 32) and scales.is_contiguous()
     return codes, scales
 
 
@@ -411,8 +411,8 @@ def arcq_mx8_add_rmsnorm_quantize_act(x, residual, gamma, eps, perm=None, flags=
     else:
         if hidden is None:
             hidden = x.new_empty((rows, K))
-        ldr, ldh = _fp16_rows(residual, device)[2], _fp16_rows(hidden, device)[2]
-        assert residual.shape == x.shape == hidden.shape
+        (rows_r, K_r, ldr), (rows_h, K_h, ldh) = _fp16_rows(residual, device), _fp16_rows(hidden, device)
+        assert rows_r == rows == rows_h and K_r == K == K_h
         r, h = residual.data_ptr(), hidden.data_ptr()
     _check(lib().arcq_mx8_add_rmsnorm_quantize_act(x.data_ptr(), rows, K, ldx, r, ldr, h, ldh, gamma.data_ptr(), eps,
                                                    _perm(perm, K, device), flags, codes.data_ptr(), scales.data_ptr(), _stream()))

@@ -19,13 +19,14 @@
 //           row), 0.5 to 1.5 us; one row of 4096 channels over 4096 features 6.1 us where SLICE takes 4.7 without an order
 //
 // Measured (weights not in cache, rows in order; us, and TB/s of weights):     M = 1         M = 4         M = 16        M = 32
-//   NVFP4   4096 features,  4096 channels                                    4.7   2.0     5.0   1.9     6.6   1.4     8.4   1.1
+//   NVFP4   4096 features,  4096 channels                                    4.7   2.0     5.0   1.9     6.2   1.5     8.4   1.1
 //          27648            5120                                            20.9   3.8    24.6   3.2    29.7   2.7    43.6   1.8
 //           8192           28672                                            29.9   4.4    35.8   3.7    42.6   3.1    59.8   2.2
-//   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    16.1   1.9    21.8   1.4
+//   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    13.9   2.2    21.8   1.4
 // From 1 to 4 rows the weights' way from memory and the tiles' uneven shares bound it, with more the rows, too: every workgroup reads all of them
-// (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).  K split over workgroups would take that back but for a second launch
-// that adds up partial results: 16 rows, 4096 x 14336 15.3 us instead of 16.3, nothing elsewhere up to 27648 x 5120, so it is not there.
+// (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).  K split over workgroups would take some of that back but for a second
+// launch that adds up partial results, 4 us: with half the row tile's traffic 4096 x 14336 went from 16.3 us to 15.3 and nothing else up to
+// 27648 x 5120 gained, so that is not there; twice the waves on one compute unit (below) gave more.
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
@@ -102,24 +103,26 @@ __device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (
 }
 
 enum Rows { WHOLE, SLICE };
-constexpr int WAVES = 8, THREADS = 64 * WAVES;
 // Tiles of 16 weight rows of a workgroup: two or four share the rows where there are enough of them for every compute unit.
 //   16 rows, NT = 1, 2, 4: 14336 x 4096 18.6, 13.4, 11.4 us; 27648 x 5120 47.7, 30.0, 29.7; 8192 x 28672 60, 43, 64; 4096 x 4096 6.8, 8.0, 10.3
 //   32 rows, NT = 1, 2:    14336 x 4096 23.7, 17.0 us; 8192 x 28672 87, 60; 4096 x 4096 8.4, 10.5
-// Up to 4 rows, one: registers then allow two workgroups on a compute unit (14336 x 4096 10.8 -> 10.1 us).
-constexpr int slice_chunks(int rows, int nt) { return rows == 4 ? 4 : rows == 16 ? (nt == 1 ? 4 : nt == 2 ? 2 : 1) : 1; }     // of a wave, as registers allow
-constexpr int slice_bytes(int rows, int nt) { return rows * slice_chunks(rows, nt) * 256; }
-constexpr int kPieces = 2;                      // WHOLE: 16-byte pieces of the rows per thread
+// Waves that split K: 16 where one tile is what a compute unit gets and K has two chunks for each.
+//   16 rows, 8 and 16 waves: 4096 x 14336 14.9, 13.9 us; 1024 x 28672 24.0, 20.3; 4096 x 4096 6.3, 6.2; 4096 x 1024 4.3, 4.6.  4 rows: 8.7, 8.9; 13.5, 12.8;
+//   4.7, 5.0; 3.5, 4.6, so 8 for them.
+// Up to 4 rows, one tile: registers then allow two workgroups on a compute unit (14336 x 4096 10.8 -> 10.1 us).
+constexpr int slice_chunks(int rows, int nt, int waves) { return rows == 4 ? 4 : rows == 16 && nt <= 2 && waves == 8 ? 2 : 1; }     // of a wave, as registers allow
+constexpr int slice_bytes(int rows, int nt, int waves) { return rows * slice_chunks(rows, nt, waves) * 256; }
+constexpr int kWhole = 8192;                    // WHOLE: most values of the rows, 16 a thread
 
 // B      16: NVFP4, 32: MXFP4
 // ROWS   most rows of x of a workgroup: 4, 16 or 32, in tiles of 16 that share every decoded weight
 // NT     tiles of 16 weight rows of a workgroup, whose WAVES waves split K
 // LDS: the rows (WHOLE: M K 2 bytes twice, the second in the channels' own order), then the waves' partial tiles, two sets
-template <int B, int ROWS, int NT, int X, typename OutT>
-__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS == 4 ? 4 : 2, 4))) void gemv_kernel(
+template <int B, int ROWS, int NT, int WAVES, int X, typename OutT>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS == 4 || WAVES == 16 ? 4 : 2, 4))) void gemv_kernel(
     const uint16_t* __restrict__ x, int64_t ldx, int M, int K, const int32_t* __restrict__ perm, const uint8_t* __restrict__ w_codes,
     const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride) {
-    constexpr int MT = (ROWS + 15) / 16;
+    constexpr int MT = (ROWS + 15) / 16, THREADS = 64 * WAVES, PIECES = kWhole / 8 / THREADS;
     static_assert(X == SLICE || MT == 1, "WHOLE: up to 16 rows");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -137,11 +140,11 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS ==
     auto count_of = [&](int turn) { return turn < rounds ? 4 : turn == rounds ? rest1 - rest0 : 0; };
 
     // ---- the rows
-    u32x4 piece_x[X == WHOLE ? kPieces : 1];
-    uint32_t chan[X == WHOLE ? kPieces : 1][4];     // source channels of a piece, two to a register
+    u32x4 piece_x[X == WHOLE ? PIECES : 1];
+    uint32_t chan[X == WHOLE ? PIECES : 1][4];     // source channels of a piece, two to a register
     if constexpr (X == WHOLE) {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             const int u = tid + p * THREADS;
             if (u < pieces) {
                 const int4 a = *reinterpret_cast<const int4*>(perm + 8 * u), b = *reinterpret_cast<const int4*>(perm + 8 * u + 4);
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS ==
             }
         }
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             const int u = tid + p * THREADS;
             if (u < rows * pieces) {
                 const int m = rows == 1 ? 0 : u / pieces;
@@ -161,9 +164,9 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS ==
     }
     // SLICE: piece (eight k) and row at unit ROWS piece + (row ^ swizzle), so that writes of a row and reads of a piece both spread over the
     // banks.  A load instruction brings a row, or two, whole lines of each.
-    constexpr int XC = slice_chunks(ROWS, NT), LPR = 16 * XC, RPL = 64 / LPR, LOADS = ROWS / RPL;     // chunks of a slice; lanes of a row; rows of a load
+    constexpr int XC = slice_chunks(ROWS, NT, WAVES), LPR = 16 * XC, RPL = 64 / LPR, LOADS = ROWS / RPL;     // chunks of a slice; lanes of a row; rows of a load
     auto unit = [](int piece, int row) { return ROWS * piece + (row ^ (ROWS == 4 ? piece >> 2 & 3 : piece & 15)); };
-    uint8_t* slice = lds + (X == SLICE ? wave * slice_bytes(ROWS, NT) : 0);
+    uint8_t* slice = lds + (X == SLICE ? wave * slice_bytes(ROWS, NT, WAVES) : 0);
     u32x4 xv[X == SLICE ? LOADS : 1];
     auto load_x = [&](int c) {
         if constexpr (X == SLICE) {
@@ -222,14 +225,14 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS ==
     if constexpr (X == WHOLE) {
         uint8_t* to = lds + (size_t)rows * K * 2;
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             const int u = tid + p * THREADS;
             if (u < rows * pieces) *reinterpret_cast<u32x4*>(to + 16 * u) = piece_x[p];
         }
         wait_lgkmcnt0();
         wg_barrier();                               // not __syncthreads(): the weights stay in flight
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             const int piece = tid + p * THREADS;
             if (piece < pieces)
                 for (int m = 0; m < rows; ++m) {
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(ROWS ==
     constexpr int CH = B == 16 && ROWS == 16 && NT == 1 ? 2 : 1;
     // Partial tiles have two buffers behind the rows, so that a barrier a tile is enough.  The next tile's weights are asked for while this one's are
     // multiplied and added up.
-    float* red = reinterpret_cast<float*>(lds + (X == WHOLE ? (uint32_t)rows * (uint32_t)K * 4u : (uint32_t)(WAVES * slice_bytes(ROWS, NT))));
+    float* red = reinterpret_cast<float*>(lds + (X == WHOLE ? (uint32_t)rows * (uint32_t)K * 4u : (uint32_t)(WAVES * slice_bytes(ROWS, NT, WAVES))));
     uint32_t turn_red = 0;
     for (int tile = tile0; tile < tiles_n; tile += (int)stride) {
         float4v acc[CH][MT][NT];
@@ -397,19 +400,19 @@ struct GemvArgs {
     hipStream_t stream;
 };
 
-bool whole_rows(int64_t M, int64_t K) { return M <= 4 && M * K <= 8 * THREADS * kPieces; }
+bool whole_rows(int64_t M, int64_t K) { return M <= 4 && M * K <= kWhole; }
 
-template <int B, int ROWS, int NT, int X, typename OutT>
+template <int B, int ROWS, int NT, int WAVES, int X, typename OutT>
 arcq_status launch_tiles(const GemvArgs& a, OutT* y) {
-    auto kern = gemv_kernel<B, ROWS, NT, X, OutT>;
+    auto kern = gemv_kernel<B, ROWS, NT, WAVES, X, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    const size_t rows = X == WHOLE ? (size_t)a.M * a.K * 4 : (size_t)WAVES * slice_bytes(ROWS, NT);
+    const size_t rows = X == WHOLE ? (size_t)a.M * a.K * 4 : (size_t)WAVES * slice_bytes(ROWS, NT, WAVES);
     const size_t lds = rows + 2 * (size_t)WAVES * ((ROWS + 15) / 16) * NT * 1024;
     const int64_t tiles_n = (a.N + 16 * NT - 1) / (16 * NT), tiles_m = (a.M + ROWS - 1) / ROWS;
-    const int per_cu = ROWS == 4 && lds <= 80 * 1024 ? 2 : 1;       // as registers and LDS allow
+    const int per_cu = ROWS == 4 && WAVES == 8 && lds <= 80 * 1024 ? 2 : 1;       // as registers and LDS allow
     const unsigned stride = (unsigned)std::min<int64_t>(tiles_n, (int64_t)num_cu() * per_cu);
-    hipLaunchKernelGGL(kern, dim3(stride * (unsigned)tiles_m), dim3(THREADS), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
+    hipLaunchKernelGGL(kern, dim3(stride * (unsigned)tiles_m), dim3(64 * WAVES), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
                        a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride);
     return check_launch("gemv_kernel");
 }
@@ -418,12 +421,12 @@ template <int B, typename OutT>
 arcq_status launch_typed(const GemvArgs& a, OutT* y) {
     const int64_t tiles = (a.N + 15) / 16;
     const int cus = num_cu();
-    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, WHOLE>(a, y) : launch_tiles<B, 4, 1, SLICE>(a, y);
+    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, 8, WHOLE>(a, y) : launch_tiles<B, 4, 1, 8, SLICE>(a, y);
     if (a.M <= 16)
-        return tiles <= cus       ? launch_tiles<B, 16, 1, SLICE>(a, y)
-               : tiles <= 2 * cus ? launch_tiles<B, 16, 2, SLICE>(a, y)
-                                  : launch_tiles<B, 16, 4, SLICE>(a, y);
-    return tiles <= cus ? launch_tiles<B, 32, 1, SLICE>(a, y) : launch_tiles<B, 32, 2, SLICE>(a, y);
+        return tiles <= cus       ? (a.K >= 4096 ? launch_tiles<B, 16, 1, 16, SLICE>(a, y) : launch_tiles<B, 16, 1, 8, SLICE>(a, y))
+               : tiles <= 2 * cus ? launch_tiles<B, 16, 2, 8, SLICE>(a, y)
+                                  : launch_tiles<B, 16, 4, 8, SLICE>(a, y);
+    return tiles <= cus ? launch_tiles<B, 32, 1, 8, SLICE>(a, y) : launch_tiles<B, 32, 2, 8, SLICE>(a, y);
 }
 
 }  // namespace

@@ -62,7 +62,8 @@ def test_products(fmt, M, N, K, S, reorder):
 # Workgroups that take one tile of weight rows after the other, over rounds of K that end in a part of one: the next tile's weights and rows are
 # asked for while the last, shorter turn of this one is multiplied.
 @pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
-@pytest.mark.parametrize("M,N,K", [(1, 8400, 4736), (1, 16700, 4192), (3, 8300, 4256), (6, 16600, 4352), (16, 33000, 4704), (20, 16500, 4896), (32, 8200, 9216)])
+@pytest.mark.parametrize("M,N,K", [(1, 8400, 4736), (1, 16700, 4192), (3, 8300, 4256), (6, 16600, 4352), (16, 33000, 4704), (20, 16500, 4896), (32, 8200, 9216),
+                                   (9, 4100, 4064), (9, 4096, 4096), (16, 100, 8224), (5, 2000, 10272)])
 def test_tile_after_tile(fmt, M, N, K):
     say(f"gemv {fmt} M={M} N={N} K={K}")
     block = 32 if fmt == "mx" else 16
