@@ -616,7 +616,7 @@ static arcq_status gemv_entry(const char* who, int block, const void* x, int64_t
     if (!aligned(w_codes, 8)) return fail(ARCQ_BAD_ALIGN, "%s: codes must be 8-byte aligned", who);
     if (!aligned(perm, 16)) return fail(ARCQ_BAD_ALIGN, "%s: perm must be 16-byte aligned", who);
     if (!aligned(y, 4)) return fail(ARCQ_BAD_ALIGN, "%s: y must be 4-byte aligned", who);
-    const size_t need = gemv_workspace_bytes(M, K, perm != nullptr);
+    const size_t need = gemv_workspace_bytes(M, N, K, perm != nullptr);
     if (need > 0) {
         if (!workspace || workspace_bytes < need)
             return fail(ARCQ_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace_bytes);
@@ -630,7 +630,7 @@ arcq_status arcq_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_p
     clear_error();
     if (arcq_status st = check_gemv_shape(16, M, N, K, 0)) return st;
     if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
-    *bytes = (M == 0 || N == 0) ? 0 : gemv_workspace_bytes(M, K, with_perm != 0);
+    *bytes = (M == 0 || N == 0) ? 0 : gemv_workspace_bytes(M, N, K, with_perm != 0);
     return ARCQ_OK;
 }
 
@@ -644,7 +644,7 @@ arcq_status arcq_mx_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int wit
     clear_error();
     if (arcq_status st = check_gemv_shape(32, M, N, K, 0)) return st;
     if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
-    *bytes = (M == 0 || N == 0) ? 0 : gemv_workspace_bytes(M, K, with_perm != 0);
+    *bytes = (M == 0 || N == 0) ? 0 : gemv_workspace_bytes(M, N, K, with_perm != 0);
     return ARCQ_OK;
 }
 

@@ -24,9 +24,7 @@
 //           8192           28672                                            29.9   4.4    35.8   3.7    42.6   3.1    59.8   2.2
 //   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    13.9   2.2    21.8   1.4
 // From 1 to 4 rows the weights' way from memory and the tiles' uneven shares bound it, with more the rows, too: every workgroup reads all of them
-// (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).  K split over workgroups would take some of that back but for a second
-// launch that adds up partial results, 4 us: with half the row tile's traffic 4096 x 14336 went from 16.3 us to 15.3 and nothing else up to
-// 27648 x 5120 gained, so that is not there; twice the waves on one compute unit (below) gave more.
+// (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
@@ -103,13 +101,6 @@ __device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (
 }
 
 enum Rows { WHOLE, SLICE };
-// Tiles of 16 weight rows of a workgroup: two or four share the rows where there are enough of them for every compute unit.
-//   16 rows, NT = 1, 2, 4: 14336 x 4096 18.6, 13.4, 11.4 us; 27648 x 5120 47.7, 30.0, 29.7; 8192 x 28672 60, 43, 64; 4096 x 4096 6.8, 8.0, 10.3
-//   32 rows, NT = 1, 2:    14336 x 4096 23.7, 17.0 us; 8192 x 28672 87, 60; 4096 x 4096 8.4, 10.5
-// Waves that split K: 16 where one tile is what a compute unit gets and K has two chunks for each.
-//   16 rows, 8 and 16 waves: 4096 x 14336 14.9, 13.9 us; 1024 x 28672 24.0, 20.3; 4096 x 4096 6.3, 6.2; 4096 x 1024 4.3, 4.6.  4 rows: 8.7, 8.9; 13.5, 12.8;
-//   4.7, 5.0; 3.5, 4.6, so 8 for them.
-// Up to 4 rows, one tile: registers then allow two workgroups on a compute unit (14336 x 4096 10.8 -> 10.1 us).
 constexpr int slice_chunks(int rows, int nt, int waves) { return rows == 4 ? 4 : rows == 16 && nt <= 2 && waves == 8 ? 2 : 1; }     // of a wave, as registers allow
 constexpr int slice_bytes(int rows, int nt, int waves) { return rows * slice_chunks(rows, nt, waves) * 256; }
 constexpr int kWhole = 8192;                    // WHOLE: most values of the rows, 16 a thread
@@ -121,22 +112,26 @@ constexpr int kWhole = 8192;                    // WHOLE: most values of the row
 template <int B, int ROWS, int NT, int WAVES, int X, typename OutT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS == 4 || WAVES == 16 ? 4 : 2, 4))) void gemv_kernel(
     const uint16_t* __restrict__ x, int64_t ldx, int M, int K, const int32_t* __restrict__ perm, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride) {
+    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride, uint32_t splits) {
     constexpr int MT = (ROWS + 15) / 16, THREADS = 64 * WAVES, PIECES = kWhole / 8 / THREADS;
     static_assert(X == SLICE || MT == 1, "WHOLE: up to 16 rows");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i = lane & 15, q = lane >> 4;
     // a workgroup takes every stride-th tile of weight rows, for one tile of rows of x
-    const int m0 = (int)(blockIdx.x / stride) * ROWS, tile0 = (int)(blockIdx.x % stride);
+    // and one of `splits` runs of K, with fp32 partial results of its own
+    const uint32_t run = blockIdx.x / stride, split = run % splits;
+    const int m0 = (int)(run / splits) * ROWS, tile0 = (int)(blockIdx.x % stride);
+    y += (int64_t)split * M * N;
     constexpr int SB = 128 / B;                     // scale bytes of a chunk
     const int rows = min(M - m0, ROWS), pieces = K >> 3;
 
     // Whole chunks of 128 k go to the waves four at a time, in turn, and what is left of them in equal shares.
-    const int whole = K >> 7, rounds = whole / (4 * WAVES), rest = whole - rounds * 4 * WAVES;
-    const int rest0 = 4 * WAVES * rounds + wave * rest / WAVES, rest1 = 4 * WAVES * rounds + (wave + 1) * rest / WAVES;
+    const int chunks = K >> 7, chunk0 = (int)(split * (uint32_t)chunks / splits), whole = (int)((split + 1) * (uint32_t)chunks / splits) - chunk0;
+    const int rounds = whole / (4 * WAVES), rest = whole - rounds * 4 * WAVES, rest_at = chunk0 + 4 * WAVES * rounds;
+    const int rest0 = rest_at + wave * rest / WAVES, rest1 = rest_at + (wave + 1) * rest / WAVES;
     const int turns = rounds + (rest1 > rest0 ? 1 : 0);
-    auto first_of = [&](int turn) { return turn < rounds ? 4 * (turn * WAVES + wave) : rest0; };
+    auto first_of = [&](int turn) { return turn < rounds ? chunk0 + 4 * (turn * WAVES + wave) : rest0; };
     auto count_of = [&](int turn) { return turn < rounds ? 4 : turn == rounds ? rest1 - rest0 : 0; };
 
     // ---- the rows
@@ -316,8 +311,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS
         // What is left of K, less than a chunk, is for the first wave (the last one has the most): blocks past the end count as zero codes, and rows of x
         // are read from their start there.
         const int blocks = K / B;
-        if ((K & 127) != 0 && wave == 0) {
-            int c = whole;
+        if ((K & 127) != 0 && wave == 0 && split + 1 == splits) {
+            int c = chunks;
             asm volatile("" : "+v"(c));             // (its addresses, the same for every tile, are not worth registers in between)
             const uint8_t *tc[NT], *ts[NT];
             rows_of(w_codes, cpitch, tile, tc);
@@ -402,8 +397,44 @@ struct GemvArgs {
 
 bool whole_rows(int64_t M, int64_t K) { return M <= 4 && M * K <= kWhole; }
 
+struct GemvPlan {
+    int nt, splits;
+};
+// Row tiles that share the decoded weights: 4, 16 or 32 rows, several of the last.
+int rows_of(int64_t M) { return M <= 4 ? 4 : M <= 16 ? 16 : 32; }
+
+// The weight tiles of a workgroup (two or four share the rows) and the runs of K, by the least modelled time: a workgroup takes a time in
+// proportion to its channels and tiles; K in several runs lets few tiles reach every compute unit and evens out their shares, at the price of
+// a launch that adds up partial results.  Measured, us:
+//   16 rows, NT = 1, 2, 4: 14336 x 4096 18.6, 13.4, 11.4; 27648 x 5120 43, 35, 30; 8192 x 28672 57, 44, 65; 4096 x 4096 6.8, 8.0, 10.3
+//   32 rows, NT = 1, 2:    14336 x 4096 23.7, 17.0; 8192 x 28672 91, 61; 4096 x 4096 8.4, 10.5
+//   1, 2, 4, 8 runs:       1 x 1024 x 28672 13.6, 10.5, 8.5, 9.6; 16 x 1024 x 28672 20.6, 14.9, 11.9, 13.9; 30 x 848 x 26208 34.2, 21.6, 14.7, 17.2;
+//                          22 x 8490 x 27648 (266 pairs of tiles for 256 compute units) 95, 79, 71; 1 x 4096 x 14336 8.7 in one run, 12 in two
+// Against every choice of both on 22 problems the model's was within 6 % of the best but for 1 x 1024 x 14336 and 16 x 1024 x 8192 (15 and 10 %).
+GemvPlan plan_gemv(int64_t M, int64_t N, int64_t K, bool reorder) {
+    static const double cost[3][3] = {{0.45, 0, 0}, {0.8, 1.4, 2.2}, {1.4, 1.9, 0}};       // us for 1000 channels, NT = 1, 2, 4
+    static const int runs[8] = {1, 2, 3, 4, 6, 8, 12, 16};
+    const int rows = rows_of(M), r = rows == 4 ? 0 : rows == 16 ? 1 : 2;
+    const int64_t tiles_m = (M + rows - 1) / rows;
+    const int cus = num_cu();
+    GemvPlan best = {1, 1};
+    double least = 1e30;
+    for (int i = 0; i < 3 && cost[r][i] > 0; ++i) {
+        const int nt = 1 << i;
+        const int64_t tiles = (N + 16 * nt - 1) / (16 * nt) * tiles_m;
+        for (int splits : runs) {
+            if (splits > 1 && (splits * 1024 > K || tiles * splits > 8 * cus || (reorder && whole_rows(M, K)))) break;
+            const int64_t slots = std::max(cus / splits, 1);
+            double us = 2.5 + (double)((tiles + slots - 1) / slots) * cost[r][i] * (double)K / (1000.0 * splits);
+            if (splits > 1) us = 1.05 * (us + 3.5 + 0.25 * splits + (double)splits * (double)M * (double)N * 8.0 / 4.0e6);
+            if (us < least) least = us, best = {nt, splits};
+        }
+    }
+    return best;
+}
+
 template <int B, int ROWS, int NT, int WAVES, int X, typename OutT>
-arcq_status launch_tiles(const GemvArgs& a, OutT* y) {
+arcq_status launch_tiles(const GemvArgs& a, int splits, OutT* y) {
     auto kern = gemv_kernel<B, ROWS, NT, WAVES, X, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
@@ -411,36 +442,47 @@ arcq_status launch_tiles(const GemvArgs& a, OutT* y) {
     const size_t lds = rows + 2 * (size_t)WAVES * ((ROWS + 15) / 16) * NT * 1024;
     const int64_t tiles_n = (a.N + 16 * NT - 1) / (16 * NT), tiles_m = (a.M + ROWS - 1) / ROWS;
     const int per_cu = ROWS == 4 && WAVES == 8 && lds <= 80 * 1024 ? 2 : 1;       // as registers and LDS allow
-    const unsigned stride = (unsigned)std::min<int64_t>(tiles_n, (int64_t)num_cu() * per_cu);
-    hipLaunchKernelGGL(kern, dim3(stride * (unsigned)tiles_m), dim3(64 * WAVES), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
-                       a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride);
+    const unsigned stride = (unsigned)std::min<int64_t>(tiles_n, std::max(num_cu() * per_cu / splits, 1));
+    hipLaunchKernelGGL(kern, dim3(stride * (unsigned)(splits * tiles_m)), dim3(64 * WAVES), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
+                       a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride, (uint32_t)splits);
     return check_launch("gemv_kernel");
 }
 
+// Waves that split K: up to 4 rows, 8, so that two workgroups fit the registers of a compute unit (14336 x 4096 10.8 -> 10.1 us; with 16, 4096 x 4096
+// 4.7 -> 5.0).  16 rows, one tile: 16 where each has two chunks of 128 (4096 x 14336 14.9 -> 13.9 us, 1024 x 28672 24.0 -> 20.3; 4096 x 1024 4.3 -> 4.6).
 template <int B, typename OutT>
-arcq_status launch_typed(const GemvArgs& a, OutT* y) {
-    const int64_t tiles = (a.N + 15) / 16;
-    const int cus = num_cu();
-    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, 8, WHOLE>(a, y) : launch_tiles<B, 4, 1, 8, SLICE>(a, y);
+arcq_status launch_planned(const GemvArgs& a, GemvPlan p, OutT* y) {
+    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, 8, WHOLE>(a, 1, y) : launch_tiles<B, 4, 1, 8, SLICE>(a, p.splits, y);
     if (a.M <= 16)
-        return tiles <= cus       ? (a.K >= 4096 ? launch_tiles<B, 16, 1, 16, SLICE>(a, y) : launch_tiles<B, 16, 1, 8, SLICE>(a, y))
-               : tiles <= 2 * cus ? launch_tiles<B, 16, 2, 8, SLICE>(a, y)
-                                  : launch_tiles<B, 16, 4, 8, SLICE>(a, y);
-    return tiles <= cus ? launch_tiles<B, 32, 1, 8, SLICE>(a, y) : launch_tiles<B, 32, 2, 8, SLICE>(a, y);
+        return p.nt == 1   ? (a.K / p.splits >= 4096 ? launch_tiles<B, 16, 1, 16, SLICE>(a, p.splits, y) : launch_tiles<B, 16, 1, 8, SLICE>(a, p.splits, y))
+               : p.nt == 2 ? launch_tiles<B, 16, 2, 8, SLICE>(a, p.splits, y)
+                           : launch_tiles<B, 16, 4, 8, SLICE>(a, p.splits, y);
+    return p.nt == 1 ? launch_tiles<B, 32, 1, 8, SLICE>(a, p.splits, y) : launch_tiles<B, 32, 2, 8, SLICE>(a, p.splits, y);
 }
 
-}  // namespace
+template <int B, typename OutT>
+arcq_status launch_typed(const GemvArgs& a, GemvPlan p, OutT* y, float* partial) {
+    if (p.splits == 1) return launch_planned<B>(a, p, y);
+    GemvArgs run = a;
+    run.alpha = 1.0f;
+    run.ldy = a.N;
+    if (arcq_status st = launch_planned<B>(run, p, partial)) return st;
+    return launch_splitk_reduce(partial, p.splits, a.M, a.N, a.alpha, y, std::is_same<OutT, _Float16>::value ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy,
+                                a.stream);
+}
 
-// Rows of a launch: grids and the reordered rows stay within bounds for any M.
-static constexpr int64_t kMostRows = 1 << 16;
+// Rows of a launch: grids and workspaces stay within bounds for any M.
+constexpr int64_t kMostRows = 1 << 16;
 
-// Rows in the weights' order, where no kernel reorders them on the way.
-size_t gemv_workspace_bytes(int64_t M, int64_t K, bool reorder) {
-    return reorder && !whole_rows(M, K) ? (size_t)std::min(M, kMostRows) * (size_t)K * 2 : 0;
+struct GemvWorkspace {
+    size_t reordered, partial;      // bytes of the rows in the weights' order, where no kernel reorders them on the way, and of partial results behind
+};
+GemvWorkspace gemv_workspace(int64_t M, int64_t N, int64_t K, bool reorder, GemvPlan p) {
+    return {reorder && !whole_rows(M, K) ? ((size_t)M * (size_t)K * 2 + 255) / 256 * 256 : 0, p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * 4 : 0};
 }
 
 template <typename OutT>
-static arcq_status launch_rows(int block, const GemvArgs& a, OutT* y, uint16_t* reordered) {
+arcq_status launch_rows(int block, const GemvArgs& a, GemvPlan p, OutT* y, uint16_t* reordered, float* partial) {
     GemvArgs run = a;
     if (reordered) {
         const unsigned parts = (unsigned)((a.K / 8 + 255) / 256);
@@ -450,18 +492,31 @@ static arcq_status launch_rows(int block, const GemvArgs& a, OutT* y, uint16_t* 
         run.ldx = a.K;
         run.perm = nullptr;
     }
-    return block == 16 ? launch_typed<16>(run, y) : launch_typed<32>(run, y);
+    return block == 16 ? launch_typed<16>(run, p, y, partial) : launch_typed<32>(run, p, y, partial);
+}
+
+}  // namespace
+
+size_t gemv_workspace_bytes(int64_t M, int64_t N, int64_t K, bool reorder) {
+    const int64_t most = std::min(M, kMostRows);
+    const GemvWorkspace w = gemv_workspace(most, N, K, reorder, plan_gemv(most, N, K, reorder));
+    return w.reordered + w.partial;
 }
 
 arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
                         const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
                         hipStream_t stream) {
-    uint16_t* reordered = gemv_workspace_bytes(M, K, perm != nullptr) > 0 ? static_cast<uint16_t*>(workspace) : nullptr;
+    const int64_t most = std::min(M, kMostRows);
+    const GemvPlan p = plan_gemv(most, N, K, perm != nullptr);
+    const GemvWorkspace w = gemv_workspace(most, N, K, perm != nullptr, p);
+    uint16_t* reordered = w.reordered > 0 ? static_cast<uint16_t*>(workspace) : nullptr;
+    float* partial = w.partial > 0 ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.reordered) : nullptr;
     for (int64_t m = 0; m < M; m += kMostRows) {
-        // (the last run of rows may be short enough to be reordered on the way: it goes like the others all the same)
-        const GemvArgs a = {static_cast<const uint16_t*>(x) + m * ldx, std::min(M - m, kMostRows), K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream};
-        const arcq_status st = y_dtype == ARCQ_DTYPE_F16 ? launch_rows(block, a, static_cast<_Float16*>(y) + m * ldy, reordered)
-                                                         : launch_rows(block, a, static_cast<float*>(y) + m * ldy, reordered);
+        const int64_t rows = std::min(M - m, kMostRows);
+        const GemvArgs a = {static_cast<const uint16_t*>(x) + m * ldx, rows, K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream};
+        // (with more rows than a launch takes, the last run goes like the others, in one tile of 32 rows at least: what fits them fits it)
+        const arcq_status st = y_dtype == ARCQ_DTYPE_F16 ? launch_rows(block, a, p, static_cast<_Float16*>(y) + m * ldy, reordered, partial)
+                                                         : launch_rows(block, a, p, static_cast<float*>(y) + m * ldy, reordered, partial);
         if (st) return st;
     }
     return ARCQ_OK;

@@ -105,7 +105,7 @@ void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool two_passes,
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
                             int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream);
 // fp16 rows times packed weights (block 16: NVFP4, 32: MXFP4)
-size_t gemv_workspace_bytes(int64_t M, int64_t K, bool reorder);
+size_t gemv_workspace_bytes(int64_t M, int64_t N, int64_t K, bool reorder);
 arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
                         const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
                         hipStream_t stream);

@@ -63,7 +63,8 @@ def test_products(fmt, M, N, K, S, reorder):
 # asked for while the last, shorter turn of this one is multiplied.
 @pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
 @pytest.mark.parametrize("M,N,K", [(1, 8400, 4736), (1, 16700, 4192), (3, 8300, 4256), (6, 16600, 4352), (16, 33000, 4704), (20, 16500, 4896), (32, 8200, 9216),
-                                   (9, 4100, 4064), (9, 4096, 4096), (16, 100, 8224), (5, 2000, 10272)])
+                                   (9, 4100, 4064), (9, 4096, 4096), (16, 100, 8224), (5, 2000, 10272),
+                                   (2, 1001, 20512), (14, 4400, 14336), (32, 850, 9312), (40, 130, 16416), (23, 8482, 4128)])
 def test_tile_after_tile(fmt, M, N, K):
     say(f"gemv {fmt} M={M} N={N} K={K}")
     block = 32 if fmt == "mx" else 16

@@ -122,6 +122,19 @@ def test_gemv_argument_errors(call, block):
         size(4, 8, block // 2, False)
 
 
+@pytest.mark.parametrize("call,block", [(gemv, 16), (mx_gemv, 32)])
+def test_gemv_workspace_of_few_features(call, block):
+    """K in several runs where features alone do not fill the chip: partial results, with and without an order of the channels."""
+    size = B.arcq_gemv_workspace_size if block == 16 else B.arcq_mx_gemv_workspace_size
+    M, N, K = 3, 512, 28672
+    need = size(M, N, K, False)
+    assert need > 0 and need % (M * N * 4) == 0 and size(M, N, K, True) == need + M * K * 2
+    short = dict(M=M, N=N, K=K, S=0, ldx=K, ldy=N)
+    assert call(**short) == call(**short, ws=FAKE, wsb=need - 1) == B.WORKSPACE_TOO_SMALL
+    assert call(**short, ws=OFF16, wsb=need) == B.BAD_ALIGN
+    assert size(M, 64, 512, False) == size(M, 65536, 4096, False) == 0
+
+
 def test_gemv_tensor_scale():
     for bad in (0.0, -1.0, float("inf"), float("nan"), 2.0 ** -70, 2.0 ** 70):
         assert gemv(ts=bad) == B.INVALID_ARG
