@@ -68,7 +68,7 @@ typedef struct {
 } arcq_route;
 arcq_status arcq_gemm_route(int64_t M, int64_t N, int64_t Kp, arcq_route* route);
 arcq_status arcq_mx_gemm_route(int64_t M, int64_t N, int64_t Kp, int with_workspace, arcq_route* route);
-/* The same for arcq_mx8_gemm (ARCQ_ROUTE_STREAM or _TILES; operands of 4 GiB and more stream with any number of rows). */
+/* The same for arcq_mx8_gemm (ARCQ_ROUTE_STREAM or _TILES; weights of 4 GiB and more stream with any number of rows; past 65536 rows: of the first launch). */
 arcq_status arcq_mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, int y_dtype, int with_workspace, arcq_route* route);
 /*
  * Weight tiles of 16 rows that a wave takes in the launch that arcq_gemm_route / arcq_mx_gemm_route names, where that is a streaming kernel (else 0):

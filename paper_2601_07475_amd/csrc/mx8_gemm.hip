@@ -50,14 +50,16 @@ __device__ __forceinline__ void split_codes(const int8v& a, int8v& large, int8v&
 template <int MT, int NT, int WAVES, bool SPLIT, typename OutT>
 __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n) {
+    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n, uint32_t tiles_m, int splits) {
     // the partial tiles of BATCH weight tiles fit the static LDS limit at a time
     constexpr int BATCH = WAVES * MT * NT > 64 ? (NT + 1) / 2 : NT;
     __shared__ float red[WAVES][MT * BATCH][4][64];
     static_assert(sizeof(red) <= 64 * 1024, "partial tiles must fit the static LDS limit");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int i = lane & 15, q = lane >> 4;
-    const int n0 = (int)(blockIdx.x % tiles_n) * (16 * NT), m0 = (int)(blockIdx.x / tiles_n) * (16 * MT);
+    const uint32_t strip = blockIdx.x / tiles_n, split = strip / tiles_m;           // one of `splits` runs of K, with fp32 partial results of its own
+    const int n0 = (int)(blockIdx.x % tiles_n) * (16 * NT), m0 = (int)(strip % tiles_m) * (16 * MT);
+    y += (int64_t)split * M * N;
     const uint8_t *ac[MT], *as[MT], *wc[NT], *ws[NT];
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
@@ -98,7 +100,7 @@ __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
         }
     };
 
-    const int groups = nb >> 4;
+    const int groups = nb >> 4, group0 = (int)split * groups / splits, group1 = ((int)split + 1) * groups / splits;
     const uint32_t sel_half = half_selector(q), sel_byte = byte_selector(q);
     // scale bytes first: they are needed first, and loads retire in order
     auto load = [&](int g, int4v (&lo)[4][MT], int4v (&hi)[4][MT], uint4 (&cw)[4][NT], uint32_t (&sa)[MT], uint32_t (&sw)[NT]) {
@@ -128,15 +130,16 @@ __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
         multiply(lo[2], hi[2], cw[2], sa, sw, std::integral_constant<int, 2>{});
         multiply(lo[3], hi[3], cw[3], sa, sw, std::integral_constant<int, 3>{});
     };
-    for (int g = wave; g < groups; g += WAVES) {
+    for (int g = group0 + wave; g < group1; g += WAVES) {
         int4v lo[4][MT], hi[4][MT];
         uint4 cw[4][NT];
         uint32_t sa[MT], sw[NT];
         load(g, lo, hi, cw, sa, sw);
         compute(lo, hi, cw, sa, sw);
     }
-    const int chunks = (nb + 3) >> 2;               // what is left, a chunk at a time; the last one may hold fewer than four blocks
-    for (int c = 4 * groups + (wave - groups % WAVES + WAVES) % WAVES; c < chunks; c += WAVES) {
+    // what is left, a chunk at a time, in the last run; the last chunk may hold fewer than four blocks
+    const int chunks = (int)split + 1 == splits ? (nb + 3) >> 2 : 0;
+    for (int c = 4 * groups + (wave - (group1 - group0) % WAVES + WAVES) % WAVES; c < chunks; c += WAVES) {
         const int b = min(4 * c + q, nb - 1);       // blocks past the end: the last one's bytes, and weight codes of zero
         const bool ok = 4 * c + q < nb;
         const int a0 = min(128 * c + 16 * q, 32 * nb - 16), a1 = min(128 * c + 64 + 16 * q, 32 * nb - 16);
@@ -471,10 +474,10 @@ struct Mx8Args {
 };
 
 template <int MT, int NT, bool SPLIT, typename OutT>
-arcq_status launch_stream(const Mx8Args& a, OutT* y) {
+arcq_status launch_stream(const Mx8Args& a, OutT* y, int splits) {
     const unsigned tiles_n = ((unsigned)a.N + 16 * NT - 1) / (16 * NT), tiles_m = ((unsigned)a.M + 16 * MT - 1) / (16 * MT);
-    hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, SPLIT, OutT>), dim3(tiles_n * tiles_m), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
-                       a.nb, a.nbw, y, a.ldy, tiles_n);
+    hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, SPLIT, OutT>), dim3(tiles_n * tiles_m * (unsigned)splits), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
+                       a.nb, a.nbw, y, a.ldy, tiles_n, tiles_m, splits);
     return check_launch("mx8_stream_kernel");
 }
 
@@ -522,8 +525,9 @@ Mx8Plan stream_plan(int64_t M, int64_t N) {
 
 // A function of the sizes, the passes and whether there is a workspace: whatever a model of their times, fitted to measurements over 32 to 3000 rows,
 // N = 1024 .. 27648 and K = 4096 .. 14336, puts first (120 problems: 1.02x the fastest of all on average, with one or two passes).
-// The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'.  With more than 128 rows
-// it has what the tiles cannot address.
+// The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'; in several
+// runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 6.1 us, 16 x 1024 over 28672 20 -> 11).  With more than 128 rows it
+// has what the tiles cannot address.
 Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool two_passes, bool workspace) {
     const bool offsets_fit = (uint64_t)M * nb * 32 < 0xFFFF0000ull && (uint64_t)N * nbw * 16 < 0xFFFF0000ull;
     const Mx8Plan stream = stream_plan(M, N);
@@ -533,8 +537,16 @@ Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool two_passes,
     double least = 0.0;
     if (M <= 128) {
         const int64_t wgs = ((N + 16 * stream.nt - 1) / (16 * stream.nt)) * ((M + 16 * stream.mt - 1) / (16 * stream.mt));
-        best = stream;
-        least = 4.0 + (double)((wgs + 255) / 256) * ((double)nb / 16.0) * (double)(5 * stream.nt + 9 * stream.mt) * 0.023;
+        for (const int sp : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (sp > 1 && (!workspace || wgs * sp > 256 || nb < 32 * sp)) break;        // runs of at least 1024 k; split only where compute units are idle
+            double us = 4.0 + (double)((wgs * sp + 255) / 256) * ((double)nb / (16.0 * sp)) * (double)(5 * stream.nt + 9 * stream.mt) * 0.023;
+            if (sp > 1) us = 1.05 * (us + 3.5 + 0.25 * sp + (double)sp * (double)M * (double)N * 8.0 / 4.0e6);
+            if (least == 0.0 || us < least) {
+                least = us;
+                best = stream;
+                best.splits = sp;
+            }
+        }
     }
     for (const Tile& t : kTiles) {
         if (t.rest[two_passes] == 0.0) continue;
@@ -555,12 +567,13 @@ Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool two_passes,
     return best;
 }
 
-template <int WM, int WN, int NS, bool TWO, typename OutT>
-arcq_status launch_split_tiles(const Mx8Args& a, OutT* y, int splits, float* partial) {
-    if (splits == 1) return launch_tiles<WM, WN, NS, TWO>(a, y, 1, 0);
+// One run of K to y, or several to `partial`, and what adds them up; launch(args, output, splits, elements between runs).
+template <typename OutT, typename Launch>
+arcq_status launch_runs(const Mx8Args& a, OutT* y, int splits, float* partial, Launch launch) {
+    if (splits == 1) return launch(a, y, 1, (int64_t)0);
     Mx8Args run = a;
     run.ldy = a.N;
-    if (arcq_status st = launch_tiles<WM, WN, NS, TWO>(run, partial, splits, (int64_t)a.M * a.N)) return st;
+    if (arcq_status st = launch(run, partial, splits, (int64_t)a.M * a.N)) return st;
     return launch_splitk_reduce(partial, splits, a.M, a.N, 1.0f, y, std::is_same<OutT, _Float16>::value ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy, a.stream);
 }
 
@@ -569,7 +582,10 @@ arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
     constexpr bool TWO = !std::is_same<OutT, _Float16>::value;
     const Mx8Plan plan = plan_mx8(a.M, a.N, a.nb, a.nbw, TWO, partial != nullptr);
 #define ARCQ_MX8_TILES(WM_, WN_, NS_) \
-    if (plan.wm == WM_ && plan.wn == WN_) return launch_split_tiles<WM_, WN_, NS_, TWO>(a, y, plan.splits, partial)
+    if (plan.wm == WM_ && plan.wn == WN_) \
+        return launch_runs(a, y, plan.splits, partial, [](const Mx8Args& args, auto* out, int splits, int64_t stride) { \
+            return launch_tiles<WM_, WN_, NS_, TWO>(args, out, splits, stride); \
+        })
     if constexpr (!TWO) {
         if (plan.wm == 4 && plan.wn == 4 && plan.splits == 1) return launch_tiles<4, 4, 3, false>(a, y, 1, 0);
     }
@@ -581,7 +597,10 @@ arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
     ARCQ_MX8_TILES(1, 2, 4);
 #undef ARCQ_MX8_TILES
 #define ARCQ_MX8_STREAM(MT_, NT_) \
-    if (plan.wm == 0 && plan.mt == MT_ && plan.nt == NT_) return launch_stream<MT_, NT_, TWO>(a, y)
+    if (plan.wm == 0 && plan.mt == MT_ && plan.nt == NT_) \
+        return launch_runs(a, y, plan.splits, partial, [](const Mx8Args& args, auto* out, int splits, int64_t) { \
+            return launch_stream<MT_, NT_, TWO>(args, out, splits); \
+        })
     ARCQ_MX8_STREAM(1, 1);
     ARCQ_MX8_STREAM(1, 2);
     ARCQ_MX8_STREAM(1, 3);
@@ -599,22 +618,38 @@ arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
 
 }  // namespace
 
+// Rows of a launch: so many that the tiles can address them and grids stay within bounds, for any M.
+static int64_t rows_of_launch(int64_t N, int64_t K) {
+    const int64_t rows = std::min<int64_t>(0xFFFF0000ll / K, (1ll << 36) / std::max<int64_t>(N, 1)) & ~255ll;
+    return std::min<int64_t>(std::max<int64_t>(rows, 256), 1 << 16);
+}
+
 size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    M = std::min(M, rows_of_launch(N, K));
     const int one = plan_mx8(M, N, K >> 5, K >> 5, false, true).splits, two = plan_mx8(M, N, K >> 5, K >> 5, true, true).splits;
     const int most = std::max(one, two);
     return most > 1 ? (size_t)most * (size_t)M * (size_t)N * sizeof(float) : 0;
 }
 
 void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool two_passes, bool workspace, arcq_route* route) {
-    const Mx8Plan p = plan_mx8(M, N, K >> 5, (K + S) >> 5, two_passes, workspace);
-    *route = p.wm ? arcq_route{ARCQ_ROUTE_TILES, 64 * p.wm, 64 * p.wn, p.splits, 0} : arcq_route{ARCQ_ROUTE_STREAM, 16 * p.mt, 16 * p.nt, 1, 0};
+    const Mx8Plan p = plan_mx8(std::min(M, rows_of_launch(N, K)), N, K >> 5, (K + S) >> 5, two_passes, workspace);
+    *route = p.wm ? arcq_route{ARCQ_ROUTE_TILES, 64 * p.wm, 64 * p.wn, p.splits, 0} : arcq_route{ARCQ_ROUTE_STREAM, 16 * p.mt, 16 * p.nt, p.splits, 0};
 }
 
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
                             int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream) {
-    const Mx8Args a = {a_codes, a_scales, w_codes, w_scales, (int)M, (int)N, (int)(K >> 5), (int)((K + S) >> 5), ldy, stream};
     float* partial = static_cast<float*>(workspace);
-    return y_dtype == ARCQ_DTYPE_F16 ? launch_typed(a, static_cast<_Float16*>(y), partial) : launch_typed(a, static_cast<float*>(y), partial);
+    const int64_t most = rows_of_launch(N, K);
+    for (int64_t m = 0; m < M; m += most) {
+        const Mx8Args a = {a_codes + m * K, a_scales + m * (K >> 5), w_codes, w_scales, (int)std::min(M - m, most), (int)N, (int)(K >> 5),
+                           (int)((K + S) >> 5), ldy, stream};
+        // (a last run of fewer rows may have a plan of its own, with more runs of K than the workspace was made for: without them)
+        float* room = m == 0 || M - m >= most ? partial : nullptr;
+        const arcq_status st = y_dtype == ARCQ_DTYPE_F16 ? launch_typed(a, static_cast<_Float16*>(y) + m * ldy, room)
+                                                         : launch_typed(a, static_cast<float*>(y) + m * ldy, room);
+        if (st) return st;
+    }
+    return ARCQ_OK;
 }
 
 }  // namespace arcq

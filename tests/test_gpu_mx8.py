@@ -237,9 +237,13 @@ TILE_SHAPES = [(154, 66, 1888, 0, F16, True, (B.ROUTE_TILES, 64, 128, 3)), (149,
                (7457, 1649, 544, 0, F16, False, (B.ROUTE_TILES, 256, 256, 1)),
                (520, 2050, 8224, 0, F16, True, (B.ROUTE_TILES, 128, 128, 3)), (300, 4100, 8224, 0, F32, True, (B.ROUTE_TILES, 64, 256, 3)),
                (520, 4100, 6176, 0, F32, True, (B.ROUTE_TILES, 128, 256, 3))]
+# the streaming kernel with K in several runs, and with more rows than a launch takes
+STREAM_SHAPES = [(15, 112, 20640, 0, F16, True, (B.ROUTE_STREAM, 16, 16, 8)), (30, 40, 16416, 0, F32, True, (B.ROUTE_STREAM, 32, 16, 8)),
+                 (16, 1030, 28704, 224, F16, True, (B.ROUTE_STREAM, 16, 16, 3)), (128, 70, 8224, 0, F32, True, (B.ROUTE_STREAM, 32, 16, 6)),
+                 (15, 112, 20640, 0, F32, False, (B.ROUTE_STREAM, 16, 16, 1)), (65600, 40, 96, 0, F32, True, (B.ROUTE_TILES, 128, 128, 1))]
 
 
-@pytest.mark.parametrize("M,N,K,S,dtype,workspace,route", TILE_SHAPES)
+@pytest.mark.parametrize("M,N,K,S,dtype,workspace,route", TILE_SHAPES + STREAM_SHAPES)
 def test_gemm_tiles(M, N, K, S, dtype, workspace, route):
     say(f"mx8_gemm M={M} N={N} K={K} S={S} {dtype} on {route}")
     assert B.arcq_mx8_gemm_route(M, N, K, S, dtype, workspace) == route
