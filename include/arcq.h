@@ -314,7 +314,7 @@ arcq_status arcq_mx_pack_weight_ex(const void* w, int64_t N, int64_t K, int64_t 
  *   eight products of eight consecutive k up and drops what lies more than 13 bits below the largest's exponent, so before the output's
  *   rounding y is off by at most 2^-10 sum |a qw| 2^(sa+sw-254), measured 3e-5 of y (norms, outlier channels, K = 512) against fp16's 2e-4.
  *   a_*  MXFP8 activations [M, K];  w_*  weights of arcq_mx_pack_weight with this K and S in the plain layout (S = 0: plain MXFP4;
- *   not ARCQ_LAYOUT_INTERLEAVED with S > 0); all codes 16-byte aligned.  y as in arcq_gemm.
+ *   not ARCQ_LAYOUT_INTERLEAVED with S > 0); all codes 16-byte aligned; N <= 2^27.  y as in arcq_gemm.
  *   workspace  256-byte aligned, at least arcq_mx8_gemm_workspace_size bytes: few-tile problems then split K into runs whose fp32 partial
  *     results a second kernel adds in index order.  NULL: never split (the same result up to the order of the fp32 additions).
  *     Calls that share a workspace must not overlap.

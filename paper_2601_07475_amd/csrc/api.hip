@@ -551,7 +551,7 @@ arcq_status arcq_mx8_add_rmsnorm_quantize_act(const void* x, int64_t M, int64_t 
 
 static arcq_status check_mx8_gemm_shape(int64_t M, int64_t N, int64_t K, int64_t S) {
     if (arcq_status st = check_KS_mx(K, S)) return st;
-    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x7FFFFF00)     // (whole tiles of features are counted in 32 bits)
+    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x8000000)      // (a launch takes 32 rows of that many features at least)
         return fail(ARCQ_BAD_SHAPE, "M = %lld, N = %lld out of range", (long long)M, (long long)N);
     return ARCQ_OK;
 }

@@ -618,10 +618,10 @@ arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
 
 }  // namespace
 
-// Rows of a launch: so many that the tiles can address them and grids stay within bounds, for any M.
+// Rows of a launch: so many that the tiles can address them (4 GiB of codes) and a grid of the smallest tiles stays within 2^32 threads, for any M.
 static int64_t rows_of_launch(int64_t N, int64_t K) {
-    const int64_t rows = std::min<int64_t>(0xFFFF0000ll / K, (1ll << 36) / std::max<int64_t>(N, 1)) & ~255ll;
-    return std::min<int64_t>(std::max<int64_t>(rows, 256), 1 << 16);
+    const int64_t rows = std::min({0xFFFF0000ll / K, (1ll << 32) / std::max<int64_t>(N, 1), 1ll << 16}) & ~31ll;
+    return std::max<int64_t>(rows, 32);
 }
 
 size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {

@@ -128,3 +128,70 @@ def test_two_streams_at_once():
                 got.append(step(x, w))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for p, q in zip(got, want) for a, b in zip(p, q))
+
+
+def test_runs_of_k_in_a_captured_graph():
+    """Few features over many channels: partial results in the workspace and a second launch, replayed."""
+    say("graph capture of products with K in several runs")
+    M, N, K = 9, 200, 12320
+    assert B.arcq_mx8_gemm_route(M, N, K, 0, torch.float16, True)[3] > 1 and B.arcq_mx_gemv_workspace_size(M, N, K, False) > 0
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    ins = [torch.randn((M, K), device="cuda", generator=gen).half() for _ in range(4)]
+    x, perm = ins[0].clone(), torch.randperm(K, device="cuda", generator=gen).int()
+    wc = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda", generator=gen)
+    mx, nv = (torch.randint(lo, hi, (N, K // b), dtype=torch.uint8, device="cuda", generator=gen) for lo, hi, b in ((115, 122, 32), (40, 60, 16)))
+    c, s = torch.empty((M, K), dtype=torch.uint8, device="cuda"), torch.empty((M, K // 32), dtype=torch.uint8, device="cuda")
+    ys = [torch.empty((M, N), dtype=t, device="cuda") for t in (torch.float16, torch.float32, torch.float32)]
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+
+    def step():
+        B.arcq_mx8_quantize_act(x, perm, codes=c, scales=s)
+        B.arcq_mx8_gemm(c, s, wc, mx, y=ys[0], workspace=ws)
+        B.arcq_mx_gemv(x, perm, wc, mx, y=ys[1], workspace=ws)
+        B.arcq_gemv(x, None, wc, nv, 0.5, y=ys[2], workspace=ws)
+
+    _replays_match(step, step, [c, s, *ys], lambda i: x.copy_(ins[i]))
+
+
+def test_weights_past_32_bit_offsets():
+    """131200 features over 65536 channels, 4.3 GB of codes: the last rows of weights against the oracle."""
+    say("weights of more than 4 GiB")
+    N, K, M = 131200, 65536, 2
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    codes = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda", generator=gen)
+    mx, nv = (torch.randint(lo, hi, (N, K // b), dtype=torch.uint8, device="cuda", generator=gen) for lo, hi, b in ((115, 122, 32), (40, 60, 16)))
+    x = torch.randn((M, K), device="cuda", generator=gen).half()
+    c, s = B.arcq_mx8_quantize_act(x)
+    got = [B.arcq_gemv(x, None, codes, nv, 0.5, out_dtype=torch.float32), B.arcq_mx_gemv(x, None, codes, mx, out_dtype=torch.float32),
+           B.arcq_mx8_gemm(c, s, codes, mx, out_dtype=torch.float32)]
+    X, cn, sn = x.cpu().numpy(), c.cpu().numpy(), s.cpu().numpy()
+    for rows in (slice(0, 20), slice(N - 20, N)):
+        w, wm, wn = codes[rows].cpu().numpy(), mx[rows].cpu().numpy(), nv[rows].cpu().numpy()
+        for y, (want, mag) in zip(got, (M8.gemv(X, None, w, wn, np.float32(0.5)), M8.gemv(X, None, w, wm), M8.gemm(cn, sn, w, wm))):
+            assert_product(y[:, rows], want, mag, K)
+
+
+def test_rows_past_32_bit_offsets():
+    """65600 rows of 65536 channels, 4.3 GB of MXFP8 codes and 8.6 GB of fp16: quantized, normalised and multiplied; the last rows against the oracle."""
+    say("activations of more than 4 GiB")
+    M, N, K = 65600, 40, 65536
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.empty((M, K), dtype=torch.float16, device="cuda")
+    for r in range(0, M, 4100):
+        x[r:r + 4100] = torch.randn((4100, K), device="cuda", generator=gen)
+    w = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda", generator=gen)
+    mx = torch.randint(115, 122, (N, K // 32), dtype=torch.uint8, device="cuda", generator=gen)
+    gamma = (1 + 0.1 * torch.randn(K, device="cuda", generator=gen)).half()
+    c, s = B.arcq_mx8_quantize_act(x)
+    nc, ns, _ = B.arcq_mx8_add_rmsnorm_quantize_act(x, None, gamma, 1e-5)
+    y = B.arcq_mx8_gemm(c, s, w, mx, out_dtype=torch.float32)
+    v = B.arcq_mx_gemv(x, None, w, mx, out_dtype=torch.float32)
+    wn, mn = w.cpu().numpy(), mx.cpu().numpy()
+    for rows in (slice(0, 3), slice(65500, 65510), slice(65534, 65538), slice(M - 3, M)):
+        X, cn, sn = x[rows].cpu().numpy(), c[rows].cpu().numpy(), s[rows].cpu().numpy()
+        for got, want in zip((cn, sn), M8.quantize_act(X)):
+            assert_same_bytes(got, want, "quantized")
+        for got, want in zip((nc[rows].cpu().numpy(), ns[rows].cpu().numpy()), M8.add_rmsnorm_quantize_act(X, None, gamma.cpu().numpy(), 1e-5)[:2]):
+            assert_same_bytes(got, want, "normalised")
+        assert_product(y[rows], *M8.gemm(cn, sn, wn, mn), K)
+        assert_product(v[rows], *M8.gemv(X, None, wn, mn), K)
