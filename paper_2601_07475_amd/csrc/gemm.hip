@@ -776,16 +776,32 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
     for (int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; idx < total; idx += (int64_t)gridDim.x * blockDim.x) {
         if (vec4) {
             const int64_t m = idx / (N >> 2), n = 4 * (idx % (N >> 2));
-            float4 sum = *reinterpret_cast<const float4*>(part + m * N + n);
-            for (int sp = 1; sp < splits; ++sp) {
-                const float4 v = *reinterpret_cast<const float4*>(part + sp * split_stride + m * N + n);
-                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+            const float* at = part + m * N + n;
+            float4 sum = *reinterpret_cast<const float4*>(at);
+            auto add = [&](const float4& v) { sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w; };
+            int sp = 1;
+            for (; sp + 3 < splits; sp += 4) {              // four runs' results in flight at once
+                float4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(at + (sp + k) * split_stride);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) add(v[k]);
             }
+            for (; sp < splits; ++sp) add(*reinterpret_cast<const float4*>(at + sp * split_stride));
             store4(y + m * ldy + n, sum.x * alpha, sum.y * alpha, sum.z * alpha, sum.w * alpha);
         } else {
             const int64_t m = idx / N, n = idx % N;
-            float sum = part[m * N + n];
-            for (int sp = 1; sp < splits; ++sp) sum += part[sp * split_stride + m * N + n];
+            const float* at = part + m * N + n;
+            float sum = *at;
+            int sp = 1;
+            for (; sp + 3 < splits; sp += 4) {
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = at[(sp + k) * split_stride];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum += v[k];
+            }
+            for (; sp < splits; ++sp) sum += at[sp * split_stride];
             store_out(y + m * ldy + n, sum * alpha);
         }
     }

@@ -441,7 +441,7 @@ arcq_status launch_tiles(const GemvArgs& a, int splits, OutT* y) {
     const size_t rows = X == WHOLE ? (size_t)a.M * a.K * 4 : (size_t)WAVES * slice_bytes(ROWS, NT, WAVES);
     const size_t lds = rows + 2 * (size_t)WAVES * ((ROWS + 15) / 16) * NT * 1024;
     const int64_t tiles_n = (a.N + 16 * NT - 1) / (16 * NT), tiles_m = (a.M + ROWS - 1) / ROWS;
-    const int per_cu = ROWS == 4 && WAVES == 8 && lds <= 80 * 1024 ? 2 : 1;       // as registers and LDS allow
+    const int per_cu = ROWS == 4 ? 2 : 1;           // as registers and LDS allow
     const unsigned stride = (unsigned)std::min<int64_t>(tiles_n, std::max(num_cu() * per_cu / splits, 1));
     hipLaunchKernelGGL(kern, dim3(stride * (unsigned)(splits * tiles_m)), dim3(64 * WAVES), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
                        a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride, (uint32_t)splits);
