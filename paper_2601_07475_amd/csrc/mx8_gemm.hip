@@ -526,7 +526,7 @@ Mx8Plan stream_plan(int64_t M, int64_t N) {
 // A function of the sizes, the passes and whether there is a workspace: whatever a model of their times, fitted to measurements over 32 to 3000 rows,
 // N = 1024 .. 27648 and K = 4096 .. 14336, puts first (120 problems: 1.02x the fastest of all on average, with one or two passes).
 // The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'; in several
-// runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 6.1 us, 16 x 1024 over 28672 20 -> 11).  With more than 128 rows it
+// runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 5.5 us, 15 x 112 over 20640 14.3 -> 6.4).  With more than 128 rows it
 // has what the tiles cannot address.
 Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool two_passes, bool workspace) {
     const bool offsets_fit = (uint64_t)M * nb * 32 < 0xFFFF0000ull && (uint64_t)N * nbw * 16 < 0xFFFF0000ull;
