@@ -117,12 +117,8 @@ def _stream():
         return torch.cuda.current_stream().cuda_stream
 
 
-def _device():
-    """Index of the current device (by torch's private function for it, as in _stream)."""
-    try:
-        return torch._C._cuda_getDevice()
-    except AttributeError:
-        return torch.cuda.current_device()
+#: Index of the current device, by torch's private function for it where there is one (as in _stream).
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _ptr(t):
@@ -347,29 +343,25 @@ def arcq_mx_gemm(a_codes, a_scales, w_codes, w_scales, out_dtype=torch.float16, 
     return y
 
 
-# The calls from here to arcq_mx_gemv want every tensor on the current device, whose current stream they use.
+# The calls from here to arcq_mx_gemv want every tensor on the current device, whose current stream they use.  Every property asked of a tensor
+# takes some 80 ns, a third of such a call's time on the host in all.
+_HALF, _FLOAT, _BYTE, _INT = torch.float16, torch.float32, torch.uint8, torch.int32
+
 
 def _fp16_rows(t, device):
     """(rows, K, pitch) of fp16 rows, checked."""
-    assert t.get_device() == device and t.dtype is torch.float16
+    assert t.get_device() == device and t.dtype is _HALF
     rows, cols = t.shape
     pitch, step = t.stride()
     assert step == 1 or cols <= 1
     return rows, cols, pitch if rows > 1 else max(cols, pitch)
 
 
-def _input_rows(x):
-    """(device, rows, K, pitch) of a call's fp16 rows, which have to be on the current device."""
-    assert x.is_cuda
-    device = _device()
-    return device, *_fp16_rows(x, device)
-
-
 def _perm(perm, K, device):
     """Address of perm, checked; none for None."""
     if perm is None:
         return None
-    assert perm.get_device() == device and perm.dtype is torch.int32 and perm.is_contiguous()
+    assert perm.get_device() == device and perm.dtype is _INT and perm.is_contiguous()
     if perm.numel() != K:
         raise ArcqError(BAD_SHAPE, "perm must have K entries")
     return perm.data_ptr()
@@ -377,11 +369,11 @@ def _perm(perm, K, device):
 
 def _mx8_outputs(x, rows, K, codes, scales, device):
     if codes is None:
-        codes = x.new_empty((rows, K), dtype=torch.uint8)
+        codes = x.new_empty((rows, K), dtype=_BYTE)
     if scales is None:
-        scales = x.new_empty((rows, K // 32), dtype=torch.uint8)
-    assert codes.get_device() == device and codes.dtype is torch.uint8 and codes.numel() == rows * K and codes.is_contiguous()
-    assert scales.get_device() == device and scales.dtype is torch.uint8 and scales.numel() == rows * (K // 32) and scales.is_contiguous()
+        scales = x.new_empty((rows, K // 32), dtype=_BYTE)
+    assert codes.get_device() == device and codes.dtype is _BYTE and codes.numel() == rows * K and codes.is_contiguous()
+    assert scales.get_device() == device and scales.dtype is _BYTE and scales.numel() == rows * (K // 32) and scales.is_contiguous()
     return codes, scales
 
 
@@ -391,19 +383,24 @@ def arcq_mx8_packed_sizes(rows, K):
     return c.value, s.value
 
 
+def _mx8_quantize_args(x, perm, flags, codes, scales):
+    device = _device()
+    rows, K, ldx = _fp16_rows(x, device)
+    codes, scales = _mx8_outputs(x, rows, K, codes, scales, device)
+    return (x.data_ptr(), rows, K, ldx, _perm(perm, K, device), flags, codes.data_ptr(), scales.data_ptr(), _stream()), codes, scales
+
+
 def arcq_mx8_quantize_act(x, perm=None, flags=0, codes=None, scales=None):
     """MXFP8: x fp16 [M, K] -> (codes uint8 [M, K], E4M3; scales uint8 [M, K/32], E8M0), channels in the order perm or their own."""
-    device, rows, K, ldx = _input_rows(x)
-    codes, scales = _mx8_outputs(x, rows, K, codes, scales, device)
-    _check(lib().arcq_mx8_quantize_act(x.data_ptr(), rows, K, ldx, _perm(perm, K, device), flags, codes.data_ptr(), scales.data_ptr(), _stream()))
+    args, codes, scales = _mx8_quantize_args(x, perm, flags, codes, scales)
+    _check(lib().arcq_mx8_quantize_act(*args))
     return codes, scales
 
 
-def arcq_mx8_add_rmsnorm_quantize_act(x, residual, gamma, eps, perm=None, flags=0, hidden=None, codes=None, scales=None):
-    """hidden = x + residual, RMSNorm (weight gamma fp16 [K], eps) and arcq_mx8_quantize_act as one kernel -> (codes, scales, hidden).
-    hidden may be x or residual (in place).  residual None: the norm of x itself, hidden is None."""
-    device, rows, K, ldx = _input_rows(x)
-    assert gamma.get_device() == device and gamma.dtype is torch.float16 and gamma.is_contiguous() and gamma.numel() == K
+def _mx8_norm_args(x, residual, gamma, eps, perm, flags, hidden, codes, scales):
+    device = _device()
+    rows, K, ldx = _fp16_rows(x, device)
+    assert gamma.get_device() == device and gamma.dtype is _HALF and gamma.is_contiguous() and gamma.numel() == K
     codes, scales = _mx8_outputs(x, rows, K, codes, scales, device)
     if residual is None:
         assert hidden is None
@@ -414,17 +411,24 @@ def arcq_mx8_add_rmsnorm_quantize_act(x, residual, gamma, eps, perm=None, flags=
         (rows_r, K_r, ldr), (rows_h, K_h, ldh) = _fp16_rows(residual, device), _fp16_rows(hidden, device)
         assert rows_r == rows == rows_h and K_r == K == K_h
         r, h = residual.data_ptr(), hidden.data_ptr()
-    _check(lib().arcq_mx8_add_rmsnorm_quantize_act(x.data_ptr(), rows, K, ldx, r, ldr, h, ldh, gamma.data_ptr(), eps,
-                                                   _perm(perm, K, device), flags, codes.data_ptr(), scales.data_ptr(), _stream()))
+    return (x.data_ptr(), rows, K, ldx, r, ldr, h, ldh, gamma.data_ptr(), eps, _perm(perm, K, device), flags, codes.data_ptr(),
+            scales.data_ptr(), _stream()), codes, scales, hidden
+
+
+def arcq_mx8_add_rmsnorm_quantize_act(x, residual, gamma, eps, perm=None, flags=0, hidden=None, codes=None, scales=None):
+    """hidden = x + residual, RMSNorm (weight gamma fp16 [K], eps) and arcq_mx8_quantize_act as one kernel -> (codes, scales, hidden).
+    hidden may be x or residual (in place).  residual None: the norm of x itself, hidden is None."""
+    args, codes, scales, hidden = _mx8_norm_args(x, residual, gamma, eps, perm, flags, hidden, codes, scales)
+    _check(lib().arcq_mx8_add_rmsnorm_quantize_act(*args))
     return codes, scales, hidden
 
 
 def _packed_weights(w_codes, w_scales, K, block, device):
     """(N, S) of packed weights [N, K + S], checked."""
-    assert w_codes.get_device() == device and w_codes.dtype is torch.uint8 and w_codes.is_contiguous()
-    assert w_scales.get_device() == device and w_scales.dtype is torch.uint8 and w_scales.is_contiguous()
+    assert w_codes.get_device() == device and w_codes.dtype is _BYTE and w_codes.is_contiguous()
+    assert w_scales.get_device() == device and w_scales.dtype is _BYTE and w_scales.is_contiguous()
     N, half = w_codes.shape
-    if 2 * half < K or w_scales.shape != (N, 2 * half // block):
+    if 2 * half < K or w_scales.numel() != N * (2 * half // block):
         raise ArcqError(BAD_SHAPE, "operand shapes disagree on K and S")
     return N, 2 * half - K
 
@@ -433,14 +437,14 @@ def _output(a, M, N, out_dtype, y, device):
     """(y, its type, its pitch): the caller's, checked, or a new one."""
     if y is None:
         y = a.new_empty((M, N), dtype=out_dtype)
-    assert y.get_device() == device and y.shape == (M, N)
+    rows, cols = y.shape
     pitch, step = y.stride()
-    assert step == 1 or N <= 1
+    assert y.get_device() == device and rows == M and cols == N and (step == 1 or N <= 1)
     if M <= 1:
         pitch = max(N, pitch)
-    if y.dtype is torch.float16:
+    if y.dtype is _HALF:
         return y, DTYPE_F16, pitch
-    assert y.dtype is torch.float32
+    assert y.dtype is _FLOAT
     return y, DTYPE_F32, pitch
 
 
@@ -450,20 +454,24 @@ def arcq_mx8_gemm_workspace_size(M, N, K):
     return b.value
 
 
+def _mx8_gemm_args(a_codes, a_scales, w_codes, w_scales, out_dtype, y, workspace):
+    device = _device()
+    assert a_codes.get_device() == device and a_codes.dtype is _BYTE and a_codes.is_contiguous()
+    assert a_scales.get_device() == device and a_scales.dtype is _BYTE and a_scales.is_contiguous()
+    M, K = a_codes.shape
+    N, S = _packed_weights(w_codes, w_scales, K, 32, device)
+    if a_scales.numel() != M * (K // 32):
+        raise ArcqError(BAD_SHAPE, "activation shapes disagree on K")
+    y, dt, ldy = _output(a_codes, M, N, out_dtype, y, device)
+    return (a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, S, y.data_ptr(), dt, ldy,
+            *_scratch(workspace, device), _stream()), y
+
+
 def arcq_mx8_gemm(a_codes, a_scales, w_codes, w_scales, out_dtype=torch.float16, y=None, workspace=None):
     """y[M, N] = MXFP8 activations [M, K] times MXFP4 weights packed [N, K + S] (the S repeated columns are passed over); returns y.
     workspace: a uint8 tensor of at least arcq_mx8_gemm_workspace_size bytes lets few-tile problems split K."""
-    assert a_codes.is_cuda and a_codes.dtype is torch.uint8 and a_codes.is_contiguous()
-    device = _device()
-    assert a_codes.get_device() == device == a_scales.get_device() and a_scales.dtype is torch.uint8 and a_scales.is_contiguous()
-    M, K = a_codes.shape
-    N, S = _packed_weights(w_codes, w_scales, K, 32, device)
-    if a_scales.shape != (M, K // 32):
-        raise ArcqError(BAD_SHAPE, "activation shapes disagree on K")
-    y, dt, ldy = _output(a_codes, M, N, out_dtype, y, device)
-    ws, ws_bytes = _scratch(workspace, device)
-    _check(lib().arcq_mx8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, S, y.data_ptr(), dt, ldy,
-                               ws, ws_bytes, _stream()))
+    args, y = _mx8_gemm_args(a_codes, a_scales, w_codes, w_scales, out_dtype, y, workspace)
+    _check(lib().arcq_mx8_gemm(*args))
     return y
 
 
@@ -496,11 +504,13 @@ def arcq_mx_gemv_workspace_size(M, N, K, with_perm):
 
 
 def _gemv(size, block, x, perm, w_codes, w_scales, out_dtype, y, workspace):
-    """Arguments of a product of fp16 rows with packed weights: what comes before the weights' scale, what comes behind it, and y."""
-    device, M, K, ldx = _input_rows(x)
+    """Arguments of a product of fp16 rows with packed weights: what comes before the weights' scale, what comes behind it, and y.
+    size: tells the bytes of a workspace to be made where none is given."""
+    device = _device()
+    M, K, ldx = _fp16_rows(x, device)
     N, S = _packed_weights(w_codes, w_scales, K, block, device)
     y, dt, ldy = _output(x, M, N, out_dtype, y, device)
-    if workspace is None:
+    if workspace is None and size is not None:
         need = size(M, N, K, perm is not None)
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     return ((x.data_ptr(), M, K, ldx, _perm(perm, K, device), w_codes.data_ptr(), w_scales.data_ptr()),
@@ -565,6 +575,35 @@ def prepare_gemm(a_codes, a_scales, a_tensor_scale, w_codes, w_scales, w_tensor_
             float(w_tensor_scale), M, N, Kp, _ptr(y), DTYPE_F16 if y.dtype == torch.float16 else DTYPE_F32,
             y.stride(0) if M > 1 else N, _ptr(workspace) if workspace is not None else None, ws_bytes, _stream())
     return _prepared(fn, args)
+
+
+def prepare_mx8_quantize_act(x, perm, flags, codes, scales):
+    """Same for arcq_mx8_quantize_act."""
+    assert codes is not None and scales is not None
+    return _prepared(lib().arcq_mx8_quantize_act, _mx8_quantize_args(x, perm, flags, codes, scales)[0])
+
+
+def prepare_mx8_add_rmsnorm_quantize_act(x, residual, gamma, eps, perm, flags, hidden, codes, scales):
+    """Same for arcq_mx8_add_rmsnorm_quantize_act."""
+    assert codes is not None and scales is not None and (hidden is None) == (residual is None)
+    return _prepared(lib().arcq_mx8_add_rmsnorm_quantize_act, _mx8_norm_args(x, residual, gamma, eps, perm, flags, hidden, codes, scales)[0])
+
+
+def prepare_mx8_gemm(a_codes, a_scales, w_codes, w_scales, y, workspace=None):
+    """Same for arcq_mx8_gemm."""
+    return _prepared(lib().arcq_mx8_gemm, _mx8_gemm_args(a_codes, a_scales, w_codes, w_scales, y.dtype, y, workspace)[0])
+
+
+def prepare_gemv(x, perm, w_codes, w_scales, w_tensor_scale, y, workspace=None):
+    """Same for arcq_gemv; where it needs a workspace, the caller's."""
+    head, tail, _ = _gemv(None, 16, x, perm, w_codes, w_scales, y.dtype, y, workspace)
+    return _prepared(lib().arcq_gemv, (*head, w_tensor_scale, *tail))
+
+
+def prepare_mx_gemv(x, perm, w_codes, w_scales, y, workspace=None):
+    """Same for arcq_mx_gemv."""
+    head, tail, _ = _gemv(None, 32, x, perm, w_codes, w_scales, y.dtype, y, workspace)
+    return _prepared(lib().arcq_mx_gemv, (*head, *tail))
 
 
 def prepare_mx_quantize_act(x, perm, S, codes, scales):

@@ -195,3 +195,40 @@ def test_rows_past_32_bit_offsets():
             assert_same_bytes(got, want, "normalised")
         assert_product(y[rows], *M8.gemm(cn, sn, wn, mn), K)
         assert_product(v[rows], *M8.gemv(X, None, wn, mn), K)
+
+
+def test_prepared_calls():
+    """Arguments checked and converted once: captured and replayed, the plain calls' results."""
+    say("prepared calls")
+    m, M = model(9), 21
+    g, pu = dev(m["gamma"]), dev(m["p_up"])
+    up, nv, ts = [dev(t) for t in m["up"]], [dev(t) for t in m["up_nv"]], float(m["ts"])
+    ins = [(torch.randn((M, D), device="cuda") * 2).half() for _ in range(4)]
+    x, r = ins[0].clone(), ins[1].clone()
+    h, y = torch.empty((M, D), dtype=torch.float16, device="cuda"), torch.empty((M, FF), dtype=torch.float16, device="cuda")
+    v, w = (torch.empty((M, FF), dtype=torch.float32, device="cuda") for _ in range(2))
+    c1, s1, c2, s2 = (torch.empty(s, dtype=torch.uint8, device="cuda") for s in ((M, D), (M, D // 32), (M, D), (M, D // 32)))
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+
+    def capture():
+        B.prepare_mx8_add_rmsnorm_quantize_act(x, r, g, 1e-5, pu, 0, h, c1, s1)()
+        B.prepare_mx8_quantize_act(x, None, B.SCALE_ROUND_UP, c2, s2)()
+        B.prepare_mx8_gemm(c1, s1, *up, y, ws)()
+        B.prepare_gemv(x, pu, *nv, ts, v, ws)()
+        B.prepare_mx_gemv(x, pu, *up, w, ws)()
+
+    def eager():
+        B.arcq_mx8_add_rmsnorm_quantize_act(x, r, g, 1e-5, pu, hidden=h, codes=c1, scales=s1)
+        B.arcq_mx8_quantize_act(x, None, B.SCALE_ROUND_UP, c2, s2)
+        B.arcq_mx8_gemm(c1, s1, *up, y=y, workspace=ws)
+        B.arcq_gemv(x, pu, *nv, ts, y=v, workspace=ws)
+        B.arcq_mx_gemv(x, pu, *up, y=w, workspace=ws)
+
+    _replays_match(capture, eager, [h, y, v, w, c1, s1, c2, s2], lambda i: x.copy_(ins[i]))
+    with pytest.raises(B.ArcqError):
+        B.prepare_mx_gemv(x, pu, *up, w)()          # 21 rows are reordered into a workspace
+    for hidden, codes in ((None, c1), (h, None)):
+        with pytest.raises(AssertionError):
+            B.prepare_mx8_add_rmsnorm_quantize_act(x, r, g, 1e-5, pu, 0, hidden, codes, s1)
+    with pytest.raises(AssertionError):
+        B.prepare_mx8_quantize_act(x, None, 0, c2, None)
