@@ -22,7 +22,7 @@
 //   NVFP4   4096 features,  4096 channels                                    4.7   2.0     5.0   1.9     6.2   1.5     8.4   1.1
 //          27648            5120                                            20.9   3.8    24.6   3.2    29.7   2.7    43.6   1.8
 //           8192           28672                                            29.9   4.4    35.8   3.7    42.6   3.1    59.8   2.2
-//   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    13.9   2.2    21.8   1.4
+//   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    13.9   2.2    17.9   1.7
 // From 1 to 4 rows the weights' way from memory and the tiles' uneven shares bound it, with more the rows, too: every workgroup reads all of them
 // (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).
 #include "gemm_decode.h"

@@ -13,6 +13,9 @@
 //   4-bit operand  k = 32 q .. 32 q + 31                                   16 bytes: one block
 //   8-bit operand  k = 16 q .. 16 q + 15 and half of the step's k further  32 bytes: half of one block, half of another
 //   scale          of block q of the step, for either operand
+// Measured: 8192 x 8192 over K = 28672 1.39 to 1.44 ms (2.7 PFLOP/s; from registers alone, with random codes and every compute unit busy, the instruction
+// reaches 3.8 at 1.82 GHz: power), fp32 output 2.7 ms; 777 x 6147 over 4352 fp32 54 us (two passes take 22 on the matrix unit); 300 x 4096 over
+// 14336 35 us; streaming: 16 x 14336 over 4096 8.8 us (3.6 TB/s of weights), 1 x 4096 over 4096 4.3.
 #include "code_rows.h"
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
