@@ -100,7 +100,7 @@ size_t mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t Kp);
 arcq_status launch_mx8_quantize(const void* x, int64_t ldx, const void* residual, int64_t ldr, void* hidden, int64_t ldh, int64_t rows, int64_t K,
                                 const void* gamma, float eps, const int32_t* perm, uint8_t* codes, uint8_t* scales, uint32_t flags, hipStream_t stream);
 size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
-void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool two_passes, bool workspace, arcq_route* route);
+void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool fp32, bool workspace, arcq_route* route);
 // workspace: fp32 partial results of a split reduction dimension, or null (never splits)
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
                             int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream);
