@@ -28,6 +28,7 @@
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
+#include <utility>
 
 namespace arcq {
 
@@ -466,7 +467,7 @@ struct Mx8Args {
 };
 
 template <int MT, int NT, typename OutT>
-arcq_status launch_stream(const Mx8Args& a, OutT* y, int splits) {
+arcq_status launch_stream(const Mx8Args& a, OutT* y, int splits, int64_t /* runs of the workspace are M N apart */) {
     const unsigned tiles_n = ((unsigned)a.N + 16 * NT - 1) / (16 * NT), tiles_m = ((unsigned)a.M + 16 * MT - 1) / (16 * MT);
     hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, OutT>), dim3(tiles_n * tiles_m * (unsigned)splits), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
                        a.nb, a.nbw, y, a.ldy, tiles_n, tiles_m, splits);
@@ -485,24 +486,29 @@ arcq_status launch_tiles(const Mx8Args& a, OutT* y, int splits, int64_t split_st
     return check_launch("mx8_tile_kernel");
 }
 
-// The tiles, by fragment rows and columns of a wave, and what a unit and the rest of a tile take (us): with few workgroups, and with every compute
-// unit busy, where two smaller ones share one and large ones meet the power limit.  [0]: fp16 output, [1]: fp32; either fitted to measured times.
+// The tiles that there are, by fragment rows and columns of a wave and slots of the ring, and what a unit and the rest of a tile take (us): with few
+// workgroups, and with every compute unit busy, where two smaller ones share one and large ones meet the power limit.  [0]: fp16 output, [1]: fp32 (the
+// rest: also of several runs of K, which store fp32); either fitted to measured times.  Plans and the launches below are made from this list.
 struct Tile {
-    int wm, wn;
+    int wm, wn, ns;
     double unit_few[2], unit_all[2], rest[2];
 };
 constexpr Tile kTiles[] = {
-    {4, 4, {2.55, 0.00}, {2.42, 0.00}, {0.3, 0.0}},      // (fp32 output: registers in scratch)
-    {3, 4, {2.10, 1.96}, {2.00, 2.17}, {0.7, 5.0}},
-    {2, 4, {1.59, 1.36}, {1.50, 1.56}, {0.4, 4.0}},
-    {3, 2, {1.53, 1.30}, {1.34, 1.45}, {0.6, 3.5}},
-    {2, 2, {0.82, 1.00}, {0.88, 0.81}, {1.1, 2.5}},
-    {1, 4, {0.90, 0.95}, {0.80, 0.89}, {0.8, 2.0}},
-    {1, 2, {0.49, 0.56}, {0.40, 0.46}, {0.8, 1.5}},
+    {4, 4, 3, {2.55, 0.00}, {2.42, 0.00}, {0.3, 0.0}},      // fp16 output only: with fp32, registers go to scratch
+    {3, 4, 3, {2.10, 1.96}, {2.00, 2.17}, {0.7, 5.0}},
+    {2, 4, 4, {1.59, 1.36}, {1.50, 1.56}, {0.4, 4.0}},
+    {3, 2, 4, {1.53, 1.30}, {1.34, 1.45}, {0.6, 3.5}},
+    {2, 2, 3, {0.82, 1.00}, {0.88, 0.81}, {1.1, 2.5}},
+    {1, 4, 5, {0.90, 0.95}, {0.80, 0.89}, {0.8, 2.0}},
+    {1, 2, 4, {0.49, 0.56}, {0.40, 0.46}, {0.8, 1.5}},
 };
+constexpr int kTileCount = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
+constexpr int first_tile(bool fp32) { return fp32 ? 1 : 0; }
+// Most weight tiles a wave of the streaming kernel, with one and with two tiles of 16 rows.
+constexpr int kStreamTiles[2] = {7, 4};
 
 struct Mx8Plan {
-    int wm = 0, wn = 0, splits = 1;             // wm = 0: the streaming kernel, 16 mt rows by 16 nt weight rows
+    int tile = -1, splits = 1;                  // of kTiles, or the streaming kernel with 16 mt rows by 16 nt weight rows
     int mt = 0, nt = 0;
 };
 
@@ -511,7 +517,7 @@ Mx8Plan stream_plan(int64_t M, int64_t N) {
     const int64_t tiles = (N + 15) / 16;
     Mx8Plan p;
     p.mt = M <= 16 ? 1 : 2;
-    p.nt = (int)std::min<int64_t>(tiles <= 1024 ? (tiles + 255) / 256 : p.mt == 1 ? (tiles + 255) / 256 : 4, 7);
+    p.nt = (int)std::min<int64_t>((tiles + 255) / 256, kStreamTiles[p.mt - 1]);
     return p;
 }
 
@@ -540,72 +546,60 @@ Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool fp32, bool 
             }
         }
     }
-    for (const Tile& t : kTiles) {
-        if (t.rest[fp32] == 0.0) continue;
+    for (int i = first_tile(fp32); i < kTileCount; ++i) {
+        const Tile& t = kTiles[i];
         const int64_t tiles = ((M + 64 * t.wm - 1) / (64 * t.wm)) * ((N + 64 * t.wn - 1) / (64 * t.wn));
         if (tiles > 0x7FFFFFFF / 8) continue;
         // runs of at least four units; split only where tiles leave compute units idle
-        for (int64_t sp = 1; sp <= (workspace && tiles <= 256 ? std::min<int64_t>(8, units / 4) : 1) || sp == 1; ++sp) {
+        const int64_t most = workspace && tiles <= 256 && i >= first_tile(true) ? std::min<int64_t>(8, units / 4) : 1;
+        for (int64_t sp = 1; sp == 1 || sp <= most; ++sp) {
             const int64_t work = tiles * sp;
             const double unit = work >= 256 ? t.unit_all[fp32] : t.unit_few[fp32];
-            double us = 3.0 + (double)((work + 255) / 256) * ((double)((units + sp - 1) / sp) * unit + t.rest[fp32]);
+            double us = 3.0 + (double)((work + 255) / 256) * ((double)((units + sp - 1) / sp) * unit + t.rest[fp32 || sp > 1]);
             if (sp > 1) us += 3.5 + (double)sp * (double)M * (double)N * 8.0 / 4.0e6;      // fp32 partial results, written and read
             if (least == 0.0 || us < least) {
                 least = us;
-                best = {t.wm, t.wn, (int)sp};
+                best = {i, (int)sp};
             }
         }
     }
     return best;
 }
 
-// One run of K to y, or several to `partial`, and what adds them up; launch(args, output, splits, elements between runs).
-template <typename OutT, typename Launch>
-arcq_status launch_runs(const Mx8Args& a, OutT* y, int splits, float* partial, Launch launch) {
-    if (splits == 1) return launch(a, y, 1, (int64_t)0);
-    Mx8Args run = a;
-    run.ldy = a.N;
-    if (arcq_status st = launch(run, partial, splits, (int64_t)a.M * a.N)) return st;
-    return launch_splitk_reduce(partial, splits, a.M, a.N, 1.0f, y, std::is_same<OutT, _Float16>::value ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy, a.stream);
+// The launch that a plan names, with an output of OutT.
+template <typename OutT>
+using Launch = arcq_status (*)(const Mx8Args& a, OutT* y, int splits, int64_t split_stride);
+
+template <typename OutT, size_t... I>
+Launch<OutT> tile_launch(int tile, std::index_sequence<I...>) {
+    constexpr int FIRST = first_tile(std::is_same<OutT, float>::value);
+    static constexpr Launch<OutT> launches[] = {launch_tiles<kTiles[FIRST + I].wm, kTiles[FIRST + I].wn, kTiles[FIRST + I].ns, OutT>...};
+    return launches[tile - FIRST];
 }
 
+template <int MT, typename OutT, size_t... I>
+Launch<OutT> stream_launch(int nt, std::index_sequence<I...>) {
+    static constexpr Launch<OutT> launches[] = {launch_stream<MT, 1 + (int)I, OutT>...};
+    return launches[nt - 1];
+}
+
+template <typename OutT>
+Launch<OutT> launch_of(const Mx8Plan& p) {
+    if (p.tile >= 0) return tile_launch<OutT>(p.tile, std::make_index_sequence<kTileCount - first_tile(std::is_same<OutT, float>::value)>{});
+    return p.mt == 1 ? stream_launch<1, OutT>(p.nt, std::make_index_sequence<kStreamTiles[0]>{})
+                     : stream_launch<2, OutT>(p.nt, std::make_index_sequence<kStreamTiles[1]>{});
+}
+
+// One run of K to y, or several to `partial`, and what adds them up.
 template <typename OutT>
 arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
     constexpr bool HALF = std::is_same<OutT, _Float16>::value;
     const Mx8Plan plan = plan_mx8(a.M, a.N, a.nb, a.nbw, !HALF, partial != nullptr);
-#define ARCQ_MX8_TILES(WM_, WN_, NS_) \
-    if (plan.wm == WM_ && plan.wn == WN_) \
-        return launch_runs(a, y, plan.splits, partial, [](const Mx8Args& args, auto* out, int splits, int64_t stride) { \
-            return launch_tiles<WM_, WN_, NS_>(args, out, splits, stride); \
-        })
-    if constexpr (HALF) {
-        if (plan.wm == 4 && plan.wn == 4 && plan.splits == 1) return launch_tiles<4, 4, 3>(a, y, 1, 0);
-    }
-    ARCQ_MX8_TILES(3, 4, 3);
-    ARCQ_MX8_TILES(2, 4, 4);
-    ARCQ_MX8_TILES(3, 2, 4);
-    ARCQ_MX8_TILES(2, 2, 3);
-    ARCQ_MX8_TILES(1, 4, 5);
-    ARCQ_MX8_TILES(1, 2, 4);
-#undef ARCQ_MX8_TILES
-#define ARCQ_MX8_STREAM(MT_, NT_) \
-    if (plan.wm == 0 && plan.mt == MT_ && plan.nt == NT_) \
-        return launch_runs(a, y, plan.splits, partial, [](const Mx8Args& args, auto* out, int splits, int64_t) { \
-            return launch_stream<MT_, NT_>(args, out, splits); \
-        })
-    ARCQ_MX8_STREAM(1, 1);
-    ARCQ_MX8_STREAM(1, 2);
-    ARCQ_MX8_STREAM(1, 3);
-    ARCQ_MX8_STREAM(1, 4);
-    ARCQ_MX8_STREAM(1, 5);
-    ARCQ_MX8_STREAM(1, 6);
-    ARCQ_MX8_STREAM(1, 7);
-    ARCQ_MX8_STREAM(2, 1);
-    ARCQ_MX8_STREAM(2, 2);
-    ARCQ_MX8_STREAM(2, 3);
-    ARCQ_MX8_STREAM(2, 4);
-#undef ARCQ_MX8_STREAM
-    return fail(ARCQ_HIP_ERROR, "no MXFP8 kernel of %d x %d fragments, %d x %d tiles", plan.wm, plan.wn, plan.mt, plan.nt);
+    if (plan.splits == 1) return launch_of<OutT>(plan)(a, y, 1, 0);
+    Mx8Args run = a;
+    run.ldy = a.N;
+    if (arcq_status st = launch_of<float>(plan)(run, partial, plan.splits, (int64_t)a.M * a.N)) return st;
+    return launch_splitk_reduce(partial, plan.splits, a.M, a.N, 1.0f, y, HALF ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy, a.stream);
 }
 
 }  // namespace
@@ -625,7 +619,7 @@ size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 
 void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool fp32, bool workspace, arcq_route* route) {
     const Mx8Plan p = plan_mx8(std::min(M, rows_of_launch(N, K)), N, K >> 5, (K + S) >> 5, fp32, workspace);
-    *route = p.wm ? arcq_route{ARCQ_ROUTE_TILES, 64 * p.wm, 64 * p.wn, p.splits, 0} : arcq_route{ARCQ_ROUTE_STREAM, 16 * p.mt, 16 * p.nt, p.splits, 0};
+    *route = p.tile >= 0 ? arcq_route{ARCQ_ROUTE_TILES, 64 * kTiles[p.tile].wm, 64 * kTiles[p.tile].wn, p.splits, 0} : arcq_route{ARCQ_ROUTE_STREAM, 16 * p.mt, 16 * p.nt, p.splits, 0};
 }
 
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
