@@ -313,8 +313,8 @@ arcq_status arcq_mx_pack_weight_ex(const void* w, int64_t N, int64_t K, int64_t 
  *   Exact products and fp32 accumulation for either y_dtype; ARCQ_DTYPE_F16 rounds the sum once more.
  *   a_*  MXFP8 activations [M, K];  w_*  weights of arcq_mx_pack_weight with this K and S in the plain layout (S = 0: plain MXFP4;
  *   not ARCQ_LAYOUT_INTERLEAVED with S > 0); all codes 16-byte aligned; N <= 2^27.  y as in arcq_gemm.
- *   workspace  256-byte aligned, at least arcq_mx8_gemm_workspace_size bytes: few-tile problems then split K into runs whose fp32 partial
- *     results a second kernel adds in index order.  NULL: never split (the same result up to the order of the fp32 additions).
+ *   workspace  256-byte aligned, at least arcq_mx8_gemm_workspace_size bytes (64 MiB do for any sizes): few-tile problems then split K into
+ *     runs whose fp32 partial results a second kernel adds in index order.  NULL: never split (the same result up to the order of the fp32 additions).
  *     Calls that share a workspace must not overlap.
  */
 arcq_status arcq_mx8_packed_sizes(int64_t rows, int64_t K, size_t* codes_bytes, size_t* scales_bytes);

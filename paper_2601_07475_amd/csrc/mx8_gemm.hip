@@ -487,20 +487,20 @@ arcq_status launch_tiles(const Mx8Args& a, OutT* y, int splits, int64_t split_st
 }
 
 // The tiles that there are, by fragment rows and columns of a wave and slots of the ring, and what a unit and the rest of a tile take (us): with few
-// workgroups, and with every compute unit busy, where two smaller ones share one and large ones meet the power limit.  [0]: fp16 output, [1]: fp32 (the
-// rest: also of several runs of K, which store fp32); either fitted to measured times.  Plans and the launches below are made from this list.
+// workgroups, and with every compute unit busy, where two smaller ones share one and large ones meet the power limit.  [0]: products with fp16 output,
+// [1]: with fp32; either fitted to measured times of products, in one and several runs of K.  Plans and the launches below are made from this list.
 struct Tile {
     int wm, wn, ns;
     double unit_few[2], unit_all[2], rest[2];
 };
 constexpr Tile kTiles[] = {
-    {4, 4, 3, {2.55, 0.00}, {2.42, 0.00}, {0.3, 0.0}},      // fp16 output only: with fp32, registers go to scratch
-    {3, 4, 3, {2.10, 1.96}, {2.00, 2.17}, {0.7, 5.0}},
-    {2, 4, 4, {1.59, 1.36}, {1.50, 1.56}, {0.4, 4.0}},
-    {3, 2, 4, {1.53, 1.30}, {1.34, 1.45}, {0.6, 3.5}},
-    {2, 2, 3, {0.82, 1.00}, {0.88, 0.81}, {1.1, 2.5}},
-    {1, 4, 5, {0.90, 0.95}, {0.80, 0.89}, {0.8, 2.0}},
-    {1, 2, 4, {0.49, 0.56}, {0.40, 0.46}, {0.8, 1.5}},
+    {4, 4, 3, {2.56, 0.00}, {2.43, 0.00}, {0.3, 0.0}},      // one run to an fp16 output only: storing fp32, registers go to scratch
+    {3, 4, 3, {1.80, 1.96}, {1.82, 2.17}, {1.8, 5.0}},
+    {2, 4, 4, {1.56, 1.36}, {1.33, 1.56}, {1.0, 4.0}},
+    {3, 2, 4, {1.57, 1.30}, {1.44, 1.45}, {0.7, 3.5}},
+    {2, 2, 3, {0.82, 1.00}, {1.05, 0.81}, {0.4, 2.5}},
+    {1, 4, 5, {0.79, 0.95}, {0.77, 0.89}, {1.2, 2.0}},
+    {1, 2, 4, {0.54, 0.56}, {0.50, 0.46}, {0.5, 1.5}},
 };
 constexpr int kTileCount = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
 constexpr int first_tile(bool fp32) { return fp32 ? 1 : 0; }
@@ -522,7 +522,8 @@ Mx8Plan stream_plan(int64_t M, int64_t N) {
 }
 
 // A function of the sizes, the output's type and whether there is a workspace: whatever a model of their times, fitted to measurements over 32 to 8192
-// rows, N = 512 .. 27648 and K = 512 .. 28672, puts first (fp16 output, 91 problems, one run of K: 1.01x the fastest tile of all on average, 1.2x at worst).
+// rows, N = 328 .. 27648 and K = 512 .. 28672, puts first (fp16 output: 1.01x the fastest tile of all on average, 1.2x at worst, of 91 problems in one
+// run of K, and 1.01x, 1.1x at worst, of 24 in any number).
 // The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'; in several
 // runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 5.5 us, 15 x 112 over 20640 14.3 -> 6.4).  With more than 128 rows it
 // has what the tiles cannot address.
@@ -550,13 +551,13 @@ Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool fp32, bool 
         const Tile& t = kTiles[i];
         const int64_t tiles = ((M + 64 * t.wm - 1) / (64 * t.wm)) * ((N + 64 * t.wn - 1) / (64 * t.wn));
         if (tiles > 0x7FFFFFFF / 8) continue;
-        // runs of at least four units; split only where tiles leave compute units idle
-        const int64_t most = workspace && tiles <= 256 && i >= first_tile(true) ? std::min<int64_t>(8, units / 4) : 1;
+        // runs of at least four units, partial results of at most 64 MiB; split only where tiles leave compute units idle
+        const int64_t most = workspace && tiles <= 256 && i >= first_tile(true) ? std::min<int64_t>({8, units / 4, (16ll << 20) / (M * N)}) : 1;
         for (int64_t sp = 1; sp == 1 || sp <= most; ++sp) {
             const int64_t work = tiles * sp;
             const double unit = work >= 256 ? t.unit_all[fp32] : t.unit_few[fp32];
-            double us = 3.0 + (double)((work + 255) / 256) * ((double)((units + sp - 1) / sp) * unit + t.rest[fp32 || sp > 1]);
-            if (sp > 1) us += 3.5 + (double)sp * (double)M * (double)N * 8.0 / 4.0e6;      // fp32 partial results, written and read
+            double us = 3.0 + (double)((work + 255) / 256) * ((double)((units + sp - 1) / sp) * unit + t.rest[fp32]);
+            if (sp > 1) us += (fp32 ? 3.5 : 2.8) + (double)sp * (double)M * (double)N * 8.0 / 4.0e6;      // fp32 partial results, written and read
             if (least == 0.0 || us < least) {
                 least = us;
                 best = {i, (int)sp};

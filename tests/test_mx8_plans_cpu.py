@@ -44,5 +44,7 @@ def test_every_plan_has_a_kernel(dtype, workspace):
         assert status == B.HIP_ERROR and "device" in message, (M, N, K, S, route, message)
         seen.add(route[:3])
         assert workspace or route[3] == 1
+        assert route[3] * M * N * 4 <= 64 << 20 or route[3] == 1            # what the header promises of a workspace
+        assert B.arcq_mx8_gemm_workspace_size(M, N, K) <= 64 << 20
     tiles = {(B.ROUTE_TILES, 64 * m, 64 * n) for m, n in ((1, 2), (1, 4), (2, 2), (3, 2), (2, 4), (3, 4))}
     assert tiles <= seen and any(r[0] == B.ROUTE_STREAM for r in seen)
