@@ -14,9 +14,9 @@
 //   4-bit operand  k = 32 q .. 32 q + 31                                   16 bytes: one block
 //   8-bit operand  k = 16 q .. 16 q + 15 and half of the step's k further  32 bytes: half of one block, half of another
 //   scale          of block q of the step, for either operand
-// Measured: 8192 x 8192 over K = 28672 2.41 ms (1.6 PFLOP/s of whole products, 3.2 on the matrix unit; from registers alone, with random codes and
-// every compute unit busy, the instruction reaches 3.8 at 1.82 GHz: power), fp32 output 2.68 ms; 777 x 6147 over 4352 48 us, fp32 54 (two passes take 22 on
-// the matrix unit); 300 x 4096 over 14336 44 us; streaming: 16 x 14336 over 4096 9.4 us (3.3 TB/s of weights), 1 x 4096 over 4096 4.5, either type.
+// Measured: 8192 x 8192 over K = 28672 2.4 ms (1.6 PFLOP/s of whole products, 3.2 on the matrix unit; from registers alone, with random codes and
+// every compute unit busy, the instruction reaches 3.8 at 1.82 GHz: power), fp32 output 2.67 ms; 777 x 6147 over 4352 48 us, fp32 53 (two passes take 22 on
+// the matrix unit); 300 x 4096 over 14336 43 us; streaming: 16 x 14336 over 4096 9.4 us (3.3 TB/s of weights), 1 x 4096 over 4096 4.5, either type.
 #include "code_rows.h"
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
@@ -525,7 +525,7 @@ Mx8Plan stream_plan(int64_t M, int64_t N) {
 // rows, N = 328 .. 27648 and K = 512 .. 28672, puts first (fp16 output: 1.01x the fastest tile of all on average, 1.2x at worst, of 91 problems in one
 // run of K, and 1.01x, 1.1x at worst, of 24 in any number).
 // The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'; in several
-// runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 5.5 us, 15 x 112 over 20640 14.3 -> 6.4).  With more than 128 rows it
+// runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 5.9 us, 15 x 112 over 20640 14.3 -> 6.7).  With more than 128 rows it
 // has what the tiles cannot address.
 Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool fp32, bool workspace) {
     const bool offsets_fit = (uint64_t)M * nb * 32 < 0xFFFF0000ull && (uint64_t)N * nbw * 16 < 0xFFFF0000ull;

@@ -14,11 +14,12 @@
 // Measured (us, and TB/s of what is read and written, the order apart):    quantize        norm          addition and norm
 //        1 x 14336, reordered                                              3.6           4.9               5.4      (2.4 the launch of one row)
 //      333 x 5120                                                          2.7  1.9      4.8  1.1          4.8  2.5  (norm alone: reordered)
-//     2048 x 8192, reordered                                              10.3  4.9     14.2  3.6         21.3  5.5
-//     8192 x 8192, reordered                                              32.2  6.3     40.0  5.1         89.3  5.3
-//     8192 x 28672, reordered                                            124    5.8    174    4.1        357    4.6
-// Single rows are bound by one compute unit's way to memory and the launch, the others by memory; the norm's barriers and the reads of LDS in the
-// order of the weights take up to a quarter more, for rows of which only one or two workgroups fit a compute unit.
+//     2048 x 8192, reordered                                              10.4  4.9     14.3  3.6         21.4  5.5
+//     8192 x 8192, reordered                                              32.2  6.3     41.6  4.9         89    5.3
+//     8192 x 28672, reordered                                            136    5.2    178    4.0        356    4.6
+// (The last line with inputs that change from pass to pass, 125 to 129 us for the quantizer where they are the same; the others with the same, of
+// which the caches have a part.)  Single rows are bound by one compute unit's way to memory and the launch, the others by memory.  From 333 rows on the
+// norm takes 29 to 39 % more than the quantizer alone (barriers), the reads of LDS in the order of the weights 4 to 30 % more than none.
 #include "internal.h"
 #include "lds_dma.h"
 #include "row_stats.h"
