@@ -500,7 +500,7 @@ constexpr Tile kTiles[] = {
     {3, 2, 4, {1.57, 1.30}, {1.44, 1.45}, {0.7, 3.5}},
     {2, 2, 3, {0.82, 1.00}, {1.05, 0.81}, {0.4, 2.5}},
     {1, 4, 5, {0.79, 0.95}, {0.77, 0.89}, {1.2, 2.0}},
-    {1, 2, 4, {0.54, 0.56}, {0.50, 0.46}, {0.5, 1.5}},
+    {1, 2, 4, {0.54, 0.56}, {0.50, 0.46}, {0.7, 1.5}},
 };
 constexpr int kTileCount = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
 constexpr int first_tile(bool fp32) { return fp32 ? 1 : 0; }
@@ -522,8 +522,8 @@ Mx8Plan stream_plan(int64_t M, int64_t N) {
 }
 
 // A function of the sizes, the output's type and whether there is a workspace: whatever a model of their times, fitted to measurements over 32 to 8192
-// rows, N = 328 .. 27648 and K = 512 .. 28672, puts first (fp16 output: 1.01x the fastest tile of all on average, 1.2x at worst, of 91 problems in one
-// run of K, and 1.01x, 1.1x at worst, of 24 in any number).
+// rows, N = 328 .. 27648 and K = 512 .. 28672, puts first (fp16 output: 1.02x the fastest tile of all on average, 1.3x at worst, over K = 544, of 85
+// problems in one run of K, and 1.01x, 1.1x at worst, of 26 in any number; 1 x 512 over 128 streamed 2.5 us, on a tile 3.3).
 // The streaming kernel's: 23 ns per load instruction of 16 rows x 64 bytes that a wave issues, of 512 k 4 nt + 8 mt and the scale bytes'; in several
 // runs of K where its tiles leave compute units idle (1 x 481 over K = 16032 13.2 -> 5.9 us, 15 x 112 over 20640 14.3 -> 6.7).  With more than 128 rows it
 // has what the tiles cannot address.

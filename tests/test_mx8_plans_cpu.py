@@ -48,3 +48,10 @@ def test_every_plan_has_a_kernel(dtype, workspace):
         assert B.arcq_mx8_gemm_workspace_size(M, N, K) <= 64 << 20
     tiles = {(B.ROUTE_TILES, 64 * m, 64 * n) for m, n in ((1, 2), (1, 4), (2, 2), (3, 2), (2, 4), (3, 4))}
     assert tiles <= seen and any(r[0] == B.ROUTE_STREAM for r in seen)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_smallest_products_stream(dtype):
+    """A launch is all that they take: the kernel with the least to set up."""
+    for M, N, K in ((1, 8, 32), (1, 512, 128), (1, 4096, 64), (16, 64, 64), (32, 512, 128), (64, 64, 64), (128, 512, 128)):
+        assert B.arcq_mx8_gemm_route(M, N, K, 0, dtype, True)[0] == B.ROUTE_STREAM
