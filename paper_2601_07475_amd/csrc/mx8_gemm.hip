@@ -619,6 +619,7 @@ size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 }
 
 void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool fp32, bool workspace, arcq_route* route) {
+    M = std::max<int64_t>(M, 1), N = std::max<int64_t>(N, 1);       // (nothing is launched without rows or features; plans are of some)
     const Mx8Plan p = plan_mx8(std::min(M, rows_of_launch(N, K)), N, K >> 5, (K + S) >> 5, fp32, workspace);
     *route = p.tile >= 0 ? arcq_route{ARCQ_ROUTE_TILES, 64 * kTiles[p.tile].wm, 64 * kTiles[p.tile].wn, p.splits, 0} : arcq_route{ARCQ_ROUTE_STREAM, 16 * p.mt, 16 * p.nt, p.splits, 0};
 }

@@ -55,3 +55,11 @@ def test_smallest_products_stream(dtype):
     """A launch is all that they take: the kernel with the least to set up."""
     for M, N, K in ((1, 8, 32), (1, 512, 128), (1, 4096, 64), (16, 64, 64), (32, 512, 128), (64, 64, 64), (128, 512, 128)):
         assert B.arcq_mx8_gemm_route(M, N, K, 0, dtype, True)[0] == B.ROUTE_STREAM
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("workspace", [False, True])
+def test_route_of_nothing(dtype, workspace):
+    """No rows, no features: the answer for one, as of the other products' routes; once a division by zero."""
+    for M, N in ((0, 8), (4, 0), (0, 0)):
+        assert B.arcq_mx8_gemm_route(M, N, 64, 0, dtype, workspace) == (B.ROUTE_STREAM, 16, 16, 1)
