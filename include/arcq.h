@@ -52,6 +52,13 @@ typedef int arcq_status;
 #define ARCQ_DTYPE_F16 0
 #define ARCQ_DTYPE_F32 1
 
+/* activations of the calls that apply one (v: the sum before it) */
+#define ARCQ_ACT_NONE      0
+#define ARCQ_ACT_RELU      1         /* max(v, 0) */
+#define ARCQ_ACT_GELU      2         /* v (1 + erf(v / sqrt(2))) / 2 */
+#define ARCQ_ACT_GELU_TANH 3         /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+#define ARCQ_ACT_SILU      4         /* v / (1 + exp(-v)) */
+
 /* flags of the *_ex entry points (0 = the behaviour of the plain entry points) */
 #define ARCQ_LAYOUT_INTERLEAVED 1u   /* Appendix D "Interleaved Channel Layout" */
 #define ARCQ_SCALE_ROUND_UP     2u   /* block scale never below max/q_max: alpha >= 1 of Section 3.4 */
@@ -355,6 +362,79 @@ arcq_status arcq_mx_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const
                          const uint8_t* w_codes, const uint8_t* w_scales,
                          int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy,
                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The products above with what a layer does next in the same kernel:
+ *   y[m, n] = act(s[m, n] + bias[n]) + residual[m, n],   s: the sums of arcq_mx8_gemm, arcq_gemv, arcq_mx_gemv;   in fp32, rounded once to y's type.
+ * bias      fp16 [N], 2-byte aligned, or NULL: none
+ * activation  an ARCQ_ACT_
+ * residual  [M, N] of y's type, pitch ldr elements (ldr >= N), 4-byte aligned, or NULL: none (ldr is ignored).  It may be y (with y's pitch: the
+ *           addition in place); any other overlap with y is not allowed.
+ * Everything else, workspace sizes included, as in the plain calls; with no bias, no residual and ARCQ_ACT_NONE they are the plain calls.
+ */
+arcq_status arcq_mx8_gemm_epilogue(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                                   int64_t M, int64_t N, int64_t K, int64_t S, const void* bias, int activation, const void* residual, int64_t ldr,
+                                   void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+arcq_status arcq_gemv_epilogue(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                               const uint8_t* w_codes, const uint8_t* w_scales, float w_tensor_scale,
+                               int64_t N, int64_t S, const void* bias, int activation, const void* residual, int64_t ldr,
+                               void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+arcq_status arcq_mx_gemv_epilogue(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                                  const uint8_t* w_codes, const uint8_t* w_scales,
+                                  int64_t N, int64_t S, const void* bias, int activation, const void* residual, int64_t ldr,
+                                  void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The router of a mixture of experts, for tokens whose experts arcq_moe / arcq_mx_moe then compute.
+ *   l[m, e] = sum_k x[m, k] router[e, k];   s[m, .] = softmax over the experts, or 1 / (1 + exp(-l)) each with ARCQ_MOE_SIGMOID
+ *   ids[m, 0 .. top_k - 1]: the experts with the largest s[m, e] + bias[e], largest first, equal ones by ascending index;
+ *   weights[m, j] = s[m, ids[m, j]], without the bias; with ARCQ_MOE_RENORMALIZE divided by the sum of the top_k.
+ * Experts are ranked by values in 64 bits (of exact products; without a bias by l, which orders them as s does).
+ * x       fp16 [M, K], pitch ldx, K % 8 == 0, 16-byte aligned, ldx % 8 == 0;  router  fp16 [E, K], pitch ldr, the same
+ * bias    fp32 [E], 4-byte aligned, or NULL: none
+ * 1 <= top_k <= E <= ARCQ_MOE_MAX_EXPERTS, top_k <= ARCQ_MOE_MAX_TOP_K
+ * ids     out, int32 [M, top_k];  weights  out, fp32 [M, top_k], both dense and 4-byte aligned
+ * workspace  256-byte aligned, at least arcq_moe_route_workspace_size bytes (may be NULL when that is 0).  Calls that share one must not overlap.
+ * Where scores are not finite, ids hold experts once each, or -1 (no expert) with a weight of 0 or NaN.
+ */
+#define ARCQ_MOE_SIGMOID     1u
+#define ARCQ_MOE_RENORMALIZE 2u
+#define ARCQ_MOE_MAX_EXPERTS 1024
+#define ARCQ_MOE_MAX_TOP_K   16
+arcq_status arcq_moe_route_workspace_size(int64_t M, int64_t K, int64_t E, size_t* bytes);
+arcq_status arcq_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, const void* router, int64_t ldr, int64_t E, const float* bias,
+                           int64_t top_k, uint32_t flags, int32_t* ids, float* weights,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The experts of a mixture for a few tokens (the decode step of such a layer), on packed NVFP4 (arcq_moe) or MXFP4 (arcq_mx_moe) weights:
+ *   y[m, n] = sum_j weights[m, j] sum_{i<I} act(g[i]) u[i] D_e[n, i] + residual[m, n],   e = ids[m, j],   g = G_e x[m],  u = U_e x[m]
+ * with fp32 accumulation; x is not rounded, weights[m, j] act(g) u is held to 22 bits (2^-32 at least) and must stay below 2^20.
+ * x        fp16 [M, K], pitch ldx, and perm as in arcq_gemv.  Any M; made for up to 64 tokens (more take the weights once for every 64).
+ * ids      int32 [M, top_k], dense: outside 0 .. E - 1 (say -1) there is no expert, and the weight there is not read.  A token without any gets its
+ *          residual, or zeros.  An expert twice in a token counts with both weights.
+ * weights  fp32 [M, top_k], dense
+ * up_*     packed weights [E, 2 I, K + S_up]: an expert's I rows of G, then its I rows of U;  up_tensor_scales: fp32 [E], on the device
+ * down_*   packed weights [E, N, I + S_down], packed without an order of their own (one that outliers need is that of the rows of G and U);
+ *          down_tensor_scales: fp32 [E].  All packed in the plain layout (not ARCQ_LAYOUT_INTERLEAVED with S > 0); the S columns that repeat the outliers'
+ *          weights are passed over.  Codes 8-byte aligned.  K, S_up and I, S_down as in the packer.
+ * activation  an ARCQ_ACT_;  residual, y  as in the calls with an epilogue: residual may be NULL or y
+ * 1 <= top_k <= ARCQ_MOE_MAX_TOP_K, 1 <= E <= ARCQ_MOE_MAX_EXPERTS
+ * workspace  256-byte aligned, at least arcq_moe_workspace_size bytes (for either format).  Calls that share one must not overlap.
+ */
+arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t K, int64_t I, int with_perm, size_t* bytes);
+arcq_status arcq_moe(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                     const int32_t* ids, const float* weights, int64_t top_k, int64_t E,
+                     const uint8_t* up_codes, const uint8_t* up_scales, const float* up_tensor_scales, int64_t I, int64_t S_up,
+                     const uint8_t* down_codes, const uint8_t* down_scales, const float* down_tensor_scales, int64_t N, int64_t S_down,
+                     int activation, const void* residual, int64_t ldr, void* y, int y_dtype, int64_t ldy,
+                     void* workspace, size_t workspace_bytes, void* stream);
+arcq_status arcq_mx_moe(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
+                        const int32_t* ids, const float* weights, int64_t top_k, int64_t E,
+                        const uint8_t* up_codes, const uint8_t* up_scales, int64_t I, int64_t S_up,
+                        const uint8_t* down_codes, const uint8_t* down_scales, int64_t N, int64_t S_down,
+                        int activation, const void* residual, int64_t ldr, void* y, int y_dtype, int64_t ldy,
+                        void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

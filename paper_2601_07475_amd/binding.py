@@ -15,6 +15,9 @@ LIB_PATH = os.environ.get("ARCQ_LIBRARY") or os.path.join(_HERE, "libarcq.so")  
 OK, INVALID_ARG, BAD_SHAPE, BAD_ALIGN, HIP_ERROR, WORKSPACE_TOO_SMALL = range(6)
 DTYPE_F16, DTYPE_F32 = 0, 1
 LAYOUT_INTERLEAVED, SCALE_ROUND_UP, RMSNORM_EXACT_SUM = 1, 2, 4
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
+MOE_SIGMOID, MOE_RENORMALIZE = 1, 2
+MOE_MAX_EXPERTS, MOE_MAX_TOP_K = 1024, 16
 MAX_K = 65536
 ROUTE_STREAM, ROUTE_KSPLIT, ROUTE_TILES, ROUTE_DIRECT = range(4)
 
@@ -76,6 +79,16 @@ SIGNATURES = {
     "arcq_gemv": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _f32, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
     "arcq_mx_gemv_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, ctypes.c_int, ctypes.POINTER(_sz)]),
     "arcq_mx_gemv": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "arcq_mx8_gemm_epilogue": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _vp, ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "arcq_gemv_epilogue": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _f32, _i64, _i64, _vp, ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "arcq_mx_gemv_epilogue": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "arcq_moe_route_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, ctypes.POINTER(_sz)]),
+    "arcq_moe_route": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _u32, _vp, _vp, _vp, _sz, _vp]),
+    "arcq_moe_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.POINTER(_sz)]),
+    "arcq_moe": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64,
+                                ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
+    "arcq_mx_moe": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64,
+                                   ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
     "arcq_check_perm": (ctypes.c_int, [_vp, _i64, _vp, ctypes.POINTER(ctypes.c_int), _vp]),
 }
 
@@ -532,6 +545,164 @@ def arcq_mx_gemv(x, perm, w_codes, w_scales, out_dtype=torch.float16, y=None, wo
     return y
 
 
+def _epilogue(bias, activation, residual, M, N, y, device):
+    """(bias, activation, residual, its pitch) of a call that finishes its product, checked."""
+    if bias is not None:
+        assert bias.get_device() == device and bias.dtype is _HALF and bias.is_contiguous()
+        if bias.numel() != N:
+            raise ArcqError(BAD_SHAPE, "bias must have N entries")
+        bias = bias.data_ptr()
+    if residual is None:
+        return bias, activation, None, 0
+    assert residual.get_device() == device and residual.dtype is y.dtype
+    if tuple(residual.shape) != (M, N):
+        raise ArcqError(BAD_SHAPE, "residual must be [M, N]")
+    pitch, step = residual.stride()
+    assert step == 1 or N <= 1
+    return bias, activation, residual.data_ptr(), pitch if M > 1 else max(N, pitch)
+
+
+def _mx8_gemm_epilogue_args(a_codes, a_scales, w_codes, w_scales, bias, activation, residual, out_dtype, y, workspace):
+    if y is None and residual is not None:
+        out_dtype = residual.dtype
+    args, y = _mx8_gemm_args(a_codes, a_scales, w_codes, w_scales, out_dtype, y, workspace)
+    return (*args[:8], *_epilogue(bias, activation, residual, args[4], args[5], y, y.get_device()), *args[8:]), y
+
+
+def arcq_mx8_gemm_epilogue(a_codes, a_scales, w_codes, w_scales, bias=None, activation=ACT_NONE, residual=None, out_dtype=torch.float16, y=None, workspace=None):
+    """y = act(product + bias) + residual, the product that of arcq_mx8_gemm; returns y.  bias: fp16 [N]; residual: [M, N] of y's type (a new y has
+    the residual's), may be y."""
+    args, y = _mx8_gemm_epilogue_args(a_codes, a_scales, w_codes, w_scales, bias, activation, residual, out_dtype, y, workspace)
+    _check(lib().arcq_mx8_gemm_epilogue(*args))
+    return y
+
+
+def _gemv_epilogue(size, block, x, perm, w_codes, w_scales, bias, activation, residual, out_dtype, y, workspace):
+    if y is None and residual is not None:
+        out_dtype = residual.dtype
+    head, tail, y = _gemv(size, block, x, perm, w_codes, w_scales, out_dtype, y, workspace)
+    return head, (*tail[:2], *_epilogue(bias, activation, residual, head[1], tail[0], y, y.get_device()), *tail[2:]), y
+
+
+def arcq_gemv_epilogue(x, perm, w_codes, w_scales, w_tensor_scale, bias=None, activation=ACT_NONE, residual=None, out_dtype=torch.float16, y=None,
+                       workspace=None):
+    """y = act(product + bias) + residual, the product that of arcq_gemv; returns y.  bias, residual as in arcq_mx8_gemm_epilogue."""
+    head, tail, y = _gemv_epilogue(arcq_gemv_workspace_size, 16, x, perm, w_codes, w_scales, bias, activation, residual, out_dtype, y, workspace)
+    _check(lib().arcq_gemv_epilogue(*head, w_tensor_scale, *tail))
+    return y
+
+
+def arcq_mx_gemv_epilogue(x, perm, w_codes, w_scales, bias=None, activation=ACT_NONE, residual=None, out_dtype=torch.float16, y=None, workspace=None):
+    """The same with MXFP4 weights, which have no tensor scale."""
+    head, tail, y = _gemv_epilogue(arcq_mx_gemv_workspace_size, 32, x, perm, w_codes, w_scales, bias, activation, residual, out_dtype, y, workspace)
+    _check(lib().arcq_mx_gemv_epilogue(*head, *tail))
+    return y
+
+
+def arcq_moe_route_workspace_size(M, K, E):
+    b = _sz(0)
+    _check(lib().arcq_moe_route_workspace_size(M, K, E, ctypes.byref(b)))
+    return b.value
+
+
+def _route_args(x, router, top_k, bias, flags, ids, weights, workspace, make):
+    device = _device()
+    M, K, ldx = _fp16_rows(x, device)
+    E, cols, ldr = _fp16_rows(router, device)
+    if cols != K:
+        raise ArcqError(BAD_SHAPE, "router must be [E, K]")
+    if bias is not None:
+        assert bias.get_device() == device and bias.dtype is _FLOAT and bias.is_contiguous()
+        if bias.numel() != E:
+            raise ArcqError(BAD_SHAPE, "bias must have E entries")
+        bias = bias.data_ptr()
+    if ids is None:
+        ids = x.new_empty((M, max(top_k, 0)), dtype=_INT)
+    if weights is None:
+        weights = x.new_empty((M, max(top_k, 0)), dtype=_FLOAT)
+    assert ids.get_device() == device and ids.dtype is _INT and ids.is_contiguous() and ids.numel() == M * max(top_k, 0)
+    assert weights.get_device() == device and weights.dtype is _FLOAT and weights.is_contiguous() and weights.numel() == M * max(top_k, 0)
+    if workspace is None and make:
+        need = arcq_moe_route_workspace_size(M, K, E)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    return (x.data_ptr(), M, K, ldx, router.data_ptr(), ldr, E, bias, top_k, flags, ids.data_ptr(), weights.data_ptr(), *_scratch(workspace, device),
+            _stream()), ids, weights
+
+
+def arcq_moe_route(x, router, top_k, bias=None, flags=0, ids=None, weights=None, workspace=None):
+    """The top_k experts of every row of x [M, K] fp16 by the scores x router^T, router [E, K] fp16 -> (ids int32 [M, top_k], weights fp32 [M, top_k]).
+    bias: fp32 [E], for the choice only; flags: MOE_SIGMOID, MOE_RENORMALIZE."""
+    args, ids, weights = _route_args(x, router, top_k, bias, flags, ids, weights, workspace, True)
+    _check(lib().arcq_moe_route(*args))
+    return ids, weights
+
+
+def arcq_moe_workspace_size(M, top_k, K, I, with_perm):
+    b = _sz(0)
+    _check(lib().arcq_moe_workspace_size(M, top_k, K, I, int(with_perm), ctypes.byref(b)))
+    return b.value
+
+
+def _experts(codes, scales, K, block, device):
+    """(E, rows, S) of packed weights [E, rows, K + S], checked."""
+    assert codes.get_device() == device and codes.dtype is _BYTE and codes.is_contiguous()
+    assert scales.get_device() == device and scales.dtype is _BYTE and scales.is_contiguous()
+    E, rows, half = codes.shape
+    if 2 * half < K or scales.numel() != E * rows * (2 * half // block):
+        raise ArcqError(BAD_SHAPE, "operand shapes disagree on K and S")
+    return E, rows, 2 * half - K
+
+
+def _moe_args(block, x, perm, ids, weights, up_codes, up_scales, up_ts, down_codes, down_scales, down_ts, activation, residual, out_dtype, y, workspace, make):
+    device = _device()
+    M, K, ldx = _fp16_rows(x, device)
+    E, twice, S_up = _experts(up_codes, up_scales, K, block, device)
+    I = twice // 2
+    same, N, S_down = _experts(down_codes, down_scales, I, block, device)
+    rows, top_k = ids.shape
+    if twice % 2 or same != E or rows != M or tuple(weights.shape) != (M, top_k):
+        raise ArcqError(BAD_SHAPE, "operand shapes disagree on M, E, I or top_k")
+    assert ids.get_device() == device and ids.dtype is _INT and ids.is_contiguous()
+    assert weights.get_device() == device and weights.dtype is _FLOAT and weights.is_contiguous()
+    up_scale = down_scale = ()
+    if block == 16:
+        for ts in (up_ts, down_ts):
+            assert ts.get_device() == device and ts.dtype is _FLOAT and ts.is_contiguous()
+            if ts.numel() != E:
+                raise ArcqError(BAD_SHAPE, "tensor scales must have E entries")
+        up_scale, down_scale = (up_ts.data_ptr(),), (down_ts.data_ptr(),)
+    if y is None and residual is not None:
+        out_dtype = residual.dtype
+    y, dt, ldy = _output(x, M, N, out_dtype, y, device)
+    if workspace is None and make:
+        need = arcq_moe_workspace_size(M, top_k, K, I, perm is not None)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    _, activation, residual, ldr = _epilogue(None, activation, residual, M, N, y, device)
+    return (x.data_ptr(), M, K, ldx, _perm(perm, K, device), ids.data_ptr(), weights.data_ptr(), top_k, E,
+            up_codes.data_ptr(), up_scales.data_ptr(), *up_scale, I, S_up, down_codes.data_ptr(), down_scales.data_ptr(), *down_scale, N, S_down,
+            activation, residual, ldr, y.data_ptr(), dt, ldy, *_scratch(workspace, device), _stream()), y
+
+
+def arcq_moe(x, perm, ids, weights, up_codes, up_scales, up_tensor_scales, down_codes, down_scales, down_tensor_scales, activation=ACT_SILU, residual=None,
+             out_dtype=torch.float16, y=None, workspace=None):
+    """The experts ids [M, top_k] int32 (outside 0 .. E - 1: none) of a few rows x [M, K] fp16, channels in the order perm (None: their own), added up with
+    weights [M, top_k] fp32: y = sum of weights (act(x G^T) (x U^T)) D^T + residual; returns y.
+    up: NVFP4 weights packed [E, 2 I, K + S], rows of G, then of U; down: [E, N, I + S]; tensor scales fp32 [E].  residual [M, N] of y's type, may be y.
+    workspace: a uint8 tensor of at least arcq_moe_workspace_size bytes (one is made where none is given)."""
+    args, y = _moe_args(16, x, perm, ids, weights, up_codes, up_scales, up_tensor_scales, down_codes, down_scales, down_tensor_scales, activation, residual,
+                        out_dtype, y, workspace, True)
+    _check(lib().arcq_moe(*args))
+    return y
+
+
+def arcq_mx_moe(x, perm, ids, weights, up_codes, up_scales, down_codes, down_scales, activation=ACT_SILU, residual=None, out_dtype=torch.float16, y=None,
+                workspace=None):
+    """The same with MXFP4 weights, which have no tensor scales."""
+    args, y = _moe_args(32, x, perm, ids, weights, up_codes, up_scales, None, down_codes, down_scales, None, activation, residual, out_dtype, y, workspace, True)
+    _check(lib().arcq_mx_moe(*args))
+    return y
+
+
 def _prepared(fn, args):
     """fn(*args) as a zero-argument callable.  The arguments are converted to their C types here, once: converting them on every
     call took 1.4 of its 3.1 us."""
@@ -604,6 +775,43 @@ def prepare_mx_gemv(x, perm, w_codes, w_scales, y, workspace=None):
     """Same for arcq_mx_gemv."""
     head, tail, _ = _gemv(None, 32, x, perm, w_codes, w_scales, y.dtype, y, workspace)
     return _prepared(lib().arcq_mx_gemv, (*head, *tail))
+
+
+def prepare_mx8_gemm_epilogue(a_codes, a_scales, w_codes, w_scales, y, bias=None, activation=ACT_NONE, residual=None, workspace=None):
+    """Same for arcq_mx8_gemm_epilogue."""
+    return _prepared(lib().arcq_mx8_gemm_epilogue,
+                     _mx8_gemm_epilogue_args(a_codes, a_scales, w_codes, w_scales, bias, activation, residual, y.dtype, y, workspace)[0])
+
+
+def prepare_gemv_epilogue(x, perm, w_codes, w_scales, w_tensor_scale, y, bias=None, activation=ACT_NONE, residual=None, workspace=None):
+    """Same for arcq_gemv_epilogue; where it needs a workspace, the caller's."""
+    head, tail, _ = _gemv_epilogue(None, 16, x, perm, w_codes, w_scales, bias, activation, residual, y.dtype, y, workspace)
+    return _prepared(lib().arcq_gemv_epilogue, (*head, w_tensor_scale, *tail))
+
+
+def prepare_mx_gemv_epilogue(x, perm, w_codes, w_scales, y, bias=None, activation=ACT_NONE, residual=None, workspace=None):
+    """Same for arcq_mx_gemv_epilogue."""
+    head, tail, _ = _gemv_epilogue(None, 32, x, perm, w_codes, w_scales, bias, activation, residual, y.dtype, y, workspace)
+    return _prepared(lib().arcq_mx_gemv_epilogue, (*head, *tail))
+
+
+def prepare_moe_route(x, router, top_k, ids, weights, bias=None, flags=0, workspace=None):
+    """Same for arcq_moe_route; where it needs a workspace, the caller's."""
+    assert ids is not None and weights is not None
+    return _prepared(lib().arcq_moe_route, _route_args(x, router, top_k, bias, flags, ids, weights, workspace, False)[0])
+
+
+def prepare_moe(x, perm, ids, weights, up_codes, up_scales, up_tensor_scales, down_codes, down_scales, down_tensor_scales, y, workspace, activation=ACT_SILU,
+                residual=None):
+    """Same for arcq_moe."""
+    return _prepared(lib().arcq_moe, _moe_args(16, x, perm, ids, weights, up_codes, up_scales, up_tensor_scales, down_codes, down_scales, down_tensor_scales,
+                                               activation, residual, y.dtype, y, workspace, False)[0])
+
+
+def prepare_mx_moe(x, perm, ids, weights, up_codes, up_scales, down_codes, down_scales, y, workspace, activation=ACT_SILU, residual=None):
+    """Same for arcq_mx_moe."""
+    return _prepared(lib().arcq_mx_moe, _moe_args(32, x, perm, ids, weights, up_codes, up_scales, None, down_codes, down_scales, None, activation, residual,
+                                                  y.dtype, y, workspace, False)[0])
 
 
 def prepare_mx_quantize_act(x, perm, S, codes, scales):

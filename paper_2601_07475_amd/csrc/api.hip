@@ -564,14 +564,27 @@ arcq_status arcq_mx8_gemm_workspace_size(int64_t M, int64_t N, int64_t K, size_t
     return ARCQ_OK;
 }
 
-arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales,
-                          int64_t M, int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy,
-                          void* workspace, size_t workspace_bytes, void* stream) {
-    const char* who = "arcq_mx8_gemm";
+// What follows a product: an activation that there is, operands of N features, a residual that lies on y or (unchecked) apart from it.
+static arcq_status check_epilogue(const char* who, const EpilogueArgs& e, int64_t M, int64_t N, const void* y, int64_t ldy) {
+    if (e.activation < ARCQ_ACT_NONE || e.activation > ARCQ_ACT_SILU) return fail(ARCQ_INVALID_ARG, "%s: activation = %d", who, e.activation);
+    if (M == 0 || N == 0) return ARCQ_OK;
+    if (!aligned(e.bias, 2)) return fail(ARCQ_BAD_ALIGN, "%s: bias must be 2-byte aligned", who);
+    if (!e.residual) return ARCQ_OK;
+    if (e.ldr < N) return fail(ARCQ_BAD_SHAPE, "%s: leading dimension of residual %lld < N = %lld", who, (long long)e.ldr, (long long)N);
+    if (!aligned(e.residual, 4)) return fail(ARCQ_BAD_ALIGN, "%s: residual must be 4-byte aligned", who);
+    // in place is one row over the same row, not part of another
+    if (M > 1 && e.residual == y && e.ldr != ldy) return fail(ARCQ_BAD_SHAPE, "%s: y in place of the residual needs its leading dimension", who);
+    return ARCQ_OK;
+}
+
+static arcq_status mx8_gemm_entry(const char* who, const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                                  int64_t M, int64_t N, int64_t K, int64_t S, const EpilogueArgs& epilogue, void* y, int y_dtype, int64_t ldy,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
     clear_error();
     if (arcq_status st = check_mx8_gemm_shape(M, N, K, S)) return st;
     if (y_dtype != ARCQ_DTYPE_F16 && y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", y_dtype);
     if (ldy < N) return fail(ARCQ_BAD_SHAPE, "ldy = %lld < N = %lld", (long long)ldy, (long long)N);
+    if (arcq_status st = check_epilogue(who, epilogue, M, N, y, ldy)) return st;
     if (M == 0 || N == 0) return ARCQ_OK;
     if (!a_codes || !a_scales || !w_codes || !w_scales || !y) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
     if (!aligned(a_codes, 16) || !aligned(w_codes, 16)) return fail(ARCQ_BAD_ALIGN, "%s: codes must be 16-byte aligned", who);
@@ -582,7 +595,20 @@ arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const
             return fail(ARCQ_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace_bytes);
         if (!aligned(workspace, 256)) return fail(ARCQ_BAD_ALIGN, "%s: workspace must be 256-byte aligned", who);
     }
-    return launch_mx8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, S, y, y_dtype, ldy, workspace, static_cast<hipStream_t>(stream));
+    return launch_mx8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, S, y, y_dtype, ldy, workspace, epilogue, static_cast<hipStream_t>(stream));
+}
+
+arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                          int64_t M, int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    return mx8_gemm_entry("arcq_mx8_gemm", a_codes, a_scales, w_codes, w_scales, M, N, K, S, {}, y, y_dtype, ldy, workspace, workspace_bytes, stream);
+}
+
+arcq_status arcq_mx8_gemm_epilogue(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                                   int64_t M, int64_t N, int64_t K, int64_t S, const void* bias, int activation, const void* residual, int64_t ldr,
+                                   void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    return mx8_gemm_entry("arcq_mx8_gemm_epilogue", a_codes, a_scales, w_codes, w_scales, M, N, K, S, {bias, residual, ldr, activation}, y, y_dtype, ldy,
+                          workspace, workspace_bytes, stream);
 }
 
 arcq_status arcq_mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, int y_dtype, int with_workspace, arcq_route* route) {
@@ -603,13 +629,14 @@ static arcq_status check_gemv_shape(int block, int64_t M, int64_t N, int64_t K, 
 
 static arcq_status gemv_entry(const char* who, int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
                               const uint8_t* w_codes, const uint8_t* w_scales, float w_tensor_scale, int64_t N, int64_t S,
-                              void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+                              const EpilogueArgs& epilogue, void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
     clear_error();
     if (arcq_status st = check_gemv_shape(block, M, N, K, S)) return st;
     if (y_dtype != ARCQ_DTYPE_F16 && y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", y_dtype);
     if (arcq_status st = check_pitch(who, "x", ldx, K)) return st;
     if (ldy < N) return fail(ARCQ_BAD_SHAPE, "ldy = %lld < N = %lld", (long long)ldy, (long long)N);
     if (arcq_status st = check_scale(w_tensor_scale, "w_tensor_scale")) return st;
+    if (arcq_status st = check_epilogue(who, epilogue, M, N, y, ldy)) return st;
     if (M == 0 || N == 0) return ARCQ_OK;
     if (arcq_status st = check_rows(who, "x", x, ldx)) return st;
     if (!w_codes || !w_scales || !y) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
@@ -623,7 +650,7 @@ static arcq_status gemv_entry(const char* who, int block, const void* x, int64_t
         if (!aligned(workspace, 256)) return fail(ARCQ_BAD_ALIGN, "%s: workspace must be 256-byte aligned", who);
     }
     return launch_gemv(block, x, M, K, ldx, perm, w_codes, w_scales, N, S, w_tensor_scale, y, y_dtype, ldy, workspace,
-                       static_cast<hipStream_t>(stream));
+                       epilogue, static_cast<hipStream_t>(stream));
 }
 
 arcq_status arcq_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes) {
@@ -637,7 +664,7 @@ arcq_status arcq_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_p
 arcq_status arcq_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes, const uint8_t* w_scales,
                       float w_tensor_scale, int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy,
                       void* workspace, size_t workspace_bytes, void* stream) {
-    return gemv_entry("arcq_gemv", 16, x, M, K, ldx, perm, w_codes, w_scales, w_tensor_scale, N, S, y, y_dtype, ldy, workspace, workspace_bytes, stream);
+    return gemv_entry("arcq_gemv", 16, x, M, K, ldx, perm, w_codes, w_scales, w_tensor_scale, N, S, {}, y, y_dtype, ldy, workspace, workspace_bytes, stream);
 }
 
 arcq_status arcq_mx_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes) {
@@ -650,7 +677,120 @@ arcq_status arcq_mx_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int wit
 
 arcq_status arcq_mx_gemv(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes, const uint8_t* w_scales,
                          int64_t N, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
-    return gemv_entry("arcq_mx_gemv", 32, x, M, K, ldx, perm, w_codes, w_scales, 1.0f, N, S, y, y_dtype, ldy, workspace, workspace_bytes, stream);
+    return gemv_entry("arcq_mx_gemv", 32, x, M, K, ldx, perm, w_codes, w_scales, 1.0f, N, S, {}, y, y_dtype, ldy, workspace, workspace_bytes, stream);
+}
+
+arcq_status arcq_gemv_epilogue(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes, const uint8_t* w_scales,
+                               float w_tensor_scale, int64_t N, int64_t S, const void* bias, int activation, const void* residual, int64_t ldr,
+                               void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    return gemv_entry("arcq_gemv_epilogue", 16, x, M, K, ldx, perm, w_codes, w_scales, w_tensor_scale, N, S, {bias, residual, ldr, activation}, y, y_dtype, ldy,
+                      workspace, workspace_bytes, stream);
+}
+
+arcq_status arcq_mx_gemv_epilogue(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes, const uint8_t* w_scales,
+                                  int64_t N, int64_t S, const void* bias, int activation, const void* residual, int64_t ldr,
+                                  void* y, int y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    return gemv_entry("arcq_mx_gemv_epilogue", 32, x, M, K, ldx, perm, w_codes, w_scales, 1.0f, N, S, {bias, residual, ldr, activation}, y, y_dtype, ldy,
+                      workspace, workspace_bytes, stream);
+}
+
+static arcq_status check_route_shape(int64_t M, int64_t K, int64_t E) {
+    if (K <= 0 || (K % 8) != 0 || K > ARCQ_MAX_K) return fail(ARCQ_BAD_SHAPE, "K = %lld: must be > 0, a multiple of 8 and at most %d", (long long)K, ARCQ_MAX_K);
+    if (M < 0 || M > 0x7FFFFFFF) return fail(ARCQ_BAD_SHAPE, "M = %lld out of range", (long long)M);
+    if (E < 1 || E > ARCQ_MOE_MAX_EXPERTS) return fail(ARCQ_BAD_SHAPE, "E = %lld: must be 1 to %d", (long long)E, ARCQ_MOE_MAX_EXPERTS);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_moe_route_workspace_size(int64_t M, int64_t K, int64_t E, size_t* bytes) {
+    clear_error();
+    if (arcq_status st = check_route_shape(M, K, E)) return st;
+    if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    *bytes = M == 0 ? 0 : moe_route_workspace_bytes(M, K, E);
+    return ARCQ_OK;
+}
+
+// A workspace of `need` bytes.
+static arcq_status check_workspace(const char* who, size_t need, const void* workspace, size_t bytes) {
+    if (need == 0) return ARCQ_OK;
+    if (!workspace || bytes < need) return fail(ARCQ_WORKSPACE_TOO_SMALL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? bytes : 0);
+    if (!aligned(workspace, 256)) return fail(ARCQ_BAD_ALIGN, "%s: workspace must be 256-byte aligned", who);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, const void* router, int64_t ldr, int64_t E, const float* bias,
+                           int64_t top_k, uint32_t flags, int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "arcq_moe_route";
+    clear_error();
+    if (arcq_status st = check_route_shape(M, K, E)) return st;
+    if (flags & ~(ARCQ_MOE_SIGMOID | ARCQ_MOE_RENORMALIZE)) return fail(ARCQ_INVALID_ARG, "%s: unknown bits in flags = 0x%x", who, flags);
+    if (top_k < 1 || top_k > ARCQ_MOE_MAX_TOP_K || top_k > E)
+        return fail(ARCQ_BAD_SHAPE, "%s: top_k = %lld: must be 1 to %d and at most E = %lld", who, (long long)top_k, ARCQ_MOE_MAX_TOP_K, (long long)E);
+    if (arcq_status st = check_pitch(who, "x", ldx, K)) return st;
+    if (arcq_status st = check_pitch(who, "router", ldr, K)) return st;
+    if (M == 0) return ARCQ_OK;
+    if (arcq_status st = check_rows(who, "x", x, ldx)) return st;
+    if (arcq_status st = check_rows(who, "router", router, ldr)) return st;
+    if (!ids || !weights) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(ids, 4) || !aligned(weights, 4) || !aligned(bias, 4)) return fail(ARCQ_BAD_ALIGN, "%s: ids, weights and bias must be 4-byte aligned", who);
+    if (arcq_status st = check_workspace(who, moe_route_workspace_bytes(M, K, E), workspace, workspace_bytes)) return st;
+    return launch_moe_route(x, M, K, ldx, router, ldr, E, bias, top_k, flags, ids, weights, workspace, static_cast<hipStream_t>(stream));
+}
+
+static arcq_status check_moe_shape(int64_t M, int64_t top_k) {
+    if (M < 0 || M > 0x7FFFFFFF) return fail(ARCQ_BAD_SHAPE, "M = %lld out of range", (long long)M);
+    if (top_k < 1 || top_k > ARCQ_MOE_MAX_TOP_K) return fail(ARCQ_BAD_SHAPE, "top_k = %lld: must be 1 to %d", (long long)top_k, ARCQ_MOE_MAX_TOP_K);
+    return ARCQ_OK;
+}
+
+arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t K, int64_t I, int with_perm, size_t* bytes) {
+    clear_error();
+    if (arcq_status st = check_moe_shape(M, top_k)) return st;
+    if (arcq_status st = check_KS(K, 0)) return st;
+    if (arcq_status st = check_KS(I, 0)) return st;
+    if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
+    *bytes = M == 0 ? 0 : moe_workspace_bytes(M, top_k, K, I, with_perm != 0);
+    return ARCQ_OK;
+}
+
+static arcq_status moe_entry(const char* who, int block, const MoeArgs& p, size_t workspace_bytes) {
+    clear_error();
+    if (arcq_status st = check_moe_shape(p.M, p.top)) return st;
+    if (p.E < 1 || p.E > ARCQ_MOE_MAX_EXPERTS) return fail(ARCQ_BAD_SHAPE, "%s: E = %lld: must be 1 to %d", who, (long long)p.E, ARCQ_MOE_MAX_EXPERTS);
+    if (arcq_status st = block == 16 ? check_KS(p.K, p.S_up) : check_KS_mx(p.K, p.S_up)) return st;
+    if (arcq_status st = block == 16 ? check_KS(p.I, p.S_down) : check_KS_mx(p.I, p.S_down)) return st;
+    if (p.N < 0 || p.N > 0x7FFFFF00) return fail(ARCQ_BAD_SHAPE, "%s: N = %lld out of range", who, (long long)p.N);
+    if (p.y_dtype != ARCQ_DTYPE_F16 && p.y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", p.y_dtype);
+    if (arcq_status st = check_pitch(who, "x", p.ldx, p.K)) return st;
+    if (p.ldy < p.N) return fail(ARCQ_BAD_SHAPE, "ldy = %lld < N = %lld", (long long)p.ldy, (long long)p.N);
+    if (arcq_status st = check_epilogue(who, {nullptr, p.residual, p.ldr, p.activation}, p.M, p.N, p.y, p.ldy)) return st;
+    if (p.M == 0 || p.N == 0) return ARCQ_OK;
+    if (arcq_status st = check_rows(who, "x", p.x, p.ldx)) return st;
+    if (!p.ids || !p.weights || !p.up_codes || !p.up_scales || !p.down_codes || !p.down_scales || !p.y) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (block == 16 && (!p.up_tensor_scales || !p.down_tensor_scales)) return fail(ARCQ_INVALID_ARG, "%s: null pointer", who);
+    if (!aligned(p.up_codes, 8) || !aligned(p.down_codes, 8)) return fail(ARCQ_BAD_ALIGN, "%s: codes must be 8-byte aligned", who);
+    if (!aligned(p.perm, 16)) return fail(ARCQ_BAD_ALIGN, "%s: perm must be 16-byte aligned", who);
+    if (!aligned(p.ids, 4) || !aligned(p.weights, 4) || !aligned(p.up_tensor_scales, 4) || !aligned(p.down_tensor_scales, 4) || !aligned(p.y, 4))
+        return fail(ARCQ_BAD_ALIGN, "%s: ids, weights, tensor scales and y must be 4-byte aligned", who);
+    if (arcq_status st = check_workspace(who, moe_workspace_bytes(p.M, p.top, p.K, p.I, p.perm != nullptr), p.workspace, workspace_bytes)) return st;
+    return launch_moe(block, p);
+}
+
+arcq_status arcq_moe(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const int32_t* ids, const float* weights, int64_t top_k, int64_t E,
+                     const uint8_t* up_codes, const uint8_t* up_scales, const float* up_tensor_scales, int64_t I, int64_t S_up,
+                     const uint8_t* down_codes, const uint8_t* down_scales, const float* down_tensor_scales, int64_t N, int64_t S_down,
+                     int activation, const void* residual, int64_t ldr, void* y, int y_dtype, int64_t ldy,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+    return moe_entry("arcq_moe", 16, {x, M, K, ldx, perm, ids, weights, top_k, E, up_codes, up_scales, up_tensor_scales, I, S_up, down_codes, down_scales,
+                                      down_tensor_scales, N, S_down, activation, residual, ldr, y, y_dtype, ldy, workspace, static_cast<hipStream_t>(stream)}, workspace_bytes);
+}
+
+arcq_status arcq_mx_moe(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const int32_t* ids, const float* weights, int64_t top_k, int64_t E,
+                        const uint8_t* up_codes, const uint8_t* up_scales, int64_t I, int64_t S_up,
+                        const uint8_t* down_codes, const uint8_t* down_scales, int64_t N, int64_t S_down,
+                        int activation, const void* residual, int64_t ldr, void* y, int y_dtype, int64_t ldy,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    return moe_entry("arcq_mx_moe", 32, {x, M, K, ldx, perm, ids, weights, top_k, E, up_codes, up_scales, nullptr, I, S_up, down_codes, down_scales,
+                                         nullptr, N, S_down, activation, residual, ldr, y, y_dtype, ldy, workspace, static_cast<hipStream_t>(stream)}, workspace_bytes);
 }
 
 }  // extern "C"

@@ -1,0 +1,183 @@
+// What a product does with its sums behind them: y = act(sum + bias[n]) + residual[m, n], in fp32, rounded once to y's type.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/arcq.h"
+#include "gemm_epilogue.h"
+
+namespace arcq {
+
+// Products that end with their sums.
+struct NoEpilogue {};
+
+// bias: fp16 [N] or null; residual: [M, N] of y's type, pitch ldr, or null (it may be y itself: an element is read by the lane that writes it)
+template <typename OutT>
+struct Epilogue {
+    const _Float16* bias;
+    const OutT* residual;
+    int64_t ldr;
+    int activation;
+};
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// v / (1 + exp(-t)): the exponential by v_exp_f32, the quotient by v_rcp_f32, each within one unit of fp32's last place.  Where the exponential
+// overflows the quotient is 0, as it is in the limit.
+__device__ __forceinline__ float times_sigmoid(float v, float t) {
+    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * t));
+}
+
+// v Phi(v) = v erfc(-v / sqrt(2)) / 2.  erfc of the magnitude by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: a polynomial of
+// degree five in 1 / (1 + p z) times exp(-z z), within 1.5e-7 of it everywhere: 14 instructions, where the library's erff takes several times as many.
+__device__ __forceinline__ float gelu_erf(float v) {
+    const float z = __builtin_fabsf(v) * 0.70710678118654752440f;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, z, 1.0f));
+    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+    p = __builtin_fmaf(p, t, 1.421413741f);
+    p = __builtin_fmaf(p, t, -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * __builtin_fminf(__builtin_fabsf(v), 64.0f) * (p * t * __builtin_amdgcn_exp2f(-kLog2e * z * z));       // |v| Phi(-|v|), 0 past 64
+    return v > 0.0f ? v - tail : v < 0.0f ? -tail : v;
+}
+
+// v Phi(v) by 0.5 v (1 + tanh u) = v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
+__device__ __forceinline__ float gelu_tanh(float v) {
+    const float u2 = 1.59576912160573071176f * __builtin_fmaf(0.044715f * v * v, v, v);
+    return times_sigmoid(v, u2);
+}
+
+// The same activation for N values; which one is uniform over a launch.
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int activation) {
+    if (activation == ARCQ_ACT_NONE) return;
+    if (activation == ARCQ_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], v[i]);
+    } else if (activation == ARCQ_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+    } else if (activation == ARCQ_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gelu_erf(v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gelu_tanh(v[i]);
+    }
+}
+
+// One output.
+template <typename OutT>
+__device__ __forceinline__ float finish(const NoEpilogue&, float sum, int64_t, int64_t) { return sum; }
+template <typename OutT>
+__device__ __forceinline__ float finish(const Epilogue<OutT>& e, float sum, int64_t m, int64_t n) {
+    float v[1] = {sum};
+    const float r = e.residual ? (float)e.residual[m * e.ldr + n] : 0.0f;
+    if (e.bias) v[0] += (float)e.bias[n];
+    activate(v, e.activation);
+    return e.residual ? v[0] + r : v[0];
+}
+
+// A wave's tile of 32 WM x 32 WN sums (accumulator layout as in store_tile_swapped), a fragment row of 32 at a time through the wave's region of LDS in
+// fp32: the bias on the way in, where a lane holds four columns side by side; the activation in place, in a loop whose body is there once (unrolled over
+// the accumulator registers, five activations would fill the instruction cache); the residual on the way out, where a wave's loads and stores are
+// whole lines.  The residual of a fragment row is asked for before its sums are written: one wait for memory a fragment row, behind the LDS work.
+// lds_wave: epilogue_lds_bytes(WN) bytes, as in store_fragment_rows_f16_via_lds.
+template <typename OutT>
+struct OutPiece {                   // a lane's 16 bytes of y
+    static constexpr int V = 16 / (int)sizeof(OutT);
+    typedef OutT type __attribute__((ext_vector_type(V), aligned(sizeof(OutT))));
+};
+
+template <int WM, int WN, int I, typename OutT>
+__device__ __forceinline__ void finish_fragment_row(const float16v (&acc)[WM][WN], const float (&bias)[WN][16], uint8_t* lds_wave, int m0, int n0, int lane, int M,
+                                                    int N, OutT* __restrict__ y, int64_t ldy, const Epilogue<OutT>& e) {
+    typedef float float4v __attribute__((ext_vector_type(4)));
+    constexpr int PITCH = 128 * WN + 16;                                // (the padding spreads the rows over the banks)
+    static_assert(32 * PITCH <= epilogue_lds_bytes(WN), "a fragment row in fp32 fits the region");
+    constexpr int V = OutPiece<OutT>::V, LPR = 32 * WN / V, RPI = 64 / LPR, PASSES = 32 / RPI;
+    using piece_t = typename OutPiece<OutT>::type;
+    const int r = lane & 31, h = lane >> 5, row0 = lane / LPR, n = n0 + V * (lane % LPR);
+    piece_t res[PASSES];
+    if (e.residual) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int m = m0 + 32 * I + p * RPI + row0;
+            const OutT* at = e.residual + (int64_t)m * e.ldr + n;
+            if (m < M && n + V <= N) {
+                res[p] = *reinterpret_cast<const piece_t*>(at);
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    res[p][k] = (OutT)0.0f;
+                    if (m < M && n + k < N) res[p][k] = at[k];
+                }
+            }
+        }
+    }
+    uint8_t* own = lds_wave + r * PITCH + 16 * h;
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4v*>(own + 128 * j + 32 * g) = float4v{acc[I][j][4 * g] + bias[j][4 * g], acc[I][j][4 * g + 1] + bias[j][4 * g + 1],
+                                                                          acc[I][j][4 * g + 2] + bias[j][4 * g + 2], acc[I][j][4 * g + 3] + bias[j][4 * g + 3]};
+    if (e.activation != ARCQ_ACT_NONE) {
+#pragma unroll 1
+        for (int k = 0; k < 4 * WN; ++k) {
+            const float4v t = *reinterpret_cast<const float4v*>(own + 32 * k);
+            float v[4] = {t[0], t[1], t[2], t[3]};
+            activate(v, e.activation);
+            *reinterpret_cast<float4v*>(own + 32 * k) = float4v{v[0], v[1], v[2], v[3]};
+        }
+    }
+    // the reads below take what other lanes of this wave wrote: LDS operations of a wave complete in order
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int m = m0 + 32 * I + p * RPI + row0;
+        const uint8_t* from = lds_wave + (p * RPI + row0) * PITCH + 4 * V * (lane % LPR);
+        piece_t out;
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+            const float4v t = *reinterpret_cast<const float4v*>(from + 4 * k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[k + i] = (OutT)(e.residual ? t[i] + (float)res[p][k + i] : t[i]);
+        }
+        if (m >= M) continue;
+        OutT* dst = y + (int64_t)m * ldy + n;
+        if (n + V <= N) {
+            *reinterpret_cast<piece_t*>(dst) = out;
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (n + k < N) dst[k] = out[k];
+        }
+    }
+    // the next fragment row reuses the region
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <int WM, int WN, typename OutT>
+__device__ __forceinline__ void finish_tile(const float16v (&acc)[WM][WN], uint8_t* lds_wave, int m0, int n0, int lane, int M, int N, OutT* __restrict__ y,
+                                            int64_t ldy, const Epilogue<OutT>& e) {
+    float bias[WN][16];                         // of the lane's columns, in the accumulators' order
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+#pragma unroll
+        for (int g = 0; g < 16; ++g) {
+            const int n = n0 + 32 * j + 8 * (g >> 2) + 4 * (lane >> 5) + (g & 3);
+            bias[j][g] = e.bias && n < N ? (float)e.bias[n] : 0.0f;
+        }
+    finish_fragment_row<WM, WN, 0>(acc, bias, lds_wave, m0, n0, lane, M, N, y, ldy, e);
+    if constexpr (WM > 1) finish_fragment_row<WM, WN, 1>(acc, bias, lds_wave, m0, n0, lane, M, N, y, ldy, e);
+    if constexpr (WM > 2) finish_fragment_row<WM, WN, 2>(acc, bias, lds_wave, m0, n0, lane, M, N, y, ldy, e);
+    if constexpr (WM > 3) finish_fragment_row<WM, WN, 3>(acc, bias, lds_wave, m0, n0, lane, M, N, y, ldy, e);
+    static_assert(WM <= 4, "up to four fragment rows");
+}
+
+}  // namespace arcq

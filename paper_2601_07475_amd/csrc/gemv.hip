@@ -25,11 +25,13 @@
 //   MXFP4   4096           14336                                             8.7   3.6     9.3   3.4    13.9   2.2    17.9   1.7
 // From 1 to 4 rows the weights' way from memory and the tiles' uneven shares bound it, with more the rows, too: every workgroup reads all of them
 // (16 rows: 2 bytes x 16 for every 9 bytes of 16 weights of NT tiles).
+#include "epilogue.h"
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
 #include "lane_transpose.h"
 #include "lds_dma.h"
+#include "row_products.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -37,68 +39,6 @@
 namespace arcq {
 
 namespace {
-
-typedef float float4v __attribute__((ext_vector_type(4)));
-// Eight codes -> fp16, unscaled.
-__device__ __forceinline__ half8 widen8(uint32_t c) {
-    const half2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 1),
-                 p2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 3);
-    return half8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-}
-// E8M0 byte -> 2^(byte - 127); byte 0 is a subnormal.
-__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte != 0 ? byte << 23 : 0x400000u); }
-
-// Scale bytes of a group of four chunks: lane group q loads chunk q's; every lane gets those it needs of all four, one for each word: all
-// bytes of a chunk (MXFP4), or those of its half of the words' blocks of 32 k (NVFP4: even ones for q < 2, odd ones for the others).
-__device__ __forceinline__ void spread(uint32_t lower, uint32_t upper, uint32_t (&out)[4]) {
-    const uint2v a = __builtin_amdgcn_permlane32_swap(lower, upper, false, false);      // of lane groups q & 1 and (q & 1) + 2
-    const uint2v x = __builtin_amdgcn_permlane16_swap(a[0], a[0], false, false), y = __builtin_amdgcn_permlane16_swap(a[1], a[1], false, false);
-    out[0] = x[0], out[1] = x[1], out[2] = y[0], out[3] = y[1];
-}
-template <int B>
-__device__ __forceinline__ void scales_of_group(uint2 s, uint32_t (&out)[4]) {
-    if constexpr (B == 32) spread(s.x, s.x, out);
-    else spread(__builtin_amdgcn_perm(s.y, s.x, 0x06040200u), __builtin_amdgcn_perm(s.y, s.x, 0x07050301u), out);
-}
-
-// One chunk of MT row tiles and NT weight tiles.  NVFP4: words 0 and 2, 1 and 3 have accumulators of their own (CH = 2) where a single chain of dependent products
-// would make every one wait for the one before.
-template <int B, int MT, int NT, int CH>
-__device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[CH][MT][NT]) {
-    half8 w[NT][4];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        transpose_words(cw[t]);
-        const uint32_t word[4] = {cw[t].x, cw[t].y, cw[t].z, cw[t].w};
-        const uint32_t s01 = B == 16 ? scale_halves(sw[t], 0x0C010C00) : 0u, s23 = B == 16 ? scale_halves(sw[t], 0x0C030C02) : 0u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[t][j] = B == 16 ? decode8_half(word[j], j < 2 ? s01 : s23, j & 1) : widen8(word[j]);
-    }
-    if constexpr (B == 16) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < MT; ++r)
-                    acc[j % CH][r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w[t][j], acc[j % CH][r][t], 0, 0, 0);
-    } else {
-#pragma unroll
-        for (int r = 0; r < MT; ++r)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                float4v sum[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w[t][j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float s = power_of(sw[t] >> (8 * j) & 0xFFu);     // of weight row lane % 16, the column that the lane holds sums of
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[0][r][t][e] = __builtin_fmaf(sum[j][e], s, acc[0][r][t][e]);
-                }
-            }
-    }
-}
 
 enum Rows { WHOLE, SLICE };
 constexpr int slice_chunks(int rows, int nt, int waves) { return rows == 4 ? 4 : rows == 16 && nt <= 2 && waves == 8 ? 2 : 1; }     // of a wave, as registers allow
@@ -109,10 +49,11 @@ constexpr int kWhole = 8192;                    // WHOLE: most values of the row
 // ROWS   most rows of x of a workgroup: 4, 16 or 32, in tiles of 16 that share every decoded weight
 // NT     tiles of 16 weight rows of a workgroup, whose WAVES waves split K
 // LDS: the rows (WHOLE: M K 2 bytes twice, the second in the channels' own order), then the waves' partial tiles, two sets
-template <int B, int ROWS, int NT, int WAVES, int X, typename OutT>
+// ep     what follows the sums
+template <int B, int ROWS, int NT, int WAVES, int X, typename OutT, typename Ep>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS == 4 || WAVES == 16 ? 4 : 2, 4))) void gemv_kernel(
     const uint16_t* __restrict__ x, int64_t ldx, int M, int K, const int32_t* __restrict__ perm, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride, uint32_t splits) {
+    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride, uint32_t splits, Ep ep) {
     constexpr int MT = (ROWS + 15) / 16, THREADS = 64 * WAVES, PIECES = kWhole / 8 / THREADS;
     static_assert(X == SLICE || MT == 1, "WHOLE: up to 16 rows");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -365,7 +306,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) sum += part[(w * MT * NT * 4 + rt * 4 + e) * 64 + l];
             const int m = m0 + 16 * (rt / NT) + 4 * (l >> 4) + e, n = (tile * NT + rt % NT) * 16 + (l & 15);
-            if (m < min(M, m0 + ROWS) && n < N) store_out(y + (int64_t)m * ldy + n, sum * alpha);
+            if (m < min(M, m0 + ROWS) && n < N) store_out(y + (int64_t)m * ldy + n, finish<OutT>(ep, sum * alpha, m, n));
         }
     }
 }
@@ -393,6 +334,7 @@ struct GemvArgs {
     float alpha;
     int64_t ldy;
     hipStream_t stream;
+    EpilogueArgs epilogue;
 };
 
 bool whole_rows(int64_t M, int64_t K) { return M <= 4 && M * K <= kWhole; }
@@ -433,9 +375,9 @@ GemvPlan plan_gemv(int64_t M, int64_t N, int64_t K, bool reorder) {
     return best;
 }
 
-template <int B, int ROWS, int NT, int WAVES, int X, typename OutT>
-arcq_status launch_tiles(const GemvArgs& a, int splits, OutT* y) {
-    auto kern = gemv_kernel<B, ROWS, NT, WAVES, X, OutT>;
+template <int B, int ROWS, int NT, int WAVES, int X, typename OutT, typename Ep>
+arcq_status launch_tiles(const GemvArgs& a, int splits, OutT* y, const Ep& ep) {
+    auto kern = gemv_kernel<B, ROWS, NT, WAVES, X, OutT, Ep>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     const size_t rows = X == WHOLE ? (size_t)a.M * a.K * 4 : (size_t)WAVES * slice_bytes(ROWS, NT, WAVES);
@@ -444,31 +386,35 @@ arcq_status launch_tiles(const GemvArgs& a, int splits, OutT* y) {
     const int per_cu = ROWS == 4 ? 2 : 1;           // as registers and LDS allow
     const unsigned stride = (unsigned)std::min<int64_t>(tiles_n, std::max(num_cu() * per_cu / splits, 1));
     hipLaunchKernelGGL(kern, dim3(stride * (unsigned)(splits * tiles_m)), dim3(64 * WAVES), lds, a.stream, a.x, a.ldx, (int)a.M, (int)a.K, a.perm,
-                       a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride, (uint32_t)splits);
+                       a.w_codes, a.w_scales, (int)a.N, (a.K + a.S) / 2, (a.K + a.S) / B, a.alpha, y, a.ldy, (int)tiles_n, stride, (uint32_t)splits, ep);
     return check_launch("gemv_kernel");
 }
 
 // Waves that split K: up to 4 rows, 8, so that two workgroups fit the registers of a compute unit (14336 x 4096 10.8 -> 10.1 us; with 16, 4096 x 4096
 // 4.7 -> 5.0).  16 rows, one tile: 16 where each has two chunks of 128 (4096 x 14336 14.9 -> 13.9 us, 1024 x 28672 24.0 -> 20.3; 4096 x 1024 4.3 -> 4.6).
-template <int B, typename OutT>
-arcq_status launch_planned(const GemvArgs& a, GemvPlan p, OutT* y) {
-    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, 8, WHOLE>(a, 1, y) : launch_tiles<B, 4, 1, 8, SLICE>(a, p.splits, y);
+template <int B, typename OutT, typename Ep>
+arcq_status launch_planned(const GemvArgs& a, GemvPlan p, OutT* y, const Ep& ep) {
+    if (a.M <= 4) return a.perm ? launch_tiles<B, 4, 1, 8, WHOLE>(a, 1, y, ep) : launch_tiles<B, 4, 1, 8, SLICE>(a, p.splits, y, ep);
     if (a.M <= 16)
-        return p.nt == 1   ? (a.K / p.splits >= 4096 ? launch_tiles<B, 16, 1, 16, SLICE>(a, p.splits, y) : launch_tiles<B, 16, 1, 8, SLICE>(a, p.splits, y))
-               : p.nt == 2 ? launch_tiles<B, 16, 2, 8, SLICE>(a, p.splits, y)
-                           : launch_tiles<B, 16, 4, 8, SLICE>(a, p.splits, y);
-    return p.nt == 1 ? launch_tiles<B, 32, 1, 8, SLICE>(a, p.splits, y) : launch_tiles<B, 32, 2, 8, SLICE>(a, p.splits, y);
+        return p.nt == 1   ? (a.K / p.splits >= 4096 ? launch_tiles<B, 16, 1, 16, SLICE>(a, p.splits, y, ep) : launch_tiles<B, 16, 1, 8, SLICE>(a, p.splits, y, ep))
+               : p.nt == 2 ? launch_tiles<B, 16, 2, 8, SLICE>(a, p.splits, y, ep)
+                           : launch_tiles<B, 16, 4, 8, SLICE>(a, p.splits, y, ep);
+    return p.nt == 1 ? launch_tiles<B, 32, 1, 8, SLICE>(a, p.splits, y, ep) : launch_tiles<B, 32, 2, 8, SLICE>(a, p.splits, y, ep);
 }
 
 template <int B, typename OutT>
 arcq_status launch_typed(const GemvArgs& a, GemvPlan p, OutT* y, float* partial) {
-    if (p.splits == 1) return launch_planned<B>(a, p, y);
+    constexpr int TYPE = std::is_same<OutT, _Float16>::value ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32;
+    const EpilogueArgs& e = a.epilogue;
+    if (p.splits == 1)
+        return e.any() ? launch_planned<B>(a, p, y, Epilogue<OutT>{static_cast<const _Float16*>(e.bias), static_cast<const OutT*>(e.residual), e.ldr, e.activation})
+                       : launch_planned<B>(a, p, y, NoEpilogue{});
     GemvArgs run = a;
     run.alpha = 1.0f;
     run.ldy = a.N;
-    if (arcq_status st = launch_planned<B>(run, p, partial)) return st;
-    return launch_splitk_reduce(partial, p.splits, a.M, a.N, a.alpha, y, std::is_same<OutT, _Float16>::value ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy,
-                                a.stream);
+    if (arcq_status st = launch_planned<B>(run, p, partial, NoEpilogue{})) return st;
+    return e.any() ? launch_splitk_epilogue(partial, p.splits, a.M, a.N, a.alpha, y, TYPE, a.ldy, e, a.stream)
+                   : launch_splitk_reduce(partial, p.splits, a.M, a.N, a.alpha, y, TYPE, a.ldy, a.stream);
 }
 
 // Rows of a launch: grids and workspaces stay within bounds for any M.
@@ -485,9 +431,7 @@ template <typename OutT>
 arcq_status launch_rows(int block, const GemvArgs& a, GemvPlan p, OutT* y, uint16_t* reordered, float* partial) {
     GemvArgs run = a;
     if (reordered) {
-        const unsigned parts = (unsigned)((a.K / 8 + 255) / 256);
-        hipLaunchKernelGGL(reorder_rows_kernel, dim3(parts * (unsigned)a.M), dim3(256), 0, a.stream, a.x, a.ldx, (int)a.K, a.perm, reordered, parts);
-        if (arcq_status st = check_launch("reorder_rows_kernel")) return st;
+        if (arcq_status st = launch_reorder_rows(a.x, a.M, a.K, a.ldx, a.perm, reordered, a.stream)) return st;
         run.x = reordered;
         run.ldx = a.K;
         run.perm = nullptr;
@@ -497,6 +441,13 @@ arcq_status launch_rows(int block, const GemvArgs& a, GemvPlan p, OutT* y, uint1
 
 }  // namespace
 
+arcq_status launch_reorder_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, void* out, hipStream_t stream) {
+    const unsigned parts = (unsigned)((K / 8 + 255) / 256);
+    hipLaunchKernelGGL(reorder_rows_kernel, dim3(parts * (unsigned)M), dim3(256), 0, stream, static_cast<const uint16_t*>(x), ldx, (int)K, perm,
+                       static_cast<uint16_t*>(out), parts);
+    return check_launch("reorder_rows_kernel");
+}
+
 size_t gemv_workspace_bytes(int64_t M, int64_t N, int64_t K, bool reorder) {
     const int64_t most = std::min(M, kMostRows);
     const GemvWorkspace w = gemv_workspace(most, N, K, reorder, plan_gemv(most, N, K, reorder));
@@ -505,7 +456,7 @@ size_t gemv_workspace_bytes(int64_t M, int64_t N, int64_t K, bool reorder) {
 
 arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
                         const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
-                        hipStream_t stream) {
+                        const EpilogueArgs& epilogue, hipStream_t stream) {
     const int64_t most = std::min(M, kMostRows);
     const GemvPlan p = plan_gemv(most, N, K, perm != nullptr);
     const GemvWorkspace w = gemv_workspace(most, N, K, perm != nullptr, p);
@@ -513,7 +464,8 @@ arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t 
     float* partial = w.partial > 0 ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.reordered) : nullptr;
     for (int64_t m = 0; m < M; m += kMostRows) {
         const int64_t rows = std::min(M - m, kMostRows);
-        const GemvArgs a = {static_cast<const uint16_t*>(x) + m * ldx, rows, K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream};
+        GemvArgs a = {static_cast<const uint16_t*>(x) + m * ldx, rows, K, ldx, perm, w_codes, w_scales, N, S, alpha, ldy, stream, epilogue};
+        if (epilogue.residual) a.epilogue.residual = static_cast<const uint8_t*>(epilogue.residual) + m * epilogue.ldr * (y_dtype == ARCQ_DTYPE_F16 ? 2 : 4);
         // (with more rows than a launch takes, the last run goes like the others, in one tile of 32 rows at least: what fits them fits it)
         const arcq_status st = y_dtype == ARCQ_DTYPE_F16 ? launch_rows(block, a, p, static_cast<_Float16*>(y) + m * ldy, reordered, partial)
                                                          : launch_rows(block, a, p, static_cast<float*>(y) + m * ldy, reordered, partial);

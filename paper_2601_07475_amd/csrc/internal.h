@@ -96,6 +96,14 @@ arcq_status launch_mx_gemm(const uint8_t* a_codes, const uint8_t* a_scales, cons
                            const uint8_t* w_scales, int64_t M, int64_t N, int64_t Kp, void* y, int y_dtype, int64_t ldy,
                            void* workspace, hipStream_t stream);
 size_t mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t Kp);
+// What follows a product's sums (epilogue.h): bias fp16 [N] or null, residual [M, N] of y's type or null, an ARCQ_ACT_.
+struct EpilogueArgs {
+    const void* bias = nullptr;
+    const void* residual = nullptr;
+    int64_t ldr = 0;
+    int activation = ARCQ_ACT_NONE;
+    bool any() const { return bias || residual || activation != ARCQ_ACT_NONE; }
+};
 // MXFP8 activations (residual and hidden: both or neither; gamma null: no norm; perm null: channels stay in order) times MXFP4 weights
 arcq_status launch_mx8_quantize(const void* x, int64_t ldx, const void* residual, int64_t ldr, void* hidden, int64_t ldh, int64_t rows, int64_t K,
                                 const void* gamma, float eps, const int32_t* perm, uint8_t* codes, uint8_t* scales, uint32_t flags, hipStream_t stream);
@@ -103,14 +111,49 @@ size_t mx8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool fp32, bool workspace, arcq_route* route);
 // workspace: fp32 partial results of a split reduction dimension, or null (never splits)
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
-                            int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream);
+                            int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, const EpilogueArgs& epilogue,
+                            hipStream_t stream);
 // fp16 rows times packed weights (block 16: NVFP4, 32: MXFP4)
 size_t gemv_workspace_bytes(int64_t M, int64_t N, int64_t K, bool reorder);
 arcq_status launch_gemv(int block, const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, const uint8_t* w_codes,
                         const uint8_t* w_scales, int64_t N, int64_t S, float alpha, void* y, int y_dtype, int64_t ldy, void* workspace,
-                        hipStream_t stream);
+                        const EpilogueArgs& epilogue, hipStream_t stream);
+// fp16 rows [M, K], channels in the order perm -> out [M, K], dense; M at most 65536
+arcq_status launch_reorder_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm, void* out, hipStream_t stream);
+// The experts of a mixture (block 16: NVFP4, 32: MXFP4; perm and residual may be null)
+struct MoeArgs {
+    const void* x;
+    int64_t M, K, ldx;
+    const int32_t* perm;
+    const int32_t* ids;
+    const float* weights;
+    int64_t top, E;
+    const uint8_t *up_codes, *up_scales;
+    const float* up_tensor_scales;
+    int64_t I, S_up;
+    const uint8_t *down_codes, *down_scales;
+    const float* down_tensor_scales;
+    int64_t N, S_down;
+    int activation;
+    const void* residual;
+    int64_t ldr;
+    void* y;
+    int y_dtype;
+    int64_t ldy;
+    void* workspace;
+    hipStream_t stream;
+};
+size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t K, int64_t I, bool reorder);
+arcq_status launch_moe(int block, const MoeArgs& p);
+// The router
+size_t moe_route_workspace_bytes(int64_t M, int64_t K, int64_t E);
+arcq_status launch_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, const void* router, int64_t ldr, int64_t E, const float* bias, int64_t top,
+                             uint32_t flags, int32_t* ids, float* weights, void* workspace, hipStream_t stream);
 // y = alpha * (partial[0] + partial[1] + ... in index order), partial results fp32 [splits][M][N]
 arcq_status launch_splitk_reduce(const float* partial, int splits, int M, int N, float alpha, void* y, int y_dtype,
                                  int64_t ldy, hipStream_t stream);
+// the same, and what follows
+arcq_status launch_splitk_epilogue(const float* partial, int splits, int M, int N, float alpha, void* y, int y_dtype, int64_t ldy, const EpilogueArgs& e,
+                                   hipStream_t stream);
 
 }  // namespace arcq

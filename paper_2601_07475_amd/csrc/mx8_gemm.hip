@@ -18,6 +18,7 @@
 // every compute unit busy, the instruction reaches 3.8 at 1.82 GHz: power), fp32 output 2.67 ms; 777 x 6147 over 4352 48 us, fp32 53 (two passes take 22 on
 // the matrix unit); 300 x 4096 over 14336 43 us; streaming: 16 x 14336 over 4096 9.4 us (3.3 TB/s of weights), 1 x 4096 over 4096 4.5, either type.
 #include "code_rows.h"
+#include "epilogue.h"
 #include "gemm_decode.h"
 #include "gemm_epilogue.h"
 #include "internal.h"
@@ -52,10 +53,10 @@ __device__ __forceinline__ void split_codes(const int8v& a, int8v& large, int8v&
 // Weight-streaming kernel: tiles of 16 MT rows by 16 NT weight rows, K split over the WAVES waves of a workgroup.  Bound by reading the
 // weights once (17/32 byte per weight) for a few rows; any sizes.  Whole chunks of 128 k go four at a time: every code of the four, and their scale
 // bytes, four to a load and transposed across the lane groups, are in flight at once.
-template <int MT, int NT, int WAVES, typename OutT>
+template <int MT, int NT, int WAVES, typename OutT, typename Ep>
 __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n, uint32_t tiles_m, int splits) {
+    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n, uint32_t tiles_m, int splits, Ep ep) {
     // the partial tiles of BATCH weight tiles fit the static LDS limit at a time
     constexpr int BATCH = WAVES * MT * NT > 64 ? (NT + 1) / 2 : NT;
     __shared__ float red[WAVES][MT * BATCH][4][64];
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) sum += red[w][rt][e][l];
             const int m = m0 + 16 * (rt / BATCH) + 4 * (l >> 4) + e, n = n0 + 16 * (t0 + rt % BATCH) + (l & 15);
-            if (m < M && n < N) store_out(y + (int64_t)m * ldy + n, sum);
+            if (m < M && n < N) store_out(y + (int64_t)m * ldy + n, finish<OutT>(ep, sum, m, n));
         }
     }
 }
@@ -214,11 +215,11 @@ __device__ __forceinline__ float16v mfma_w4a8(const uint4& w, const int8v& a, co
                   : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vw, a, c, 4, 0, 2, (int)sw, 2, (int)sa);
 }
 
-template <int WM, int WN, int GM, int GN, int NS, typename OutT>
+template <int WM, int WN, int GM, int GN, int NS, typename OutT, typename Ep>
 __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
     const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, int tiles_m, int tiles_n,
-    int group_rows, int splits, int64_t split_stride) {
+    int group_rows, int splits, int64_t split_stride, Ep ep) {
     using C = Mx8Tile<WM, WN, GM, GN, NS>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     // With splits > 1 workgroup split * num_tiles + tile adds up a run of K and stores an fp32 partial tile at y + split * split_stride
@@ -448,7 +449,11 @@ __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
     wait_vmcnt<0>();                            // no copy may still be in flight when the LDS is released
 
     const int m0 = wg_m0 + wrow0, n0 = wg_n0 + wcol0;
-    if constexpr (std::is_same<OutT, _Float16>::value) {
+    if constexpr (std::is_same<Ep, Epilogue<OutT>>::value) {
+        static_assert(epilogue_lds_bytes(WN) * GM * GN <= C::LDS_BYTES, "one epilogue region per wave must fit");
+        wg_barrier();                           // every wave has read its last operands: the ring is free
+        finish_tile<WM, WN>(acc, lds + wave * epilogue_lds_bytes(WN), m0, n0, lane, M, N, y, ldy, ep);
+    } else if constexpr (std::is_same<OutT, _Float16>::value) {
         static_assert(epilogue_lds_bytes(WN) * GM * GN <= C::LDS_BYTES, "one epilogue region per wave must fit");
         wg_barrier();                           // every wave has read its last operands: the ring is free
         uint8_t* region = lds + wave * epilogue_lds_bytes(WN);
@@ -464,25 +469,33 @@ struct Mx8Args {
     int M, N, nb, nbw;
     int64_t ldy;
     hipStream_t stream;
+    EpilogueArgs epilogue;
 };
 
-template <int MT, int NT, typename OutT>
+// The kernels' last argument: nothing (NoEpilogue), or what a.epilogue says.
+template <typename Ep>
+Ep epilogue_of(const Mx8Args& a) {
+    if constexpr (std::is_same<Ep, NoEpilogue>::value) return Ep{};
+    else return Ep{static_cast<const _Float16*>(a.epilogue.bias), static_cast<decltype(Ep::residual)>(a.epilogue.residual), a.epilogue.ldr, a.epilogue.activation};
+}
+
+template <int MT, int NT, typename OutT, typename Ep>
 arcq_status launch_stream(const Mx8Args& a, OutT* y, int splits, int64_t /* runs of the workspace are M N apart */) {
     const unsigned tiles_n = ((unsigned)a.N + 16 * NT - 1) / (16 * NT), tiles_m = ((unsigned)a.M + 16 * MT - 1) / (16 * MT);
-    hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, OutT>), dim3(tiles_n * tiles_m * (unsigned)splits), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
-                       a.nb, a.nbw, y, a.ldy, tiles_n, tiles_m, splits);
+    hipLaunchKernelGGL((mx8_stream_kernel<MT, NT, 8, OutT, Ep>), dim3(tiles_n * tiles_m * (unsigned)splits), dim3(512), 0, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales, a.M, a.N,
+                       a.nb, a.nbw, y, a.ldy, tiles_n, tiles_m, splits, epilogue_of<Ep>(a));
     return check_launch("mx8_stream_kernel");
 }
 
-template <int WM, int WN, int NS, typename OutT>
+template <int WM, int WN, int NS, typename OutT, typename Ep>
 arcq_status launch_tiles(const Mx8Args& a, OutT* y, int splits, int64_t split_stride) {
     using C = Mx8Tile<WM, WN, 2, 2, NS>;
     const int tiles_m = (a.M + C::BM - 1) / C::BM, tiles_n = (a.N + C::BN - 1) / C::BN;
-    auto kern = mx8_tile_kernel<WM, WN, 2, 2, NS, OutT>;
+    auto kern = mx8_tile_kernel<WM, WN, 2, 2, NS, OutT, Ep>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     hipLaunchKernelGGL(kern, dim3(tiles_m * tiles_n * splits), dim3(C::NT), C::LDS_BYTES, a.stream, a.a_codes, a.a_scales, a.w_codes, a.w_scales,
-                       a.M, a.N, a.nb, a.nbw, y, a.ldy, tiles_m, tiles_n, tile_group_rows(tiles_m, tiles_n), splits, split_stride);
+                       a.M, a.N, a.nb, a.nbw, y, a.ldy, tiles_m, tiles_n, tile_group_rows(tiles_m, tiles_n), splits, split_stride, epilogue_of<Ep>(a));
     return check_launch("mx8_tile_kernel");
 }
 
@@ -571,24 +584,24 @@ Mx8Plan plan_mx8(int64_t M, int64_t N, int64_t nb, int64_t nbw, bool fp32, bool 
 template <typename OutT>
 using Launch = arcq_status (*)(const Mx8Args& a, OutT* y, int splits, int64_t split_stride);
 
-template <typename OutT, size_t... I>
+template <typename OutT, typename Ep, size_t... I>
 Launch<OutT> tile_launch(int tile, std::index_sequence<I...>) {
     constexpr int FIRST = first_tile(std::is_same<OutT, float>::value);
-    static constexpr Launch<OutT> launches[] = {launch_tiles<kTiles[FIRST + I].wm, kTiles[FIRST + I].wn, kTiles[FIRST + I].ns, OutT>...};
+    static constexpr Launch<OutT> launches[] = {launch_tiles<kTiles[FIRST + I].wm, kTiles[FIRST + I].wn, kTiles[FIRST + I].ns, OutT, Ep>...};
     return launches[tile - FIRST];
 }
 
-template <int MT, typename OutT, size_t... I>
+template <int MT, typename OutT, typename Ep, size_t... I>
 Launch<OutT> stream_launch(int nt, std::index_sequence<I...>) {
-    static constexpr Launch<OutT> launches[] = {launch_stream<MT, 1 + (int)I, OutT>...};
+    static constexpr Launch<OutT> launches[] = {launch_stream<MT, 1 + (int)I, OutT, Ep>...};
     return launches[nt - 1];
 }
 
-template <typename OutT>
+template <typename OutT, typename Ep>
 Launch<OutT> launch_of(const Mx8Plan& p) {
-    if (p.tile >= 0) return tile_launch<OutT>(p.tile, std::make_index_sequence<kTileCount - first_tile(std::is_same<OutT, float>::value)>{});
-    return p.mt == 1 ? stream_launch<1, OutT>(p.nt, std::make_index_sequence<kStreamTiles[0]>{})
-                     : stream_launch<2, OutT>(p.nt, std::make_index_sequence<kStreamTiles[1]>{});
+    if (p.tile >= 0) return tile_launch<OutT, Ep>(p.tile, std::make_index_sequence<kTileCount - first_tile(std::is_same<OutT, float>::value)>{});
+    return p.mt == 1 ? stream_launch<1, OutT, Ep>(p.nt, std::make_index_sequence<kStreamTiles[0]>{})
+                     : stream_launch<2, OutT, Ep>(p.nt, std::make_index_sequence<kStreamTiles[1]>{});
 }
 
 // One run of K to y, or several to `partial`, and what adds them up.
@@ -596,11 +609,14 @@ template <typename OutT>
 arcq_status launch_typed(const Mx8Args& a, OutT* y, float* partial) {
     constexpr bool HALF = std::is_same<OutT, _Float16>::value;
     const Mx8Plan plan = plan_mx8(a.M, a.N, a.nb, a.nbw, !HALF, partial != nullptr);
-    if (plan.splits == 1) return launch_of<OutT>(plan)(a, y, 1, 0);
+    const bool more = a.epilogue.any();
+    if (plan.splits == 1) return more ? launch_of<OutT, Epilogue<OutT>>(plan)(a, y, 1, 0) : launch_of<OutT, NoEpilogue>(plan)(a, y, 1, 0);
     Mx8Args run = a;
     run.ldy = a.N;
-    if (arcq_status st = launch_of<float>(plan)(run, partial, plan.splits, (int64_t)a.M * a.N)) return st;
-    return launch_splitk_reduce(partial, plan.splits, a.M, a.N, 1.0f, y, HALF ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32, a.ldy, a.stream);
+    if (arcq_status st = launch_of<float, NoEpilogue>(plan)(run, partial, plan.splits, (int64_t)a.M * a.N)) return st;
+    constexpr int TYPE = HALF ? ARCQ_DTYPE_F16 : ARCQ_DTYPE_F32;
+    return more ? launch_splitk_epilogue(partial, plan.splits, a.M, a.N, 1.0f, y, TYPE, a.ldy, a.epilogue, a.stream)
+                : launch_splitk_reduce(partial, plan.splits, a.M, a.N, 1.0f, y, TYPE, a.ldy, a.stream);
 }
 
 }  // namespace
@@ -625,12 +641,14 @@ void mx8_gemm_route(int64_t M, int64_t N, int64_t K, int64_t S, bool fp32, bool 
 }
 
 arcq_status launch_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t M,
-                            int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, hipStream_t stream) {
+                            int64_t N, int64_t K, int64_t S, void* y, int y_dtype, int64_t ldy, void* workspace, const EpilogueArgs& epilogue,
+                            hipStream_t stream) {
     float* partial = static_cast<float*>(workspace);
     const int64_t most = rows_of_launch(N, K);
     for (int64_t m = 0; m < M; m += most) {
-        const Mx8Args a = {a_codes + m * K, a_scales + m * (K >> 5), w_codes, w_scales, (int)std::min(M - m, most), (int)N, (int)(K >> 5),
-                           (int)((K + S) >> 5), ldy, stream};
+        Mx8Args a = {a_codes + m * K, a_scales + m * (K >> 5), w_codes, w_scales, (int)std::min(M - m, most), (int)N, (int)(K >> 5),
+                     (int)((K + S) >> 5), ldy, stream, epilogue};
+        if (epilogue.residual) a.epilogue.residual = static_cast<const uint8_t*>(epilogue.residual) + m * epilogue.ldr * (y_dtype == ARCQ_DTYPE_F16 ? 2 : 4);
         // (a last run of fewer rows may have a plan of its own, with more runs of K than the workspace was made for: without them)
         float* room = m == 0 || M - m >= most ? partial : nullptr;
         const arcq_status st = y_dtype == ARCQ_DTYPE_F16 ? launch_typed(a, static_cast<_Float16*>(y) + m * ldy, room)
