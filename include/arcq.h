@@ -419,10 +419,10 @@ arcq_status arcq_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, con
  *          down_tensor_scales: fp32 [E].  All packed in the plain layout (not ARCQ_LAYOUT_INTERLEAVED with S > 0); the S columns that repeat the outliers'
  *          weights are passed over.  Codes 8-byte aligned.  K, S_up and I, S_down as in the packer.
  * activation  an ARCQ_ACT_;  residual, y  as in the calls with an epilogue: residual may be NULL or y
- * 1 <= top_k <= ARCQ_MOE_MAX_TOP_K, 1 <= E <= ARCQ_MOE_MAX_EXPERTS
+ * 1 <= top_k <= ARCQ_MOE_MAX_TOP_K, 1 <= E <= ARCQ_MOE_MAX_EXPERTS, N <= 2^24
  * workspace  256-byte aligned, at least arcq_moe_workspace_size bytes (for either format).  Calls that share one must not overlap.
  */
-arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t K, int64_t I, int with_perm, size_t* bytes);
+arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t E, int64_t K, int64_t I, int64_t N, int with_perm, size_t* bytes);
 arcq_status arcq_moe(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,
                      const int32_t* ids, const float* weights, int64_t top_k, int64_t E,
                      const uint8_t* up_codes, const uint8_t* up_scales, const float* up_tensor_scales, int64_t I, int64_t S_up,

@@ -84,7 +84,7 @@ SIGNATURES = {
     "arcq_mx_gemv_epilogue": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
     "arcq_moe_route_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, ctypes.POINTER(_sz)]),
     "arcq_moe_route": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _u32, _vp, _vp, _vp, _sz, _vp]),
-    "arcq_moe_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, _i64, ctypes.c_int, ctypes.POINTER(_sz)]),
+    "arcq_moe_workspace_size": (ctypes.c_int, [_i64, _i64, _i64, _i64, _i64, _i64, ctypes.c_int, ctypes.POINTER(_sz)]),
     "arcq_moe": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64,
                                 ctypes.c_int, _vp, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]),
     "arcq_mx_moe": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64,
@@ -637,9 +637,9 @@ def arcq_moe_route(x, router, top_k, bias=None, flags=0, ids=None, weights=None,
     return ids, weights
 
 
-def arcq_moe_workspace_size(M, top_k, K, I, with_perm):
+def arcq_moe_workspace_size(M, top_k, E, K, I, N, with_perm):
     b = _sz(0)
-    _check(lib().arcq_moe_workspace_size(M, top_k, K, I, int(with_perm), ctypes.byref(b)))
+    _check(lib().arcq_moe_workspace_size(M, top_k, E, K, I, N, int(with_perm), ctypes.byref(b)))
     return b.value
 
 
@@ -675,7 +675,7 @@ def _moe_args(block, x, perm, ids, weights, up_codes, up_scales, up_ts, down_cod
         out_dtype = residual.dtype
     y, dt, ldy = _output(x, M, N, out_dtype, y, device)
     if workspace is None and make:
-        need = arcq_moe_workspace_size(M, top_k, K, I, perm is not None)
+        need = arcq_moe_workspace_size(M, top_k, E, K, I, N, perm is not None)
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _, activation, residual, ldr = _epilogue(None, activation, residual, M, N, y, device)
     return (x.data_ptr(), M, K, ldx, _perm(perm, K, device), ids.data_ptr(), weights.data_ptr(), top_k, E,

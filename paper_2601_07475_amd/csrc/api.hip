@@ -736,29 +736,29 @@ arcq_status arcq_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, con
     return launch_moe_route(x, M, K, ldx, router, ldr, E, bias, top_k, flags, ids, weights, workspace, static_cast<hipStream_t>(stream));
 }
 
-static arcq_status check_moe_shape(int64_t M, int64_t top_k) {
-    if (M < 0 || M > 0x7FFFFFFF) return fail(ARCQ_BAD_SHAPE, "M = %lld out of range", (long long)M);
+static arcq_status check_moe_shape(int64_t M, int64_t N, int64_t top_k, int64_t E) {
+    if (M < 0 || N < 0 || M > 0x7FFFFFFF || N > 0x1000000)      // (a launch has a workgroup for every 128 features of an expert, and their results of 1024 slots)
+        return fail(ARCQ_BAD_SHAPE, "M = %lld, N = %lld out of range", (long long)M, (long long)N);
+    if (E < 1 || E > ARCQ_MOE_MAX_EXPERTS) return fail(ARCQ_BAD_SHAPE, "E = %lld: must be 1 to %d", (long long)E, ARCQ_MOE_MAX_EXPERTS);
     if (top_k < 1 || top_k > ARCQ_MOE_MAX_TOP_K) return fail(ARCQ_BAD_SHAPE, "top_k = %lld: must be 1 to %d", (long long)top_k, ARCQ_MOE_MAX_TOP_K);
     return ARCQ_OK;
 }
 
-arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t K, int64_t I, int with_perm, size_t* bytes) {
+arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t E, int64_t K, int64_t I, int64_t N, int with_perm, size_t* bytes) {
     clear_error();
-    if (arcq_status st = check_moe_shape(M, top_k)) return st;
+    if (arcq_status st = check_moe_shape(M, N, top_k, E)) return st;
     if (arcq_status st = check_KS(K, 0)) return st;
     if (arcq_status st = check_KS(I, 0)) return st;
     if (!bytes) return fail(ARCQ_INVALID_ARG, "null output pointer");
-    *bytes = M == 0 ? 0 : moe_workspace_bytes(M, top_k, K, I, with_perm != 0);
+    *bytes = M == 0 || N == 0 ? 0 : moe_workspace_bytes(M, top_k, E, K, I, N, with_perm != 0);
     return ARCQ_OK;
 }
 
 static arcq_status moe_entry(const char* who, int block, const MoeArgs& p, size_t workspace_bytes) {
     clear_error();
-    if (arcq_status st = check_moe_shape(p.M, p.top)) return st;
-    if (p.E < 1 || p.E > ARCQ_MOE_MAX_EXPERTS) return fail(ARCQ_BAD_SHAPE, "%s: E = %lld: must be 1 to %d", who, (long long)p.E, ARCQ_MOE_MAX_EXPERTS);
+    if (arcq_status st = check_moe_shape(p.M, p.N, p.top, p.E)) return st;
     if (arcq_status st = block == 16 ? check_KS(p.K, p.S_up) : check_KS_mx(p.K, p.S_up)) return st;
     if (arcq_status st = block == 16 ? check_KS(p.I, p.S_down) : check_KS_mx(p.I, p.S_down)) return st;
-    if (p.N < 0 || p.N > 0x7FFFFF00) return fail(ARCQ_BAD_SHAPE, "%s: N = %lld out of range", who, (long long)p.N);
     if (p.y_dtype != ARCQ_DTYPE_F16 && p.y_dtype != ARCQ_DTYPE_F32) return fail(ARCQ_INVALID_ARG, "y_dtype = %d", p.y_dtype);
     if (arcq_status st = check_pitch(who, "x", p.ldx, p.K)) return st;
     if (p.ldy < p.N) return fail(ARCQ_BAD_SHAPE, "ldy = %lld < N = %lld", (long long)p.ldy, (long long)p.N);
@@ -771,7 +771,7 @@ static arcq_status moe_entry(const char* who, int block, const MoeArgs& p, size_
     if (!aligned(p.perm, 16)) return fail(ARCQ_BAD_ALIGN, "%s: perm must be 16-byte aligned", who);
     if (!aligned(p.ids, 4) || !aligned(p.weights, 4) || !aligned(p.up_tensor_scales, 4) || !aligned(p.down_tensor_scales, 4) || !aligned(p.y, 4))
         return fail(ARCQ_BAD_ALIGN, "%s: ids, weights, tensor scales and y must be 4-byte aligned", who);
-    if (arcq_status st = check_workspace(who, moe_workspace_bytes(p.M, p.top, p.K, p.I, p.perm != nullptr), p.workspace, workspace_bytes)) return st;
+    if (arcq_status st = check_workspace(who, moe_workspace_bytes(p.M, p.top, p.E, p.K, p.I, p.N, p.perm != nullptr), p.workspace, workspace_bytes)) return st;
     return launch_moe(block, p);
 }
 

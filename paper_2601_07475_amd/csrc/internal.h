@@ -143,7 +143,7 @@ struct MoeArgs {
     void* workspace;
     hipStream_t stream;
 };
-size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t K, int64_t I, bool reorder);
+size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t E, int64_t K, int64_t I, int64_t N, bool reorder);
 arcq_status launch_moe(int block, const MoeArgs& p);
 // The router
 size_t moe_route_workspace_bytes(int64_t M, int64_t K, int64_t E);

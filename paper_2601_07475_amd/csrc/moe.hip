@@ -38,154 +38,98 @@ struct Experts {
     int rows;                                   // of an expert
 };
 
-// Which slots (token, choice) every expert has.
-struct Lists {
-    int start[kMostExperts + 1], count[kMostExperts];
-    int active[kMostExperts];                   // experts with slots, ascending
-    int slots[kMostSlots];
-    int actives;
+struct UpArgs {
+    const uint16_t* x;
+    int64_t ldx;
+    const int32_t* ids;
+    const float* weights;
+    int M, top, E, K, I, activation;
+    Experts up;
+    uint16_t *high, *low;                       // [M top, pitch]
+    int pitch;                                  // I in whole chunks, zeros behind
+    int tiles;                                  // of 16 columns
 };
 
-// All threads of the workgroup.  ids outside 0 .. E - 1: no expert.
-template <int THREADS>
-__device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E, Lists& l) {
-    const int tid = threadIdx.x, slots = M * top;
-    constexpr int PER = (kMostSlots + THREADS - 1) / THREADS;
-    int id[PER], at[PER];
-    for (int e = tid; e < E; e += THREADS) l.count[e] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-        const int t = tid + p * THREADS;
-        id[p] = -1;
-        if (t < slots) {
-            const int e = ids[t], first = t - t % top;
-            bool fresh = e >= 0 && e < E;
-            for (int u = first; u < t; ++u) fresh = fresh && ids[u] != e;       // (a later choice of the same expert counts with the first)
-            if (fresh) {
-                id[p] = e;
-                at[p] = atomicAdd(&l.count[e], 1);
-            }
-        }
-    }
-    __syncthreads();
-    if (tid < 64) {
-        int begin = 0, actives = 0;
-        for (int base = 0; base < E; base += 64) {
-            const int e = base + tid, n = e < E ? l.count[e] : 0;
-            int sum = n;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int other = __shfl_up(sum, d);
-                if (tid >= d) sum += other;
-            }
-            const uint64_t some = __ballot(n > 0);
-            if (e < E) l.start[e] = begin + sum - n;
-            if (n > 0) l.active[actives + __popcll(some & ((1ull << tid) - 1ull))] = e;
-            begin += __shfl(sum, 63);
-            actives += __popcll(some);
-        }
-        if (tid == 0) l.actives = actives;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int p = 0; p < PER; ++p)
-        if (id[p] >= 0) l.slots[l.start[id[p]] + at[p]] = tid + p * THREADS;
-    __syncthreads();
+template <typename OutT>
+struct DownArgs {
+    const uint16_t *high, *low;
+    const int32_t* ids;
+    int M, top, E, I, pitch, N;
+    Experts down;
+    const OutT* residual;
+    int64_t ldr;
+    OutT* y;
+    int64_t ldy;
+    float* partial;                             // [splits][M top, N]
+    int groups, splits;
+};
+
+// h of one slot and column.
+__device__ __forceinline__ void store_h(const UpArgs& a, int slot, int n, float g, float u, float weight) {
+    float v[1] = {g};
+    activate(v, a.activation);
+    const float h = v[0] * u * weight * (1.0f / kUnit);
+    const _Float16 high = (_Float16)h, low = (_Float16)((h - (float)high) * (1.0f / kLow));
+    const int64_t to = (int64_t)slot * a.pitch + n;
+    a.high[to] = __builtin_bit_cast(uint16_t, high);
+    a.low[to] = __builtin_bit_cast(uint16_t, low);
+    if (n >= a.I - 16)                          // whoever has the last tile clears what is left of the last chunk
+        for (int z = n + 16; z < a.pitch; z += 16) a.high[to + z - n] = a.low[to + z - n] = 0;
 }
 
-// A wave's product of up to 16 MT rows (fragments from `row`, where `valid`) with NT tiles of 16 weight rows (this lane's: wc, ws) over chunks c0 .. c1 - 1
-// of 128 k, the last of which may be the part behind the last whole one of K.
-template <int B, int MT, int NT>
-__device__ __forceinline__ void accumulate(const uint16_t* const (&row)[MT], const bool (&valid)[MT], const uint8_t* const (&wc)[NT], const uint8_t* const (&ws)[NT],
-                                           int K, int c0, int c1, float4v (&acc)[1][MT][NT]) {
-    constexpr int SB = 128 / B, G = MT == 1 ? 4 : MT == 2 ? 2 : 1;     // scale bytes of a chunk; chunks in flight
-    const int lane = threadIdx.x & 63, q = lane >> 4;
-    const int whole = min(c1, K >> 7);
-    for (int c = c0; c < whole; c += G) {
-        const int count = min(G, whole - c);
-        u32x2 sc[NT];
-        u32x4 cw[G][NT];
-        half8 xf[G][MT][4];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int64_t at = (int64_t)SB * (c + min(q, count - 1));
-            if constexpr (B == 16) {
-                const uint2 v = load8_a1(ws[t] + at);
-                sc[t] = u32x2{v.x, v.y};
-            } else {
-                sc[t] = u32x2{load4_a1(ws[t] + at), 0u};
-            }
-        }
-#pragma unroll
-        for (int d = 0; d < G; ++d)
-            if (d < count)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) cw[d][t] = *reinterpret_cast<const u32x4_a4*>(wc[t] + 64 * (int64_t)(c + d) + 16 * q);
-#pragma unroll
-        for (int r = 0; r < MT; ++r) {
-#pragma unroll
-            for (int d = 0; d < G; ++d)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) xf[d][r][j] = half8{0, 0, 0, 0, 0, 0, 0, 0};
-            if (valid[r]) {
-#pragma unroll
-                for (int d = 0; d < G; ++d)
-                    if (d < count)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) xf[d][r][j] = *reinterpret_cast<const half8*>(row[r] + 128 * (c + d) + 32 * j + 8 * q);
-            }
-        }
-        uint32_t sw[4][NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            uint32_t s[4];
-            scales_of_group<B>(make_uint2(sc[t][0], sc[t][1]), s);
-#pragma unroll
-            for (int d = 0; d < 4; ++d) sw[d][t] = s[d];
-        }
-#pragma unroll
-        for (int d = 0; d < G; ++d) {
-            if (d < count) {
-                uint4 words[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) words[t] = make_uint4(cw[d][t][0], cw[d][t][1], cw[d][t][2], cw[d][t][3]);
-                multiply_chunk<B, MT, NT, 1>(xf[d], words, sw[d], acc);
-            }
+// Chunks of 128 k of a tile of 16 rows of weights, the last of which may be a part.  Kernels ask for them some chunks ahead, every lane for every chunk alike
+// (a load that a branch may pass over makes the compiler wait for all of them), so what lies past the end of a row of K >= 128 is moved back into it:
+//   codes   MXFP4: block 4 c + q, or the last one; NVFP4: blocks 8 c + 2 q and the next, or the last two
+//   scales  the chunk's 4 or 8 bytes, or the last ones of the row
+// and whole() puts right on arrival what was moved.  Codes of blocks past the end are those of some block; rows are zero there.  Addresses are a
+// tile's, the same for all lanes, and a lane's offset, the same for all tiles and chunks.
+template <int B>
+struct Row {                                        // the lane's
+    static constexpr int SB = 128 / B;              // scale bytes of a chunk
+    uint32_t code, part, scale;                     // offsets of the codes of chunk 0 and of the part of a chunk, and of the scales
+    int blocks, last;                               // of a row; the part's chunk
+    bool odd;                                       // the lane's first block of the part is the row's last
+    __device__ Row(int row, int q, int K, int64_t code_pitch, int64_t scale_pitch) {
+        blocks = K / B;
+        last = K >> 7;
+        odd = 8 * last + 2 * q == blocks - 1;
+        code = (uint32_t)row * (uint32_t)code_pitch + 16u * q;
+        part = (uint32_t)row * (uint32_t)code_pitch + (uint32_t)(B == 16 ? 8 * min(8 * last + 2 * q, blocks - 2) : 16 * min(4 * last + q, blocks - 1));
+        scale = (uint32_t)row * (uint32_t)scale_pitch;
+    }
+    __device__ u32x4 codes(const uint8_t* tile, int c) const {
+        return *reinterpret_cast<const u32x4_a4*>(c == last ? tile + part : tile + 64 * c + code);
+    }
+    __device__ u32x2 scales(const uint8_t* tile, int c) const {
+        const uint8_t* at = tile + (scale + (uint32_t)min(SB * c, blocks - SB));
+        if constexpr (B == 16) {
+            const uint2 v = load8_a1(at);
+            return u32x2{v.x, v.y};
+        } else {
+            return u32x2{load4_a1(at), 0u};
         }
     }
-    if (c1 > whole && c0 < c1) {                        // less than a chunk: blocks past the end count as zero codes, rows are read from their start there
-        const int c = K >> 7, blocks = K / B, pieces = K >> 3;
-        const int b0 = B == 16 ? 8 * c + 2 * q : 4 * c + q;
-        uint4 words[NT];
-        uint32_t sw[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if constexpr (B == 16) {
-                const uint2 lo = load8_a8(wc[t] + 8 * (int64_t)min(b0, blocks - 1)), hi = load8_a8(wc[t] + 8 * (int64_t)min(b0 + 1, blocks - 1));
-                const bool ok0 = b0 < blocks, ok1 = b0 + 1 < blocks;
-                words[t] = make_uint4(ok0 ? lo.x : 0, ok0 ? lo.y : 0, ok1 ? hi.x : 0, ok1 ? hi.y : 0);
-            } else {
-                const uint4 v = load16_a4(wc[t] + 16 * (int64_t)min(b0, blocks - 1));
-                const bool ok = b0 < blocks;
-                words[t] = make_uint4(ok ? v.x : 0, ok ? v.y : 0, ok ? v.z : 0, ok ? v.w : 0);
-            }
-            sw[t] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sw[t] |= (uint32_t)ws[t][min(B == 16 ? 8 * c + 2 * j + (q >> 1) : 4 * c + j, blocks - 1)] << (8 * j);
-        }
-        half8 xf[MT][4];
-#pragma unroll
-        for (int r = 0; r < MT; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int piece = 16 * c + 4 * j + q;
-                xf[r][j] = half8{0, 0, 0, 0, 0, 0, 0, 0};
-                if (valid[r] && piece < pieces) xf[r][j] = *reinterpret_cast<const half8*>(row[r] + 8 * piece);
-            }
-        multiply_chunk<B, MT, NT, 1>(xf, words, sw, acc);
+    // the chunk's scale bytes in their places; of a whole chunk nothing changes
+    __device__ u32x2 whole(u32x2 s, int c) const {
+        const int off = 8 * max(SB * c - (blocks - SB), 0);
+        if constexpr (B == 32) return u32x2{s[0] >> off, 0u};
+        const uint64_t v = ((uint64_t)s[1] << 32 | s[0]) >> off;
+        return u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
     }
-}
+    // and its codes: NVFP4's last block may be the second of two that were read
+    __device__ uint4 whole(u32x4 v, int c) const {
+        if constexpr (B == 32) return make_uint4(v[0], v[1], v[2], v[3]);
+        const bool second = c == last && odd;
+        return make_uint4(second ? v[2] : v[0], second ? v[3] : v[1], v[2], v[3]);
+    }
+    // those of a chunk's bytes that go with the lane's words, one for each
+    __device__ static uint32_t of_lane(u32x2 s, int q) {
+        return B == 16 ? __builtin_amdgcn_perm(s[1], s[0], q < 2 ? 0x06040200u : 0x07050301u) : s[0];
+    }
+};
+// Where a tile starts whose first row is `row` of expert e (uniform).
+__device__ __forceinline__ const uint8_t* codes_of(const Experts& w, int e, int64_t row) { return w.codes + ((int64_t)e * w.rows + row) * w.code_pitch; }
+__device__ __forceinline__ const uint8_t* scales_of(const Experts& w, int e, int64_t row) { return w.scales + ((int64_t)e * w.rows + row) * w.scale_pitch; }
 
 template <int MT, int NT>
 __device__ __forceinline__ void clear(float4v (&acc)[1][MT][NT]) {
@@ -195,75 +139,473 @@ __device__ __forceinline__ void clear(float4v (&acc)[1][MT][NT]) {
         for (int t = 0; t < NT; ++t) acc[0][r][t] = float4v{0.f, 0.f, 0.f, 0.f};
 }
 
-struct UpArgs {
-    const uint16_t* x;
-    int64_t ldx;
-    const int32_t* ids;
-    const float* weights;
-    int M, top, E, K, I, activation;
-    Experts up;
-    uint16_t *high, *low;                       // [M top, I]
-    int tiles;
+// ---- a few tokens: up to 64 slots, which a wave holds in its lanes
+
+// The distinct experts of up to 64 slots, in the order in which they appear, in lanes 0 .. count - 1 of the result.  id: of the lane's slot, -1 for none.
+__device__ __forceinline__ int distinct(int id, int slots, int& count) {
+    const int lane = threadIdx.x & 63;
+    int found = -1, n = 0;
+    for (int u = 0; u < slots; ++u) {
+        const int e = __builtin_amdgcn_readlane(id, u);
+        const uint64_t same = __ballot(id == e);
+        if (e >= 0 && (int)__builtin_ctzll(same) == u) {
+            if (lane == n) found = e;
+            ++n;
+        }
+    }
+    count = n;
+    return found;
+}
+__device__ __forceinline__ int checked_id(const int32_t* ids, int t, int slots, int E) {
+    const int e = t < slots ? ids[t] : -1;
+    return e >= 0 && e < E ? e : -1;
+}
+
+// All tokens are rows of one tile, for every expert, so no list of an expert's tokens is needed: what comes out for one that does not choose it is passed over.
+// They lie in LDS, eight k of all tokens after the other.  A tile of 16 columns of an expert, that is 16 rows of G and of U, is for KW waves, which split K;
+// workgroups take one such tile for each of their 8 / KW teams after the other, and ask for the next one's weights while they multiply and add up this one's.
+// ROWS: places for tokens in LDS.
+template <int B, int KW, int ROWS>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) void up_few_kernel(UpArgs a) {
+    constexpr int TEAMS = 8 / KW, G = 4;            // chunks in flight
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float(&red)[2][8][2][4][64] = *reinterpret_cast<float(*)[2][8][2][4][64]>(lds);     // wave, G or U, element, lane
+    int* ids_of = reinterpret_cast<int*>(lds + sizeof(red));
+    float* weights_of = reinterpret_cast<float*>(lds + sizeof(red) + 256);
+    uint8_t* xs = lds + sizeof(red) + 512;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    const int kw = wave % KW, team = wave / KW, slots = a.M * a.top;
+    const int id = checked_id(a.ids, lane, slots, a.E);
+    const float weight_of = lane < slots ? a.weights[lane] : 0.0f;
+    const int chunks = (a.K + 127) >> 7, pieces = a.K >> 3;
+    for (int u = tid; u < 16 * chunks * a.M; u += 512) {                // (pieces past the end are zeros)
+        const int m = a.M == 1 ? 0 : u / (16 * chunks), p = u - m * 16 * chunks;
+        u32x4 v = {0, 0, 0, 0};
+        if (p < pieces) v = *reinterpret_cast<const u32x4*>(a.x + m * a.ldx + 8 * p);
+        *reinterpret_cast<u32x4*>(xs + 16 * (p * ROWS + m)) = v;
+    }
+    if (wave == 0) {
+        ids_of[lane] = id;
+        weights_of[lane] = weight_of;
+    }
+    int actives;
+    const int active = distinct(id, slots, actives);
+    const int all = actives * a.tiles, stride = (int)gridDim.x * TEAMS;
+    const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
+    const uint8_t* x_lane = xs + 16 * (q * ROWS + min(i, a.M - 1));
+    const int c0 = kw * chunks / KW, n = (kw + 1) * chunks / KW - c0, groups = (n + G - 1) / G;     // n >= 1
+    const uint8_t *wc[2], *ws[2];
+    auto take = [&](int item) {                     // the item whose weights are asked for next
+        const int nth = item / a.tiles, e = __builtin_amdgcn_readlane(active, nth);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {               // (I is a multiple of 16)
+            wc[t] = codes_of(a.up, e, t * a.I + 16 * (item - nth * a.tiles));
+            ws[t] = scales_of(a.up, e, t * a.I + 16 * (item - nth * a.tiles));
+        }
+    };
+    u32x4 cw[G][2];
+    u32x2 sc[2];
+    auto ask_scales = [&](int g) {                  // lane group q: of the q-th chunk of the group
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sc[t] = of.scales(ws[t], c0 + min(G * g + q, n - 1));
+    };
+    auto ask_codes = [&](int g, int d) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) cw[d][t] = of.codes(wc[t], c0 + min(G * g + d, n - 1));
+    };
+    int item = (int)blockIdx.x * TEAMS + team;
+    const int rounds = (all - (int)blockIdx.x * TEAMS + stride - 1) / stride;       // of the workgroup's first team: the others have as many, or one fewer
+    if (rounds <= 0) return;
+    take(min(item, all - 1));                       // (a team without work asks for the last item's)
+    ask_scales(0);
+#pragma unroll
+    for (int d = 0; d < G; ++d) ask_codes(0, d);
+    wait_lgkmcnt0();
+    wg_barrier();                                   // not __syncthreads(): the weights stay in flight
+    for (int round = 0; round < rounds; ++round, item += stride) {
+        float4v acc[1][1][2];
+        clear<1, 2>(acc);
+        for (int g = 0; g < groups; ++g) {
+            const bool over = g + 1 == groups;
+            const int count = min(G, n - G * g), next = over ? 0 : g + 1, c = c0 + G * g;
+            uint32_t sw[4][2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const u32x2 v = of.whole(sc[t], c0 + min(G * g + q, n - 1));
+                uint32_t s[4];
+                scales_of_group<B>(make_uint2(v[0], v[1]), s);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) sw[d][t] = s[d];
+            }
+            if (over) take(min(item + stride, all - 1));
+            ask_scales(next);
+#pragma unroll
+            for (int d = 0; d < G; ++d) {
+                if (d < count) {
+                    half8 xf[1][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(x_lane + 256 * ROWS * c + 16 * ROWS * (16 * d + 4 * j));
+                    uint4 words[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) words[t] = of.whole(cw[d][t], c + d);
+                    multiply_chunk<B, 1, 2, 1>(xf, words, sw[d], acc);
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (the next chunk's rows are not read from LDS before: registers)
+                ask_codes(next, d);
+            }
+        }
+        float(&part)[8][2][4][64] = red[round & 1];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[wave][t][k][lane] = acc[0][0][t][k];
+        wait_lgkmcnt0();
+        wg_barrier();
+        if (item < all) {
+            const int nth = item / a.tiles, e = __builtin_amdgcn_readlane(active, nth), n0 = 16 * (item - nth * a.tiles);
+            const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f;
+            for (int idx = kw * 64 + lane; idx < 16 * a.M; idx += 64 * KW) {
+                const int m = idx >> 4, at = 16 * (m >> 2) + (idx & 15), k = m & 3;
+                int slot = -1;
+                float weight = 0.0f;
+                for (int j = 0; j < a.top; ++j)
+                    if (ids_of[m * a.top + j] == e) {
+                        slot = slot < 0 ? m * a.top + j : slot;
+                        weight += weights_of[m * a.top + j];
+                    }
+                if (slot < 0) continue;
+                float g = 0.f, u = 0.f;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) g += part[team * KW + w][0][k][at], u += part[team * KW + w][1][k][at];
+                store_h(a, slot, n0 + (idx & 15), g * alpha, u * alpha, weight);
+            }
+        }
+    }
+}
+
+// Up to 8 tokens: 16 columns of y a workgroup.  The reduction runs over all chosen experts' channels one after the other, in equal shares for the waves; a wave
+// adds what it has of an expert to its own sums of all tokens, and the waves' sums are added in their order at the end.
+// Rows of h reach a wave's registers through a slice of LDS of its own, so that a chunk on its way takes TOKENS / 2 registers of 16 bytes and not four.
+template <int B, int TOKENS, int WAVES, int DEPTH, typename OutT>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4))) void down_few_kernel(DownArgs<OutT> a) {
+    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float(&sums)[WAVES][8][16] = *reinterpret_cast<float(*)[WAVES][8][16]>(lds);
+    int* ids_of = reinterpret_cast<int*>(lds + sizeof(sums));
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    uint8_t* slice = lds + sizeof(sums) + 256 + wave * TOKENS * 512;
+    const int slots = a.M * a.top, id = checked_id(a.ids, lane, slots, a.E);
+    if (wave == 0) ids_of[lane] = id;
+    for (int k = lane; k < 128; k += 64) (&sums[wave][0][0])[k] = 0.0f;
+    int actives;
+    const int active = distinct(id, slots, actives);
+    __syncthreads();
+    const int n0 = (int)blockIdx.x * 16;
+    const Row<B> of(min(i, a.N - 1 - n0), q, a.I, a.down.code_pitch, a.down.scale_pitch);
+    const int per = (a.I + 127) >> 7, all = actives * per;
+    const int s0 = (int)((int64_t)wave * all / WAVES), s1 = (int)((int64_t)(wave + 1) * all / WAVES);
+    auto slot_of = [&](int m, int e) {              // -1: token m does not choose it
+        int slot = -1;
+        if (m < a.M)
+            for (int j = a.top - 1; j >= 0; --j) slot = ids_of[m * a.top + j] == e ? m * a.top + j : slot;
+        return slot;
+    };
+    // pieces of a chunk: rows r = 2 token + (0: high, 1: low), four a load, 16 lanes a row
+    auto unit = [](int piece, int r) { return 16 * (2 * TOKENS * piece + (r ^ (piece & (2 * TOKENS - 1)))); };
+    const uint8_t *wc = nullptr, *ws = nullptr;
+    uint32_t row[LOADS];                            // offsets from a.high
+    const uint32_t low = (uint32_t)(a.low - a.high);
+    struct {
+        u32x4 codes, rows[LOADS];
+        u32x2 scales;
+    } ring[DEPTH];
+    int ask_nth = -1, ask_c = 0;                    // of the chunk asked for next
+    auto take = [&](int nth) {
+        ask_nth = nth;
+        const int e = __builtin_amdgcn_readlane(active, nth);
+        wc = codes_of(a.down, e, n0);
+        ws = scales_of(a.down, e, n0);
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+            const int r = 4 * l + q, slot = slot_of(r >> 1, e);         // (rows of a token that does not choose it are some slot's: passed over)
+            row[l] = ((r & 1) == 0 ? 0u : low) + (uint32_t)max(slot, 0) * (uint32_t)a.pitch;
+        }
+    };
+    auto ask = [&](int d) {
+        ring[d].scales = of.scales(ws, ask_c);
+        ring[d].codes = of.codes(wc, ask_c);
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) ring[d].rows[l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + 128u * (uint32_t)ask_c + 8u * (uint32_t)i));
+    };
+    auto advance = [&](int s) {                     // chunk s is asked for next; past the end: the last one again
+        if (s >= s1) return;
+        if (++ask_c == per) {
+            ask_c = 0;
+            take(ask_nth + 1);
+        }
+    };
+    float4v acc[1][1][1];
+    clear<1, 1>(acc);
+    if (s0 < s1) {
+        int nth = s0 / per, c = s0 - nth * per;     // of the chunk that is multiplied
+        take(nth);
+        ask_c = c;
+        float alpha = 0.0f;
+        bool chosen[4];                             // by tokens 4 (q & 1) + k
+        auto expert = [&]() {
+            const int e = __builtin_amdgcn_readlane(active, nth);
+            alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) chosen[k] = slot_of(4 * (q & 1) + k, e) >= 0;
+        };
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            ask(d);
+            advance(s0 + d + 1);
+        }
+        for (int s = s0; s < s1; s += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                if (s + d < s1) {
+#pragma unroll
+                    for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4*>(slice + unit(i, 4 * l + q)) = ring[d].rows[l];
+                    half8 xf[1][4];                 // (LDS operations of a wave complete in order)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(slice + unit(4 * j + q, 2 * (i & (TOKENS - 1)) + (i >> 3)));
+                    uint4 words[1] = {of.whole(ring[d].codes, c)};
+                    const uint32_t sw[1] = {of.of_lane(of.whole(ring[d].scales, c), q)};
+                    multiply_chunk<B, 1, 1, 1>(xf, words, sw, acc);
+                    if (c + 1 == per || s + d + 1 == s1) {
+                        expert();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            // lanes of the first half hold sums of high numbers, those of the second of low ones of the same rows
+                            const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][0][0][k]), __float_as_uint(acc[0][0][0][k]), false, false);
+                            const float sum = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
+                            if (lane < 32 && chosen[k]) sums[wave][4 * q + k][i] += sum * alpha;
+                        }
+                        clear<1, 1>(acc);
+                        ++nth;
+                        c = -1;
+                    }
+                    ++c;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                ask(d);
+                advance(s + d + DEPTH + 1);
+            }
+        }
+    }
+    __syncthreads();
+    for (int idx = tid; idx < a.M * 16; idx += THREADS) {
+        const int m = idx >> 4, n = n0 + (idx & 15);
+        if (n >= a.N) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += sums[w][m][idx & 15];
+        if (a.residual) sum += (float)a.residual[m * a.ldr + n];
+        store_out(a.y + m * a.ldy + n, sum);
+    }
+}
+
+// ---- more tokens: rows gathered by expert
+
+// Which slots (token, choice) every expert has.
+struct Lists {
+    uint16_t start[kMostExperts], count[kMostExperts];
+    uint16_t active[kMostExperts];              // experts with slots, ascending
+    uint16_t slots[kMostSlots];                 // by expert
+    int16_t id[kMostSlots];                     // by slot, -1 for none
+    uint32_t fill[kMostExperts];
+    int actives;
 };
 
-// A workgroup: 16 columns of one expert, that is 16 rows of G and of U, K split over the waves, tokens 32 (16) at a time.
-template <int B, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 4))) void up_kernel(UpArgs a) {
-    constexpr int THREADS = 64 * WAVES;
+// All threads of the workgroup.
+template <int THREADS>
+__device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E, Lists& l) {
+    const int tid = threadIdx.x, slots = M * top;
+    constexpr int PER = (kMostSlots + THREADS - 1) / THREADS;
+    int id[PER];
+    uint32_t at[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const int t = tid + p * THREADS;
+        id[p] = checked_id(ids, t, slots, E);
+        if (t < slots) l.id[t] = (int16_t)id[p];
+    }
+    for (int e = tid; e < E; e += THREADS) l.fill[e] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const int t = tid + p * THREADS;
+        for (int u = t - t % top; u < t && id[p] >= 0; ++u)
+            if (l.id[u] == id[p]) id[p] = -1;       // (a later choice of the same expert counts with the first)
+        if (id[p] >= 0) at[p] = atomicAdd(&l.fill[id[p]], 1u);
+    }
+    __syncthreads();
+    if (tid < 64) {
+        int begin = 0, actives = 0;
+        for (int base = 0; base < E; base += 64) {
+            const int e = base + tid, n = e < E ? (int)l.fill[e] : 0;
+            int sum = n;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(sum, d);
+                if (tid >= d) sum += other;
+            }
+            const uint64_t some = __ballot(n > 0);
+            if (e < E) {
+                l.start[e] = (uint16_t)(begin + sum - n);
+                l.count[e] = (uint16_t)n;
+            }
+            if (n > 0) l.active[actives + __popcll(some & ((1ull << tid) - 1ull))] = (uint16_t)e;
+            begin += __shfl(sum, 63);
+            actives += __popcll(some);
+        }
+        if (tid == 0) l.actives = actives;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+        if (id[p] >= 0) l.slots[l.start[id[p]] + at[p]] = (uint16_t)(tid + p * THREADS);
+    __syncthreads();
+}
+
+// Eight waves' products of the same 16 MT rows, chunks c0 .. c1 - 1, each wave with NT tiles of weights of its own (from wc, ws on).  Rows reach all
+// waves through LDS, a chunk at a time in two buffers; `from`: the row that this thread copies a piece of 8 k of (piece tid % 16, row tid / 16).
+// Loads of rows and of weights are DEPTH chunks ahead alike: they return in order.
+template <int MT>
+constexpr int kRowBytes = MT * 4096;                // of a buffer
+
+template <int B, int MT, int NT, int DEPTH>
+__device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>& of, const uint8_t* const (&wc)[NT], const uint8_t* const (&ws)[NT], int K, int c0, int c1,
+                                              uint8_t* lds, float4v (&acc)[1][MT][NT]) {
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
+    const int piece = tid & 15, copy_row = tid >> 4, pieces = K >> 3, blocks = of.blocks;
+    const bool copies = copy_row < 16 * MT;
+    auto unit = [](int p, int r) { return 16 * (256 * (r >> 4) + 16 * p + ((r & 15) ^ p)); };
+    const int to = unit(piece, copy_row);
+    if (c0 >= c1) return;
+    if (blocks < of.SB) {                         // less than one chunk: too short to be moved back into
+        if (copies) *reinterpret_cast<u32x4*>(lds + to) = piece < pieces ? *reinterpret_cast<const u32x4*>(from + 8 * piece) : u32x4{0, 0, 0, 0};
+        uint4 words[NT];
+        uint32_t sw[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            u32x4 v = {0, 0, 0, 0};
+            uint64_t s = 0;
+            if constexpr (B == 16) {
+                if (2 * q < blocks) {
+                    const uint2 w = load8_a8(wc[t] + of.code);
+                    v[0] = w.x, v[1] = w.y;
+                }
+                if (2 * q + 1 < blocks) {
+                    const uint2 w = load8_a8(wc[t] + of.code + 8);
+                    v[2] = w.x, v[3] = w.y;
+                }
+            } else {
+                if (q < blocks) v = *reinterpret_cast<const u32x4_a4*>(wc[t] + of.code);
+            }
+            for (int k = 0; k < blocks; ++k) s |= (uint64_t)ws[t][of.scale + k] << (8 * k);
+            words[t] = make_uint4(v[0], v[1], v[2], v[3]);
+            sw[t] = of.of_lane(u32x2{(uint32_t)s, (uint32_t)(s >> 32)}, q);
+        }
+        __syncthreads();
+        half8 xf[MT][4];
+#pragma unroll
+        for (int r = 0; r < MT; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
+        multiply_chunk<B, MT, NT, 1>(xf, words, sw, acc);
+        __syncthreads();
+        return;
+    }
+    struct {
+        u32x4 codes[NT], piece;
+        u32x2 scales[NT];
+    } ring[DEPTH];
+    auto ask = [&](int d, int at) {                 // (past the end: the last chunk again)
+        const int c = min(at, c1 - 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) ring[d].scales[t] = of.scales(ws[t], c);
+        ring[d].piece = *reinterpret_cast<const u32x4*>(from + 8 * min(16 * c + piece, pieces - 1));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) ring[d].codes[t] = of.codes(wc[t], c);
+    };
+    auto put = [&](int d, int c) {
+        const bool in = 16 * c + piece < pieces;
+        if (copies) *reinterpret_cast<u32x4*>(lds + (c & 1) * kRowBytes<MT> + to) = in ? ring[d].piece : u32x4{0, 0, 0, 0};
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) ask(d, c0 + d);
+    put(0, c0);
+    wait_lgkmcnt0();
+    wg_barrier();
+    for (int at = c0; at < c1; at += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int c = at + d;
+            if (c < c1) {
+                put((d + 1) % DEPTH, c + 1);        // (behind the last one: a buffer that nobody reads)
+                half8 xf[MT][4];
+#pragma unroll
+                for (int r = 0; r < MT; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + (c & 1) * kRowBytes<MT> + unit(4 * j + q, 16 * r + i));
+                uint4 words[NT];
+                uint32_t sw[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    words[t] = of.whole(ring[d].codes[t], c);
+                    sw[t] = of.of_lane(of.whole(ring[d].scales[t], c), q);
+                }
+                multiply_chunk<B, MT, NT, 1>(xf, words, sw, acc);
+                wait_lgkmcnt0();
+                wg_barrier();                       // not __syncthreads(): loads stay in flight
+            }
+            ask(d, c + DEPTH);
+        }
+    }
+}
+
+// 128 columns of an expert a workgroup, 16 rows of G and of U for each wave; its tokens 16 or 32 at a time.
+template <int B, int DEPTH>
+__global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
     __shared__ Lists l;
-    __shared__ float red[WAVES][2][2][4][64];       // row tile, G or U, element, lane
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15;
-    lists_of<THREADS>(a.ids, a.M, a.top, a.E, l);
-    const int nth = (int)(blockIdx.x / (uint32_t)a.tiles), n0 = 16 * (int)(blockIdx.x % (uint32_t)a.tiles);
+    __shared__ __attribute__((aligned(16))) uint8_t rows[2 * kRowBytes<2>];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    lists_of<512>(a.ids, a.M, a.top, a.E, l);
+    const int groups = (a.tiles + 7) >> 3, nth = (int)(blockIdx.x / (uint32_t)groups);
     if (nth >= l.actives) return;
+    const int tile = min(8 * (int)(blockIdx.x % (uint32_t)groups) + wave, a.tiles - 1), n = 16 * tile + i;      // (waves past the last tile repeat it)
+    const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
     const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
     const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f;
     const uint8_t *wc[2], *ws[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int64_t at = (int64_t)e * a.up.rows + t * a.I + n0 + i;   // (I is a multiple of 16)
-        wc[t] = a.up.codes + at * a.up.code_pitch;
-        ws[t] = a.up.scales + at * a.up.scale_pitch;
+        wc[t] = codes_of(a.up, e, t * a.I + 16 * tile);
+        ws[t] = scales_of(a.up, e, t * a.I + 16 * tile);
     }
-    const int chunks = (a.K + 127) >> 7, c0 = wave * chunks / WAVES, c1 = (wave + 1) * chunks / WAVES;
     auto tokens = [&](auto mt_tag, int r0) {
         constexpr int MT = decltype(mt_tag)::value;
-        const uint16_t* row[MT];
-        bool valid[MT];
-#pragma unroll
-        for (int r = 0; r < MT; ++r) {
-            valid[r] = r0 + 16 * r + i < count;
-            row[r] = a.x + (int64_t)(l.slots[first + min(r0 + 16 * r + i, count - 1)] / a.top) * a.ldx;
-        }
+        const int which = r0 + (tid >> 4);
+        const uint16_t* from = a.x + (int64_t)(l.slots[first + min(which, count - 1)] / a.top) * a.ldx;
         float4v acc[1][MT][2];
         clear<MT, 2>(acc);
-        accumulate<B, MT, 2>(row, valid, wc, ws, a.K, c0, c1, acc);
-        if (r0 > 0) __syncthreads();
+        multiply_rows<B, MT, 2, DEPTH>(from, of, wc, ws, a.K, 0, (a.K + 127) >> 7, rows, acc);
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) red[wave][r][t][k][lane] = acc[0][r][t][k];
-        __syncthreads();
-        for (int idx = tid; idx < MT * 256; idx += THREADS) {
-            const int r = idx >> 8, k = (idx >> 6) & 3, at = idx & 63, which = r0 + 16 * r + 4 * (at >> 4) + k;
-            if (which >= count) continue;
-            float g = 0.f, u = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) g += red[w][r][0][k][at], u += red[w][r][1][k][at];
-            float v[1] = {g * alpha};
-            activate(v, a.activation);
-            const int slot = l.slots[first + which];
-            float weight = a.weights[slot];
-            for (int s = slot + 1; s % a.top != 0; ++s)                  // the same expert again
-                if (a.ids[s] == e) weight += a.weights[s];
-            const float h = v[0] * (u * alpha) * weight * (1.0f / kUnit);
-            const _Float16 high = (_Float16)h, low = (_Float16)((h - (float)high) * (1.0f / kLow));
-            const int64_t to = (int64_t)slot * a.I + n0 + (at & 15);
-            a.high[to] = __builtin_bit_cast(uint16_t, high);
-            a.low[to] = __builtin_bit_cast(uint16_t, low);
-        }
+            for (int k = 0; k < 4; ++k) {
+                const int at = r0 + 16 * r + 4 * q + k;
+                if (at >= count) continue;
+                const int slot = l.slots[first + at];
+                float weight = a.weights[slot];
+                for (int s = slot + 1; s % a.top != 0; ++s)             // the same expert again
+                    if (l.id[s] == e) weight += a.weights[s];
+                store_h(a, slot, n, acc[0][r][0][k] * alpha, acc[0][r][1][k] * alpha, weight);
+            }
     };
     for (int r0 = 0; r0 < count; r0 += 32) {
         if (count - r0 <= 16) tokens(std::integral_constant<int, 1>{}, r0);
@@ -271,104 +613,118 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 4
     }
 }
 
-template <typename OutT>
-struct DownArgs {
-    const uint16_t *high, *low;
-    const int32_t* ids;
-    int M, top, E, I, N;
-    Experts down;
-    const OutT* residual;
-    int64_t ldr;
-    OutT* y;
-    int64_t ldy;
-};
-
-// A workgroup: 16 NT columns of y for all tokens.
-template <int B, int NT, int WAVES, typename OutT>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 4))) void down_kernel(DownArgs<OutT> a) {
-    constexpr int THREADS = 64 * WAVES, COLS = 16 * NT;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    Lists& l = *reinterpret_cast<Lists*>(lds);
-    float* sums = reinterpret_cast<float*>(lds + sizeof(Lists));        // [WAVES][M][COLS]
+// Results of every slot by itself, in fp32: 16 columns a wave of an expert, 128 a workgroup, over one of `splits` runs of I; its tokens 8, 16 or 32 at a time.
+template <int B, int DEPTH, typename OutT>
+__global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
+    __shared__ Lists l;
+    __shared__ __attribute__((aligned(16))) uint8_t rows[2 * kRowBytes<2>];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    for (int k = tid; k < WAVES * a.M * COLS; k += THREADS) sums[k] = 0.0f;
-    lists_of<THREADS>(a.ids, a.M, a.top, a.E, l);
-    float* own = sums + wave * a.M * COLS;
-    const int n0 = (int)blockIdx.x * COLS;
-    const int per = (a.I + 127) >> 7, all = __builtin_amdgcn_readfirstlane(l.actives) * per;
-    const int end = (int)((int64_t)(wave + 1) * all / WAVES);
-    for (int c = (int)((int64_t)wave * all / WAVES); c < end;) {
-        const int nth = c / per, c0 = c - nth * per, c1 = min(per, c0 + end - c);
-        c += c1 - c0;
-        const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
-        const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit;
-        const uint8_t *wc[NT], *ws[NT];
+    lists_of<512>(a.ids, a.M, a.top, a.E, l);
+    const uint32_t item = blockIdx.x / (uint32_t)a.groups;
+    const int nth = (int)(item / (uint32_t)a.splits), split = (int)(item % (uint32_t)a.splits);
+    if (nth >= l.actives) return;
+    const int n0 = 16 * (8 * (int)(blockIdx.x % (uint32_t)a.groups) + wave), n = min(n0, (a.N - 1) & ~15) + i;     // (waves past the last tile repeat it)
+    const Row<B> of(min(i, a.N - 1 - (n - i)), q, a.I, a.down.code_pitch, a.down.scale_pitch);
+    const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
+    const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit;
+    const uint8_t* const wc[1] = {codes_of(a.down, e, n - i)};
+    const uint8_t* const ws[1] = {scales_of(a.down, e, n - i)};
+    const int chunks = (a.I + 127) >> 7, c0 = split * chunks / a.splits, c1 = (split + 1) * chunks / a.splits;
+    float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
+    auto tokens = [&](auto mt_tag, int r0) {
+        constexpr int MT = decltype(mt_tag)::value;
+        const int copy = tid >> 4, which = r0 + 8 * (copy >> 4) + (copy & 7);
+        const uint16_t* from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[first + min(which, count - 1)] * a.pitch;
+        float4v acc[1][MT][1];
+        clear<MT, 1>(acc);
+        multiply_rows<B, MT, 1, DEPTH>(from, of, wc, ws, a.I, c0, c1, rows, acc);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int64_t at = (int64_t)e * a.down.rows + min(n0 + 16 * t + i, a.N - 1);
-            wc[t] = a.down.codes + at * a.down.code_pitch;
-            ws[t] = a.down.scales + at * a.down.scale_pitch;
-        }
-        auto tokens = [&](auto mt_tag, int r0) {
-            constexpr int MT = decltype(mt_tag)::value;
-            const uint16_t* row[MT];
-            bool valid[MT];
+        for (int r = 0; r < MT; ++r)
 #pragma unroll
-            for (int r = 0; r < MT; ++r) {
-                const int which = r0 + 8 * r + (i & 7);
-                valid[r] = which < count;
-                row[r] = (i < 8 ? a.high : a.low) + (int64_t)l.slots[first + min(which, count - 1)] * a.I;
+            for (int k = 0; k < 4; ++k) {
+                const int at = r0 + 8 * r + 4 * (q & 1) + k;
+                float* to = out + (int64_t)l.slots[first + min(at, count - 1)] * a.N;
+                const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][r][0][k]), __float_as_uint(acc[0][r][0][k]), false, false);
+                const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
+                if (lane < 32 && at < count && n < a.N) to[n] = v * alpha;
             }
-            float4v acc[1][MT][NT];
-            clear<MT, NT>(acc);
-            accumulate<B, MT, NT>(row, valid, wc, ws, a.I, c0, c1, acc);
-#pragma unroll
-            for (int r = 0; r < MT; ++r)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int which = r0 + 8 * r + 4 * (q & 1) + k;
-                    float* to = own + l.slots[first + min(which, count - 1)] / a.top * COLS + i;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        // lanes of the first half hold sums of high numbers, those of the second of low ones of the same rows
-                        const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][r][t][k]), __float_as_uint(acc[0][r][t][k]), false, false);
-                        const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
-                        if (lane < 32 && which < count) to[16 * t] += v * alpha;
-                    }
-                }
-        };
-        for (int r0 = 0; r0 < count; r0 += 32) {
-            if (count - r0 <= 8) tokens(std::integral_constant<int, 1>{}, r0);
-            else if (count - r0 <= 16) tokens(std::integral_constant<int, 2>{}, r0);
-            else tokens(std::integral_constant<int, 4>{}, r0);
-        }
-    }
-    __syncthreads();
-    for (int idx = tid; idx < a.M * COLS; idx += THREADS) {
-        const int m = idx / COLS, n = n0 + idx % COLS;
-        if (n >= a.N) continue;
-        float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum += sums[w * a.M * COLS + idx];
-        if (a.residual) sum += (float)a.residual[m * a.ldr + n];
-        store_out(a.y + m * a.ldy + n, sum);
+    };
+    for (int r0 = 0; r0 < count; r0 += 16) {
+        if (count - r0 <= 8) tokens(std::integral_constant<int, 1>{}, r0);
+        else tokens(std::integral_constant<int, 2>{}, r0);
     }
 }
 
+// y of a token: its slots' results, each over its runs, in their order, and the residual.
+template <typename OutT>
+__global__ __launch_bounds__(256) void join_kernel(DownArgs<OutT> a, uint32_t parts) {
+    const int m = (int)(blockIdx.x / parts), n = (int)(blockIdx.x % parts) * 256 + (int)threadIdx.x;
+    if (n >= a.N) return;
+    float sum = 0.0f;
+    for (int j = 0; j < a.top; ++j) {
+        const int slot = m * a.top + j, e = a.ids[slot];
+        bool counts = e >= 0 && e < a.E;
+        for (int u = 0; u < j; ++u) counts = counts && a.ids[m * a.top + u] != e;       // (a later choice of the same expert counts with the first)
+        if (!counts) continue;
+        for (int s = 0; s < a.splits; ++s) sum += a.partial[((int64_t)s * a.M * a.top + slot) * a.N + n];
+    }
+    if (a.residual) sum += (float)a.residual[m * a.ldr + n];
+    store_out(a.y + m * a.ldy + n, sum);
+}
+
+// Whether a launch's tokens go as rows of one tile.
+constexpr int64_t kUpRows = 80 << 10;               // LDS of a workgroup of up_few_kernel, two on a compute unit
+int64_t up_row_bytes(int64_t M, int64_t K) { return (M == 1 ? 1 : M <= 4 ? 4 : 16) * ((K + 127) / 128) * 256; }
+bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 64 && K >= 256 && up_row_bytes(M, K) <= kUpRows - 33 * 1024; }
+bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
+
+// Runs of I for down_many_kernel.
+int down_splits(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
+    const int64_t groups = (N + 127) / 128 * std::min<int64_t>(E, M * top), chunks = (I + 127) / 128;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(groups, 1), chunks / 8, 8}));
+}
+
+int64_t pitch_of(int64_t I) { return (I + 127) / 128 * 128; }
+
 // Bytes of a launch's parts of the workspace.
 struct MoeWorkspace {
-    size_t reordered, half;                     // rows in the weights' order; one of the two numbers of h
+    size_t reordered, half, partial;            // rows in the weights' order; one of the two numbers of h; slots' results
 };
-MoeWorkspace workspace_of(int64_t M, int64_t top, int64_t K, int64_t I, bool reorder) {
+MoeWorkspace workspace_of(int64_t M, int64_t top, int64_t K, int64_t I, int64_t N, int64_t E, bool reorder) {
     auto whole = [](int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; };
-    return {reorder ? whole(M * K * 2) : 0, whole(M * top * I * 2)};
+    return {reorder ? whole(M * K * 2) : 0, whole(M * top * pitch_of(I) * 2), down_few(M, top, I) ? 0 : whole((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4)};
+}
+
+template <int B, int KW, int ROWS>
+arcq_status launch_up_rows(const UpArgs& u, int64_t items, int cus, hipStream_t stream) {
+    auto kern = up_few_kernel<B, KW, ROWS>;
+    static std::atomic<uint64_t> lds_raised{0};
+    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+    const int64_t teams = 8 / KW;
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>((items + teams - 1) / teams, 2 * cus)), dim3(512), 2 * 16384 + 512 + (size_t)up_row_bytes(u.M, u.K), stream, u);
+    return check_launch("up_few_kernel");
+}
+template <int B, int KW>
+arcq_status launch_up_few(const UpArgs& u, int64_t items, int cus, hipStream_t stream) {
+    return u.M == 1 ? launch_up_rows<B, KW, 1>(u, items, cus, stream) : u.M <= 4 ? launch_up_rows<B, KW, 4>(u, items, cus, stream) : launch_up_rows<B, KW, 16>(u, items, cus, stream);
+}
+
+template <int B, int TOKENS, int DEPTH, typename OutT>
+arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
+    constexpr int WAVES = 16;
+    auto kern = down_few_kernel<B, TOKENS, WAVES, DEPTH, OutT>;
+    static std::atomic<uint64_t> lds_raised{0};
+    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256, stream, d);
+    return check_launch("down_few_kernel");
 }
 
 template <int B, typename OutT>
 arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
-    const MoeWorkspace w = workspace_of(std::min<int64_t>(p.M, kMostTokens), p.top, p.K, p.I, p.perm != nullptr);
+    const MoeWorkspace w = workspace_of(std::min<int64_t>(p.M, kMostTokens), p.top, p.K, p.I, p.N, p.E, p.perm != nullptr);
     uint8_t* at = static_cast<uint8_t*>(p.workspace);
     uint16_t *reordered = reinterpret_cast<uint16_t*>(at), *high = reinterpret_cast<uint16_t*>(at + w.reordered), *low = reinterpret_cast<uint16_t*>(at + w.reordered + w.half);
+    float* partial = reinterpret_cast<float*>(at + w.reordered + 2 * w.half);
     const uint16_t* x = static_cast<const uint16_t*>(p.x) + m0 * p.ldx;
     int64_t ldx = p.ldx;
     if (p.perm) {
@@ -380,24 +736,38 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     const int tiles = (int)(p.I / 16);
     const Experts up = {p.up_codes, p.up_scales, p.up_tensor_scales, (p.K + p.S_up) / 2, (p.K + p.S_up) / B, (int)(2 * p.I)};
     const Experts down = {p.down_codes, p.down_scales, p.down_tensor_scales, (p.I + p.S_down) / 2, (p.I + p.S_down) / B, (int)p.N};
-    const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, high, low, tiles};
-    hipLaunchKernelGGL((up_kernel<B, 8>), dim3((unsigned)(most * tiles)), dim3(512), 0, p.stream, u);
-    if (arcq_status st = check_launch("up_kernel")) return st;
-    const DownArgs<OutT> d = {high, low, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
-                              static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy};
-    constexpr int NT = 1, WAVES = 8;
-    auto kern = down_kernel<B, NT, WAVES, OutT>;
-    static std::atomic<uint64_t> lds_raised{0};
-    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((p.N + 16 * NT - 1) / (16 * NT))), dim3(64 * WAVES), sizeof(Lists) + (size_t)(WAVES * M * 16 * NT * 4), p.stream, d);
-    return check_launch("down_kernel");
+    const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, high, low, (int)pitch_of(p.I), tiles};
+    const int cus = num_cu();
+    if (up_few(M, p.top, p.K)) {
+        const int64_t items = most * tiles;
+        const int chunks = (int)((p.K + 127) / 128);
+        int kw = 2;
+        while (kw < 8 && items * kw < 16 * cus && chunks >= 4 * kw) kw *= 2;
+        const arcq_status st = kw == 2   ? launch_up_few<B, 2>(u, items, cus, p.stream)
+                               : kw == 4 ? launch_up_few<B, 4>(u, items, cus, p.stream)
+                                         : launch_up_few<B, 8>(u, items, cus, p.stream);
+        if (st) return st;
+    } else {
+        hipLaunchKernelGGL((up_many_kernel<B, 4>), dim3((unsigned)(most * ((tiles + 7) / 8))), dim3(512), 0, p.stream, u);
+        if (arcq_status st = check_launch("up_many_kernel")) return st;
+    }
+    DownArgs<OutT> d = {high, low, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
+                        static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 127) / 128), 1};
+    if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2, 4>(d, p.stream) : M <= 4 ? launch_down_few<B, 4, 4>(d, p.stream) : launch_down_few<B, 8, 2>(d, p.stream);
+    // (a last launch of fewer tokens has the runs of the first: there is room for those)
+    d.splits = down_splits(std::min<int64_t>(p.M, kMostTokens), p.top, p.E, p.I, p.N);
+    hipLaunchKernelGGL((down_many_kernel<B, 4, OutT>), dim3((unsigned)(most * d.splits * d.groups)), dim3(512), 0, p.stream, d);
+    if (arcq_status st = check_launch("down_many_kernel")) return st;
+    const unsigned parts = (unsigned)((p.N + 255) / 256);
+    hipLaunchKernelGGL((join_kernel<OutT>), dim3(parts * (unsigned)M), dim3(256), 0, p.stream, d, parts);
+    return check_launch("join_kernel");
 }
 
 }  // namespace
 
-size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t K, int64_t I, bool reorder) {
-    const MoeWorkspace w = workspace_of(std::min<int64_t>(M, kMostTokens), top, K, I, reorder);
-    return w.reordered + 2 * w.half;
+size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t E, int64_t K, int64_t I, int64_t N, bool reorder) {
+    const MoeWorkspace w = workspace_of(std::min<int64_t>(M, kMostTokens), top, K, I, N, E, reorder);
+    return w.reordered + 2 * w.half + w.partial;
 }
 
 // Tokens go kMostTokens at a time.

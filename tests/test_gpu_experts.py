@@ -149,7 +149,7 @@ def check(fmt, M, K, I, N, E, top, S=0, S2=0, act="silu", residual=False, reorde
     if residual:
         res = y if in_place else output(M, N, dtype, 1)[1]
         res.copy_(dev(r))
-    need = B.arcq_moe_workspace_size(M, ids.shape[1], K, I, reorder)
+    need = B.arcq_moe_workspace_size(M, ids.shape[1], E, K, I, N, reorder)
     buf = torch.full((need + 512,), 0xFF, dtype=torch.uint8, device="cuda")
     call(fmt, strided(x, 8 * (M % 3)), None if perm is None else dev(perm), ids, w, up, down, activation=ACT[act], residual=res, y=y, workspace=buf[:need])
     torch.cuda.synchronize()
@@ -332,7 +332,7 @@ def test_whole_layer(fmt):
     xd, rd, pd = dev(x), dev(router), dev(perm)
     ids, w = torch.empty((M, top), dtype=torch.int32, device="cuda"), torch.empty((M, top), device="cuda")
     h = dev(hidden)
-    scratch = torch.empty(B.arcq_moe_workspace_size(M, top, K, I, True) + B.arcq_moe_route_workspace_size(M, K, E) + 256, dtype=torch.uint8, device="cuda")
+    scratch = torch.empty(B.arcq_moe_workspace_size(M, top, E, K, I, K, True) + B.arcq_moe_route_workspace_size(M, K, E) + 256, dtype=torch.uint8, device="cuda")
     parts = (up[0], up[1], up[2], down[0], down[1], down[2]) if fmt == "nvfp4" else (up[0], up[1], down[0], down[1])
 
     def eager():

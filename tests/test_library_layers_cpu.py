@@ -98,7 +98,7 @@ def test_router_argument_errors():
 def test_experts_argument_errors(call, block):
     assert call(K=block // 2) == call(K=BIG, ldx=BIG) == call(K=0) == call(S=block // 2) == call(S=96) == call(S=-block) == B.BAD_SHAPE
     assert call(I=0) == call(I=block // 2) == call(I=BIG) == call(S2=block // 2) == call(S2=96) == B.BAD_SHAPE
-    assert call(M=-1) == call(M=1 << 31) == call(N=-1) == call(N=1 << 31) == B.BAD_SHAPE
+    assert call(M=-1) == call(M=1 << 31) == call(N=-1) == call(N=1 << 25) == B.BAD_SHAPE
     assert call(E=0) == call(E=B.MOE_MAX_EXPERTS + 1) == call(top=0) == call(top=B.MOE_MAX_TOP_K + 1) == B.BAD_SHAPE
     assert call(ldx=56) == B.BAD_SHAPE
     nulls = ["x", "ids", "w", "uc", "us", "dc", "ds", "y"] + (["ut", "dt_"] if block == 16 else [])
@@ -107,19 +107,20 @@ def test_experts_argument_errors(call, block):
     offs = {"x": OFF8, "ldx": 68, "uc": OFF4, "dc": OFF4, "perm": OFF8, "ids": OFF2, "w": OFF2, "y": OFF2} | ({"ut": OFF2, "dt_": OFF1} if block == 16 else {})
     for name, off in offs.items():
         assert call(**{name: off}) == B.BAD_ALIGN, name
-    need = B.arcq_moe_workspace_size(3, 2, 64, 64, False)
+    need = B.arcq_moe_workspace_size(3, 2, 8, 64, 64, 8, False)
     assert need >= 2 * 3 * 2 * 64 * 2
     assert call(wsb=need - 1) == call(ws=None) == B.WORKSPACE_TOO_SMALL and "workspace" in last()
     assert call(ws=OFF16) == B.BAD_ALIGN
-    more = B.arcq_moe_workspace_size(3, 2, 64, 64, True)
+    more = B.arcq_moe_workspace_size(3, 2, 8, 64, 64, 8, True)
     assert more > need and call(perm=FAKE, wsb=need) == B.WORKSPACE_TOO_SMALL
 
 
 def test_experts_workspace():
     size = B.arcq_moe_workspace_size
-    assert size(0, 2, 64, 64, True) == 0
-    assert size(10 ** 6, 8, 4096, 14336, True) == size(64, 8, 4096, 14336, True) <= 64 << 20       # tokens go so many at a time
+    assert size(0, 2, 8, 64, 64, 64, True) == size(2, 2, 8, 64, 64, 0, True) == 0
+    assert size(10 ** 6, 8, 32, 4096, 14336, 4096, True) == size(64, 8, 32, 4096, 14336, 4096, True) <= 64 << 20      # tokens go so many at a time
     n = ctypes.c_size_t(9)
     raw = B.lib().arcq_moe_workspace_size
-    assert raw(4, 0, 64, 64, 0, ctypes.byref(n)) == raw(4, 17, 64, 64, 0, ctypes.byref(n)) == raw(-1, 2, 64, 64, 0, ctypes.byref(n)) == B.BAD_SHAPE
-    assert raw(4, 2, 40, 64, 0, ctypes.byref(n)) == raw(4, 2, 64, 8, 0, ctypes.byref(n)) == B.BAD_SHAPE and raw(4, 2, 64, 64, 0, None) == B.INVALID_ARG
+    for bad in ((4, 0, 8, 64, 64, 8), (4, 17, 32, 64, 64, 8), (-1, 2, 8, 64, 64, 8), (4, 2, 0, 64, 64, 8), (4, 2, 8, 40, 64, 8), (4, 2, 8, 64, 8, 8), (4, 2, 8, 64, 64, -1)):
+        assert raw(*bad, 0, ctypes.byref(n)) == B.BAD_SHAPE, bad
+    assert raw(4, 2, 8, 64, 64, 8, 0, None) == B.INVALID_ARG
