@@ -132,26 +132,23 @@ __device__ __forceinline__ const uint8_t* codes_of(const Experts& w, int e, int6
 __device__ __forceinline__ const uint8_t* scales_of(const Experts& w, int e, int64_t row) { return w.scales + ((int64_t)e * w.rows + row) * w.scale_pitch; }
 
 template <int MT, int NT>
-__device__ __forceinline__ void clear(float4v (&acc)[1][MT][NT]) {
+__device__ __forceinline__ void clear(float4v (&acc)[MT][NT]) {
 #pragma unroll
     for (int r = 0; r < MT; ++r)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[0][r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NT; ++t) acc[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
 }
 
 // ---- a few tokens: up to 64 slots, which a wave holds in its lanes
 
 // The distinct experts of up to 64 slots, in the order in which they appear, in lanes 0 .. count - 1 of the result.  id: of the lane's slot, -1 for none.
-__device__ __forceinline__ int distinct(int id, int slots, int& count) {
+__device__ __forceinline__ int distinct(int id, int& count) {
     const int lane = threadIdx.x & 63;
     int found = -1, n = 0;
-    for (int u = 0; u < slots; ++u) {
-        const int e = __builtin_amdgcn_readlane(id, u);
-        const uint64_t same = __ballot(id == e);
-        if (e >= 0 && (int)__builtin_ctzll(same) == u) {
-            if (lane == n) found = e;
-            ++n;
-        }
+    for (uint64_t left = __ballot(id >= 0); left != 0; ++n) {
+        const int e = __builtin_amdgcn_readlane(id, (int)__builtin_ctzll(left));
+        left &= ~__ballot(id == e);
+        if (lane == n) found = e;
     }
     count = n;
     return found;
@@ -189,7 +186,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
         weights_of[lane] = weight_of;
     }
     int actives;
-    const int active = distinct(id, slots, actives);
+    const int active = distinct(id, actives);
     const int all = actives * a.tiles, stride = (int)gridDim.x * TEAMS;
     const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
     const uint8_t* x_lane = xs + 16 * (q * ROWS + min(i, a.M - 1));
@@ -223,7 +220,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
     wait_lgkmcnt0();
     wg_barrier();                                   // not __syncthreads(): the weights stay in flight
     for (int round = 0; round < rounds; ++round, item += stride) {
-        float4v acc[1][1][2];
+        float4v acc[1][2];
         clear<1, 2>(acc);
         for (int g = 0; g < groups; ++g) {
             const bool over = g + 1 == groups;
@@ -248,7 +245,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
                     uint4 words[2];
 #pragma unroll
                     for (int t = 0; t < 2; ++t) words[t] = of.whole(cw[d][t], c + d);
-                    multiply_chunk<B, 1, 2, 1>(xf, words, sw[d], acc);
+                    multiply_folded<B, 1, 2>(xf, words, sw[d], acc);
                 }
                 __builtin_amdgcn_sched_barrier(0);  // (the next chunk's rows are not read from LDS before: registers)
                 ask_codes(next, d);
@@ -258,12 +255,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) part[wave][t][k][lane] = acc[0][0][t][k];
+            for (int k = 0; k < 4; ++k) part[wave][t][k][lane] = acc[0][t][k];
         wait_lgkmcnt0();
         wg_barrier();
         if (item < all) {
             const int nth = item / a.tiles, e = __builtin_amdgcn_readlane(active, nth), n0 = 16 * (item - nth * a.tiles);
-            const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f;
+            const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
             for (int idx = kw * 64 + lane; idx < 16 * a.M; idx += 64 * KW) {
                 const int m = idx >> 4, at = 16 * (m >> 2) + (idx & 15), k = m & 3;
                 int slot = -1;
@@ -283,117 +280,105 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
     }
 }
 
-// Up to 8 tokens: 16 columns of y a workgroup.  The reduction runs over all chosen experts' channels one after the other, in equal shares for the waves; a wave
-// adds what it has of an expert to its own sums of all tokens, and the waves' sums are added in their order at the end.
+// Up to 8 tokens: 16 columns of y a workgroup.  The reduction runs over all chosen experts' channels one after the other, in equal shares for the waves, G
+// chunks at a time; a wave adds what it has of an expert to its own sums of all tokens, and the waves' sums are added in their order at the end.
 // Rows of h reach a wave's registers through a slice of LDS of its own, so that a chunk on its way takes TOKENS / 2 registers of 16 bytes and not four.
-template <int B, int TOKENS, int WAVES, int DEPTH, typename OutT>
+template <int B, int TOKENS, int WAVES, typename OutT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4))) void down_few_kernel(DownArgs<OutT> a) {
-    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2;
+    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2, G = TOKENS == 8 ? 3 : 4;      // (as registers allow)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     float(&sums)[WAVES][8][16] = *reinterpret_cast<float(*)[WAVES][8][16]>(lds);
     int* ids_of = reinterpret_cast<int*>(lds + sizeof(sums));
+    int8_t(&slot_of)[64][8] = *reinterpret_cast<int8_t(*)[64][8]>(lds + sizeof(sums) + 256);       // of an active expert and a token; -1: it does not choose it
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    uint8_t* slice = lds + sizeof(sums) + 256 + wave * TOKENS * 512;
+    uint8_t* slice = lds + sizeof(sums) + 256 + 512 + wave * TOKENS * 512;
     const int slots = a.M * a.top, id = checked_id(a.ids, lane, slots, a.E);
     if (wave == 0) ids_of[lane] = id;
     for (int k = lane; k < 128; k += 64) (&sums[wave][0][0])[k] = 0.0f;
     int actives;
-    const int active = distinct(id, slots, actives);
+    const int active = distinct(id, actives);
     __syncthreads();
-    const int n0 = (int)blockIdx.x * 16;
-    const Row<B> of(min(i, a.N - 1 - n0), q, a.I, a.down.code_pitch, a.down.scale_pitch);
-    const int per = (a.I + 127) >> 7, all = actives * per;
-    const int s0 = (int)((int64_t)wave * all / WAVES), s1 = (int)((int64_t)(wave + 1) * all / WAVES);
-    auto slot_of = [&](int m, int e) {              // -1: token m does not choose it
+    for (int k0 = 64 * wave; k0 < 8 * actives; k0 += THREADS) {
+        const int nth = (k0 + lane) >> 3, m = lane & 7, e = __shfl(active, nth & 63);       // (every lane takes part)
         int slot = -1;
         if (m < a.M)
             for (int j = a.top - 1; j >= 0; --j) slot = ids_of[m * a.top + j] == e ? m * a.top + j : slot;
-        return slot;
-    };
+        if (nth < actives) slot_of[nth][m] = (int8_t)slot;
+    }
+    __syncthreads();
+    const int n0 = (int)blockIdx.x * 16;
+    const Row<B> of(min(i, a.N - 1 - n0), q, a.I, a.down.code_pitch, a.down.scale_pitch);
+    const int per = (a.I + 127) >> 7, groups = (per + G - 1) / G, all = actives * groups;
+    const int s0 = wave * all / WAVES, s1 = (wave + 1) * all / WAVES;
     // pieces of a chunk: rows r = 2 token + (0: high, 1: low), four a load, 16 lanes a row
     auto unit = [](int piece, int r) { return 16 * (2 * TOKENS * piece + (r ^ (piece & (2 * TOKENS - 1)))); };
     const uint8_t *wc = nullptr, *ws = nullptr;
     uint32_t row[LOADS];                            // offsets from a.high
     const uint32_t low = (uint32_t)(a.low - a.high);
-    struct {
-        u32x4 codes, rows[LOADS];
-        u32x2 scales;
-    } ring[DEPTH];
-    int ask_nth = -1, ask_c = 0;                    // of the chunk asked for next
-    auto take = [&](int nth) {
-        ask_nth = nth;
+    auto take = [&](int nth) {                      // the expert whose weights are asked for next
         const int e = __builtin_amdgcn_readlane(active, nth);
         wc = codes_of(a.down, e, n0);
         ws = scales_of(a.down, e, n0);
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) {
-            const int r = 4 * l + q, slot = slot_of(r >> 1, e);         // (rows of a token that does not choose it are some slot's: passed over)
-            row[l] = ((r & 1) == 0 ? 0u : low) + (uint32_t)max(slot, 0) * (uint32_t)a.pitch;
+        for (int l = 0; l < LOADS; ++l) {           // (rows of a token that does not choose it are some slot's: passed over)
+            const int r = 4 * l + q, slot = slot_of[nth][r >> 1];
+            row[l] = ((r & 1) == 0 ? 0u : low) + (uint32_t)max(slot, 0) * (uint32_t)a.pitch + 8u * i;
         }
     };
-    auto ask = [&](int d) {
-        ring[d].scales = of.scales(ws, ask_c);
-        ring[d].codes = of.codes(wc, ask_c);
+    u32x4 cw[G], rows[G][LOADS];
+    u32x2 sc;
+    auto ask_scales = [&](int g) { sc = of.scales(ws, min(G * g + q, per - 1)); };
+    auto ask_chunk = [&](int g, int d) {
+        const int c = min(G * g + d, per - 1);
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) ring[d].rows[l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + 128u * (uint32_t)ask_c + 8u * (uint32_t)i));
+        for (int l = 0; l < LOADS; ++l) rows[d][l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + 128u * (uint32_t)c));
+        cw[d] = of.codes(wc, c);
     };
-    auto advance = [&](int s) {                     // chunk s is asked for next; past the end: the last one again
-        if (s >= s1) return;
-        if (++ask_c == per) {
-            ask_c = 0;
-            take(ask_nth + 1);
-        }
-    };
-    float4v acc[1][1][1];
-    clear<1, 1>(acc);
     if (s0 < s1) {
-        int nth = s0 / per, c = s0 - nth * per;     // of the chunk that is multiplied
+        int nth = s0 / groups, g = s0 - nth * groups;
         take(nth);
-        ask_c = c;
-        float alpha = 0.0f;
-        bool chosen[4];                             // by tokens 4 (q & 1) + k
-        auto expert = [&]() {
-            const int e = __builtin_amdgcn_readlane(active, nth);
-            alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit;
+        ask_scales(g);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) chosen[k] = slot_of(4 * (q & 1) + k, e) >= 0;
-        };
+        for (int d = 0; d < G; ++d) ask_chunk(g, d);
+        float4v acc[1][1];
+        clear<1, 1>(acc);
+        for (int s = s0; s < s1; ++s) {
+            const int count = min(G, per - G * g);
+            const bool over = g + 1 == groups, end = s + 1 == s1;
+            const int next = end ? g : over ? 0 : g + 1;        // (behind the last one: itself again)
+            const u32x2 v = of.whole(sc, min(G * g + q, per - 1));
+            uint32_t sw[4];
+            scales_of_group<B>(make_uint2(v[0], v[1]), sw);
+            if (over && !end) take(nth + 1);
+            ask_scales(next);
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            ask(d);
-            advance(s0 + d + 1);
-        }
-        for (int s = s0; s < s1; s += DEPTH) {
+            for (int d = 0; d < G; ++d) {
+                if (d < count) {
 #pragma unroll
-            for (int d = 0; d < DEPTH; ++d) {
-                if (s + d < s1) {
-#pragma unroll
-                    for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4*>(slice + unit(i, 4 * l + q)) = ring[d].rows[l];
+                    for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4*>(slice + unit(i, 4 * l + q)) = rows[d][l];
                     half8 xf[1][4];                 // (LDS operations of a wave complete in order)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(slice + unit(4 * j + q, 2 * (i & (TOKENS - 1)) + (i >> 3)));
-                    uint4 words[1] = {of.whole(ring[d].codes, c)};
-                    const uint32_t sw[1] = {of.of_lane(of.whole(ring[d].scales, c), q)};
-                    multiply_chunk<B, 1, 1, 1>(xf, words, sw, acc);
-                    if (c + 1 == per || s + d + 1 == s1) {
-                        expert();
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            // lanes of the first half hold sums of high numbers, those of the second of low ones of the same rows
-                            const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][0][0][k]), __float_as_uint(acc[0][0][0][k]), false, false);
-                            const float sum = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
-                            if (lane < 32 && chosen[k]) sums[wave][4 * q + k][i] += sum * alpha;
-                        }
-                        clear<1, 1>(acc);
-                        ++nth;
-                        c = -1;
-                    }
-                    ++c;
+                    uint4 words[1] = {of.whole(cw[d], G * g + d)};
+                    const uint32_t one[1] = {sw[d]};
+                    multiply_folded<B, 1, 1>(xf, words, one, acc);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                ask(d);
-                advance(s + d + DEPTH + 1);
+                ask_chunk(next, d);
             }
+            if (over || end) {
+                const float alpha = B == 16 ? a.down.tensor_scales[__builtin_amdgcn_readlane(active, nth)] * kUnit : kUnit / kFolded<B>;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    // lanes of the first half hold sums of high numbers, those of the second of low ones of the same rows
+                    const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][0][k]), __float_as_uint(acc[0][0][k]), false, false);
+                    const float sum = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
+                    if (lane < 32 && slot_of[nth][4 * q + k] >= 0) sums[wave][4 * q + k][i] += sum * alpha;
+                }
+                clear<1, 1>(acc);
+                ++nth;
+            }
+            g = next;
         }
     }
     __syncthreads();
@@ -479,7 +464,7 @@ constexpr int kRowBytes = MT * 4096;                // of a buffer
 
 template <int B, int MT, int NT, int DEPTH>
 __device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>& of, const uint8_t* const (&wc)[NT], const uint8_t* const (&ws)[NT], int K, int c0, int c1,
-                                              uint8_t* lds, float4v (&acc)[1][MT][NT]) {
+                                              uint8_t* lds, float4v (&acc)[MT][NT]) {
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
     const int piece = tid & 15, copy_row = tid >> 4, pieces = K >> 3, blocks = of.blocks;
     const bool copies = copy_row < 16 * MT;
@@ -516,7 +501,7 @@ __device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>
         for (int r = 0; r < MT; ++r)
 #pragma unroll
             for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
-        multiply_chunk<B, MT, NT, 1>(xf, words, sw, acc);
+        multiply_folded<B, MT, NT>(xf, words, sw, acc);
         __syncthreads();
         return;
     }
@@ -559,7 +544,7 @@ __device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>
                     words[t] = of.whole(ring[d].codes[t], c);
                     sw[t] = of.of_lane(of.whole(ring[d].scales[t], c), q);
                 }
-                multiply_chunk<B, MT, NT, 1>(xf, words, sw, acc);
+                multiply_folded<B, MT, NT>(xf, words, sw, acc);
                 wait_lgkmcnt0();
                 wg_barrier();                       // not __syncthreads(): loads stay in flight
             }
@@ -580,7 +565,7 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
     const int tile = min(8 * (int)(blockIdx.x % (uint32_t)groups) + wave, a.tiles - 1), n = 16 * tile + i;      // (waves past the last tile repeat it)
     const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
     const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
-    const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f;
+    const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
     const uint8_t *wc[2], *ws[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -591,7 +576,7 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
         constexpr int MT = decltype(mt_tag)::value;
         const int which = r0 + (tid >> 4);
         const uint16_t* from = a.x + (int64_t)(l.slots[first + min(which, count - 1)] / a.top) * a.ldx;
-        float4v acc[1][MT][2];
+        float4v acc[MT][2];
         clear<MT, 2>(acc);
         multiply_rows<B, MT, 2, DEPTH>(from, of, wc, ws, a.K, 0, (a.K + 127) >> 7, rows, acc);
 #pragma unroll
@@ -604,7 +589,7 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
                 float weight = a.weights[slot];
                 for (int s = slot + 1; s % a.top != 0; ++s)             // the same expert again
                     if (l.id[s] == e) weight += a.weights[s];
-                store_h(a, slot, n, acc[0][r][0][k] * alpha, acc[0][r][1][k] * alpha, weight);
+                store_h(a, slot, n, acc[r][0][k] * alpha, acc[r][1][k] * alpha, weight);
             }
     };
     for (int r0 = 0; r0 < count; r0 += 32) {
@@ -626,7 +611,7 @@ __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
     const int n0 = 16 * (8 * (int)(blockIdx.x % (uint32_t)a.groups) + wave), n = min(n0, (a.N - 1) & ~15) + i;     // (waves past the last tile repeat it)
     const Row<B> of(min(i, a.N - 1 - (n - i)), q, a.I, a.down.code_pitch, a.down.scale_pitch);
     const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
-    const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit;
+    const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
     const uint8_t* const wc[1] = {codes_of(a.down, e, n - i)};
     const uint8_t* const ws[1] = {scales_of(a.down, e, n - i)};
     const int chunks = (a.I + 127) >> 7, c0 = split * chunks / a.splits, c1 = (split + 1) * chunks / a.splits;
@@ -635,7 +620,7 @@ __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
         constexpr int MT = decltype(mt_tag)::value;
         const int copy = tid >> 4, which = r0 + 8 * (copy >> 4) + (copy & 7);
         const uint16_t* from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[first + min(which, count - 1)] * a.pitch;
-        float4v acc[1][MT][1];
+        float4v acc[MT][1];
         clear<MT, 1>(acc);
         multiply_rows<B, MT, 1, DEPTH>(from, of, wc, ws, a.I, c0, c1, rows, acc);
 #pragma unroll
@@ -644,7 +629,7 @@ __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
             for (int k = 0; k < 4; ++k) {
                 const int at = r0 + 8 * r + 4 * (q & 1) + k;
                 float* to = out + (int64_t)l.slots[first + min(at, count - 1)] * a.N;
-                const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][r][0][k]), __float_as_uint(acc[0][r][0][k]), false, false);
+                const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[r][0][k]), __float_as_uint(acc[r][0][k]), false, false);
                 const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
                 if (lane < 32 && at < count && n < a.N) to[n] = v * alpha;
             }
@@ -701,7 +686,7 @@ arcq_status launch_up_rows(const UpArgs& u, int64_t items, int cus, hipStream_t 
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     const int64_t teams = 8 / KW;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>((items + teams - 1) / teams, 2 * cus)), dim3(512), 2 * 16384 + 512 + (size_t)up_row_bytes(u.M, u.K), stream, u);
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>((items + teams - 1) / teams, cus)), dim3(512), 2 * 16384 + 512 + (size_t)up_row_bytes(u.M, u.K), stream, u);
     return check_launch("up_few_kernel");
 }
 template <int B, int KW>
@@ -709,13 +694,13 @@ arcq_status launch_up_few(const UpArgs& u, int64_t items, int cus, hipStream_t s
     return u.M == 1 ? launch_up_rows<B, KW, 1>(u, items, cus, stream) : u.M <= 4 ? launch_up_rows<B, KW, 4>(u, items, cus, stream) : launch_up_rows<B, KW, 16>(u, items, cus, stream);
 }
 
-template <int B, int TOKENS, int DEPTH, typename OutT>
+template <int B, int TOKENS, typename OutT>
 arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
     constexpr int WAVES = 16;
-    auto kern = down_few_kernel<B, TOKENS, WAVES, DEPTH, OutT>;
+    auto kern = down_few_kernel<B, TOKENS, WAVES, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256, stream, d);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256 + 512, stream, d);
     return check_launch("down_few_kernel");
 }
 
@@ -741,8 +726,7 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     if (up_few(M, p.top, p.K)) {
         const int64_t items = most * tiles;
         const int chunks = (int)((p.K + 127) / 128);
-        int kw = 2;
-        while (kw < 8 && items * kw < 16 * cus && chunks >= 4 * kw) kw *= 2;
+        const int kw = chunks >= 32 ? 8 : chunks >= 16 ? 4 : 2;
         const arcq_status st = kw == 2   ? launch_up_few<B, 2>(u, items, cus, p.stream)
                                : kw == 4 ? launch_up_few<B, 4>(u, items, cus, p.stream)
                                          : launch_up_few<B, 8>(u, items, cus, p.stream);
@@ -753,7 +737,7 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     }
     DownArgs<OutT> d = {high, low, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
                         static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 127) / 128), 1};
-    if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2, 4>(d, p.stream) : M <= 4 ? launch_down_few<B, 4, 4>(d, p.stream) : launch_down_few<B, 8, 2>(d, p.stream);
+    if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2>(d, p.stream) : M <= 4 ? launch_down_few<B, 4>(d, p.stream) : launch_down_few<B, 8>(d, p.stream);
     // (a last launch of fewer tokens has the runs of the first: there is room for those)
     d.splits = down_splits(std::min<int64_t>(p.M, kMostTokens), p.top, p.E, p.I, p.N);
     hipLaunchKernelGGL((down_many_kernel<B, 4, OutT>), dim3((unsigned)(most * d.splits * d.groups)), dim3(512), 0, p.stream, d);
