@@ -457,22 +457,25 @@ __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E,
 }
 
 // Eight waves' products of the same 16 MT rows, chunks c0 .. c1 - 1, each wave with NT tiles of weights of its own (from wc, ws on).  Rows reach all
-// waves through LDS, a chunk at a time in two buffers; `from`: the row that this thread copies a piece of 8 k of (piece tid % 16, row tid / 16).
-// Loads of rows and of weights are DEPTH chunks ahead alike: they return in order.
+// waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  `from`: the row that this thread copies pieces of 8 k of (piece tid % 16 of a
+// chunk, row tid / 16; with 16 rows, half of the threads copy every other chunk).  Rows and weights of the next stage are asked for in this one, rows first:
+// they are needed first, and loads return in order.
+constexpr int kStage = 4;
 template <int MT>
-constexpr int kRowBytes = MT * 4096;                // of a buffer
+constexpr int kRowBytes = kStage * MT * 4096;       // of a buffer
 
-template <int B, int MT, int NT, int DEPTH>
+template <int B, int MT, int NT>
 __device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>& of, const uint8_t* const (&wc)[NT], const uint8_t* const (&ws)[NT], int K, int c0, int c1,
                                               uint8_t* lds, float4v (&acc)[MT][NT]) {
+    constexpr int G = kStage, PER = 2 * MT;         // pieces of a thread
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
-    const int piece = tid & 15, copy_row = tid >> 4, pieces = K >> 3, blocks = of.blocks;
-    const bool copies = copy_row < 16 * MT;
+    const int piece = tid & 15, copy_row = (tid >> 4) & (16 * MT - 1), pieces = K >> 3, blocks = of.blocks;
+    auto chunk_of = [&](int k) { return MT == 2 ? k : 2 * k + (tid >> 8); };
     auto unit = [](int p, int r) { return 16 * (256 * (r >> 4) + 16 * p + ((r & 15) ^ p)); };
     const int to = unit(piece, copy_row);
     if (c0 >= c1) return;
     if (blocks < of.SB) {                         // less than one chunk: too short to be moved back into
-        if (copies) *reinterpret_cast<u32x4*>(lds + to) = piece < pieces ? *reinterpret_cast<const u32x4*>(from + 8 * piece) : u32x4{0, 0, 0, 0};
+        if (tid < 256 * MT) *reinterpret_cast<u32x4*>(lds + to) = piece < pieces ? *reinterpret_cast<const u32x4*>(from + 8 * piece) : u32x4{0, 0, 0, 0};
         uint4 words[NT];
         uint32_t sw[NT];
 #pragma unroll
@@ -505,59 +508,76 @@ __device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>
         __syncthreads();
         return;
     }
-    struct {
-        u32x4 codes[NT], piece;
-        u32x2 scales[NT];
-    } ring[DEPTH];
-    auto ask = [&](int d, int at) {                 // (past the end: the last chunk again)
-        const int c = min(at, c1 - 1);
+    u32x4 rows[PER], cw[G][NT];
+    u32x2 sc[NT];
+    auto ask_rows = [&](int c) {                    // (past the end: the last chunk again)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) ring[d].scales[t] = of.scales(ws[t], c);
-        ring[d].piece = *reinterpret_cast<const u32x4*>(from + 8 * min(16 * c + piece, pieces - 1));
-#pragma unroll
-        for (int t = 0; t < NT; ++t) ring[d].codes[t] = of.codes(wc[t], c);
+        for (int k = 0; k < PER; ++k) rows[k] = *reinterpret_cast<const u32x4*>(from + 8 * min(16 * min(c + chunk_of(k), c1 - 1) + piece, pieces - 1));
     };
-    auto put = [&](int d, int c) {
-        const bool in = 16 * c + piece < pieces;
-        if (copies) *reinterpret_cast<u32x4*>(lds + (c & 1) * kRowBytes<MT> + to) = in ? ring[d].piece : u32x4{0, 0, 0, 0};
-    };
+    auto put_rows = [&](int c, int buffer) {
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) ask(d, c0 + d);
-    put(0, c0);
+        for (int k = 0; k < PER; ++k) {
+            const bool in = 16 * (c + chunk_of(k)) + piece < pieces;
+            *reinterpret_cast<u32x4*>(lds + buffer * kRowBytes<MT> + chunk_of(k) * MT * 4096 + to) = in ? rows[k] : u32x4{0, 0, 0, 0};
+        }
+    };
+    auto ask_scales = [&](int c) {                  // lane group q: of chunk c + q
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sc[t] = of.scales(ws[t], min(c + q, c1 - 1));
+    };
+    auto ask_codes = [&](int d, int c) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) cw[d][t] = of.codes(wc[t], min(c + d, c1 - 1));
+    };
+    ask_rows(c0);
+    ask_scales(c0);
+#pragma unroll
+    for (int d = 0; d < G; ++d) ask_codes(d, c0);
+    put_rows(c0, 0);
     wait_lgkmcnt0();
     wg_barrier();
-    for (int at = c0; at < c1; at += DEPTH) {
+    int buffer = 0;
+    for (int c = c0; c < c1; c += G) {
+        ask_rows(c + G);
+        uint32_t sw[4][NT];
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int c = at + d;
-            if (c < c1) {
-                put((d + 1) % DEPTH, c + 1);        // (behind the last one: a buffer that nobody reads)
+        for (int t = 0; t < NT; ++t) {
+            const u32x2 v = of.whole(sc[t], min(c + q, c1 - 1));
+            uint32_t one[4];
+            scales_of_group<B>(make_uint2(v[0], v[1]), one);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) sw[d][t] = one[d];
+        }
+        ask_scales(c + G);
+#pragma unroll
+        for (int d = 0; d < G; ++d) {
+            if (c + d < c1) {
                 half8 xf[MT][4];
 #pragma unroll
                 for (int r = 0; r < MT; ++r)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + (c & 1) * kRowBytes<MT> + unit(4 * j + q, 16 * r + i));
+                    for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + buffer * kRowBytes<MT> + d * MT * 4096 + unit(4 * j + q, 16 * r + i));
                 uint4 words[NT];
-                uint32_t sw[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    words[t] = of.whole(ring[d].codes[t], c);
-                    sw[t] = of.of_lane(of.whole(ring[d].scales[t], c), q);
-                }
-                multiply_folded<B, MT, NT>(xf, words, sw, acc);
-                wait_lgkmcnt0();
-                wg_barrier();                       // not __syncthreads(): loads stay in flight
+                for (int t = 0; t < NT; ++t) words[t] = of.whole(cw[d][t], c + d);
+                multiply_folded<B, MT, NT>(xf, words, sw[d], acc);
             }
-            ask(d, c + DEPTH);
+            __builtin_amdgcn_sched_barrier(0);
+            ask_codes(d, c + G);
         }
+        buffer ^= 1;
+        put_rows(c + G, buffer);                    // (behind the last stage: a buffer that nobody reads)
+        wait_lgkmcnt0();
+        wg_barrier();                               // not __syncthreads(): loads stay in flight
     }
 }
 
 // 128 columns of an expert a workgroup, 16 rows of G and of U for each wave; its tokens 16 or 32 at a time.
-template <int B, int DEPTH>
+template <int B>
 __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
-    __shared__ Lists l;
-    __shared__ __attribute__((aligned(16))) uint8_t rows[2 * kRowBytes<2>];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    uint8_t* rows = lds;
+    Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<2>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     lists_of<512>(a.ids, a.M, a.top, a.E, l);
     const int groups = (a.tiles + 7) >> 3, nth = (int)(blockIdx.x / (uint32_t)groups);
@@ -574,11 +594,11 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
     }
     auto tokens = [&](auto mt_tag, int r0) {
         constexpr int MT = decltype(mt_tag)::value;
-        const int which = r0 + (tid >> 4);
+        const int which = r0 + ((tid >> 4) & (16 * MT - 1));
         const uint16_t* from = a.x + (int64_t)(l.slots[first + min(which, count - 1)] / a.top) * a.ldx;
         float4v acc[MT][2];
         clear<MT, 2>(acc);
-        multiply_rows<B, MT, 2, DEPTH>(from, of, wc, ws, a.K, 0, (a.K + 127) >> 7, rows, acc);
+        multiply_rows<B, MT, 2>(from, of, wc, ws, a.K, 0, (a.K + 127) >> 7, rows, acc);
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
@@ -598,40 +618,47 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
     }
 }
 
-// Results of every slot by itself, in fp32: 16 columns a wave of an expert, 128 a workgroup, over one of `splits` runs of I; its tokens 8, 16 or 32 at a time.
-template <int B, int DEPTH, typename OutT>
+// Results of every slot by itself, in fp32: 32 columns a wave of an expert, 256 a workgroup, over one of `splits` runs of I; its tokens 8, 16 or 32 at a time.
+template <int B, typename OutT>
 __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
-    __shared__ Lists l;
-    __shared__ __attribute__((aligned(16))) uint8_t rows[2 * kRowBytes<2>];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    uint8_t* rows = lds;
+    Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<2>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     lists_of<512>(a.ids, a.M, a.top, a.E, l);
     const uint32_t item = blockIdx.x / (uint32_t)a.groups;
     const int nth = (int)(item / (uint32_t)a.splits), split = (int)(item % (uint32_t)a.splits);
     if (nth >= l.actives) return;
-    const int n0 = 16 * (8 * (int)(blockIdx.x % (uint32_t)a.groups) + wave), n = min(n0, (a.N - 1) & ~15) + i;     // (waves past the last tile repeat it)
-    const Row<B> of(min(i, a.N - 1 - (n - i)), q, a.I, a.down.code_pitch, a.down.scale_pitch);
+    // two tiles of 16 columns; those past the last one begin at the last whole 16, which are another's, and are not stored
+    const int n0 = 32 * (8 * (int)(blockIdx.x % (uint32_t)a.groups) + wave), last = a.N < 16 ? 0 : a.N - 16;
+    const Row<B> of(min(i, a.N - 1), q, a.I, a.down.code_pitch, a.down.scale_pitch);
     const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
     const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
-    const uint8_t* const wc[1] = {codes_of(a.down, e, n - i)};
-    const uint8_t* const ws[1] = {scales_of(a.down, e, n - i)};
+    const int at0 = min(n0, last), at1 = min(n0 + 16, last);
+    const uint8_t* const wc[2] = {codes_of(a.down, e, at0), codes_of(a.down, e, at1)};
+    const uint8_t* const ws[2] = {scales_of(a.down, e, at0), scales_of(a.down, e, at1)};
     const int chunks = (a.I + 127) >> 7, c0 = split * chunks / a.splits, c1 = (split + 1) * chunks / a.splits;
     float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
     auto tokens = [&](auto mt_tag, int r0) {
         constexpr int MT = decltype(mt_tag)::value;
-        const int copy = tid >> 4, which = r0 + 8 * (copy >> 4) + (copy & 7);
+        const int copy = (tid >> 4) & (16 * MT - 1), which = r0 + 8 * (copy >> 4) + (copy & 7);
         const uint16_t* from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[first + min(which, count - 1)] * a.pitch;
-        float4v acc[MT][1];
-        clear<MT, 1>(acc);
-        multiply_rows<B, MT, 1, DEPTH>(from, of, wc, ws, a.I, c0, c1, rows, acc);
+        float4v acc[MT][2];
+        clear<MT, 2>(acc);
+        multiply_rows<B, MT, 2>(from, of, wc, ws, a.I, c0, c1, rows, acc);
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int at = r0 + 8 * r + 4 * (q & 1) + k;
                 float* to = out + (int64_t)l.slots[first + min(at, count - 1)] * a.N;
-                const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[r][0][k]), __float_as_uint(acc[r][0][k]), false, false);
-                const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
-                if (lane < 32 && at < count && n < a.N) to[n] = v * alpha;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[r][t][k]), __float_as_uint(acc[r][t][k]), false, false);
+                    const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
+                    const int n = (t == 0 ? at0 : at1) + i;             // a column that an earlier tile has, too, is that one's
+                    if (lane < 32 && at < count && n >= n0 + 16 * t && n < a.N) to[n] = v * alpha;
+                }
             }
     };
     for (int r0 = 0; r0 < count; r0 += 16) {
@@ -663,9 +690,11 @@ int64_t up_row_bytes(int64_t M, int64_t K) { return (M == 1 ? 1 : M <= 4 ? 4 : 1
 bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 64 && K >= 256 && up_row_bytes(M, K) <= kUpRows - 33 * 1024; }
 bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
 
+constexpr size_t kManyLds = 2 * kRowBytes<2> + sizeof(Lists);
+
 // Runs of I for down_many_kernel.
 int down_splits(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
-    const int64_t groups = (N + 127) / 128 * std::min<int64_t>(E, M * top), chunks = (I + 127) / 128;
+    const int64_t groups = (N + 255) / 256 * std::min<int64_t>(E, M * top), chunks = (I + 127) / 128;
     return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(groups, 1), chunks / 8, 8}));
 }
 
@@ -732,15 +761,21 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
                                          : launch_up_few<B, 8>(u, items, cus, p.stream);
         if (st) return st;
     } else {
-        hipLaunchKernelGGL((up_many_kernel<B, 4>), dim3((unsigned)(most * ((tiles + 7) / 8))), dim3(512), 0, p.stream, u);
+        auto kern = up_many_kernel<B>;
+        static std::atomic<uint64_t> lds_raised{0};
+        if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(most * ((tiles + 7) / 8))), dim3(512), kManyLds, p.stream, u);
         if (arcq_status st = check_launch("up_many_kernel")) return st;
     }
     DownArgs<OutT> d = {high, low, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
-                        static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 127) / 128), 1};
+                        static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 255) / 256), 1};
     if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2>(d, p.stream) : M <= 4 ? launch_down_few<B, 4>(d, p.stream) : launch_down_few<B, 8>(d, p.stream);
     // (a last launch of fewer tokens has the runs of the first: there is room for those)
     d.splits = down_splits(std::min<int64_t>(p.M, kMostTokens), p.top, p.E, p.I, p.N);
-    hipLaunchKernelGGL((down_many_kernel<B, 4, OutT>), dim3((unsigned)(most * d.splits * d.groups)), dim3(512), 0, p.stream, d);
+    auto kern = down_many_kernel<B, OutT>;
+    static std::atomic<uint64_t> lds_raised{0};
+    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(most * d.splits * d.groups)), dim3(512), kManyLds, p.stream, d);
     if (arcq_status st = check_launch("down_many_kernel")) return st;
     const unsigned parts = (unsigned)((p.N + 255) / 256);
     hipLaunchKernelGGL((join_kernel<OutT>), dim3(parts * (unsigned)M), dim3(256), 0, p.stream, d, parts);
