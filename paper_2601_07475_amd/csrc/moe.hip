@@ -395,28 +395,40 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
 
 // ---- more tokens: rows gathered by expert
 
-// Which slots (token, choice) every expert has.
+// Which slots (token, choice) every expert has, in blocks of up to ROWS.
 struct Lists {
     uint16_t start[kMostExperts], count[kMostExperts];
-    uint16_t active[kMostExperts];              // experts with slots, ascending
     uint16_t slots[kMostSlots];                 // by expert
     int16_t id[kMostSlots];                     // by slot, -1 for none
+    __attribute__((aligned(16))) int16_t first[kMostSlots];      // the same without a token's later choices of an expert: those count with the first
+    uint16_t expert[kMostSlots], begin[kMostSlots];     // of a block: its expert, and the first of that expert's slots
     uint32_t fill[kMostExperts];
-    int actives;
+    int blocks;
 };
 
-// All threads of the workgroup.
-template <int THREADS>
+// Of a value a lane: the sum over the lanes before.
+__device__ __forceinline__ int sum_before(int n) {
+    const int lane = threadIdx.x & 63;
+    int sum = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+    }
+    return sum - n;
+}
+
+// All threads of the workgroup.  An expert's slots are in ascending order: every workgroup has the same blocks.
+template <int THREADS, int ROWS>
 __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E, Lists& l) {
     const int tid = threadIdx.x, slots = M * top;
     constexpr int PER = (kMostSlots + THREADS - 1) / THREADS;
-    int id[PER];
-    uint32_t at[PER];
+    int id[PER], at[PER];
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         const int t = tid + p * THREADS;
         id[p] = checked_id(ids, t, slots, E);
-        if (t < slots) l.id[t] = (int16_t)id[p];
+        if (t < kMostSlots) l.id[t] = (int16_t)id[p];
     }
     for (int e = tid; e < E; e += THREADS) l.fill[e] = 0;
     __syncthreads();
@@ -424,30 +436,43 @@ __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E,
     for (int p = 0; p < PER; ++p) {
         const int t = tid + p * THREADS;
         for (int u = t - t % top; u < t && id[p] >= 0; ++u)
-            if (l.id[u] == id[p]) id[p] = -1;       // (a later choice of the same expert counts with the first)
-        if (id[p] >= 0) at[p] = atomicAdd(&l.fill[id[p]], 1u);
+            if (l.id[u] == id[p]) id[p] = -1;
+        if (t < kMostSlots) l.first[t] = (int16_t)id[p];
+        if (id[p] >= 0) atomicAdd(&l.fill[id[p]], 1u);
     }
     __syncthreads();
-    if (tid < 64) {
-        int begin = 0, actives = 0;
-        for (int base = 0; base < E; base += 64) {
-            const int e = base + tid, n = e < E ? (int)l.fill[e] : 0;
-            int sum = n;
+    // a slot's place: how many before it have its expert, eight ids a read
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int other = __shfl_up(sum, d);
-                if (tid >= d) sum += other;
+    for (int p = 0; p < PER; ++p) {
+        const int t = tid + p * THREADS, until = min(t | 63, slots - 1) >> 3;
+        at[p] = 0;
+        if (p * THREADS >= slots) continue;
+        for (int g = 0; g <= until; ++g) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(l.first + 8 * g);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int other = (int16_t)(k & 1 ? v[k >> 1] >> 16 : v[k >> 1]);
+                at[p] += other == id[p] && 8 * g + k < t ? 1 : 0;
             }
-            const uint64_t some = __ballot(n > 0);
+        }
+    }
+    if (tid < 64) {
+        int begin = 0, blocks = 0;
+        for (int base = 0; base < E; base += 64) {
+            const int e = base + tid, n = e < E ? (int)l.fill[e] : 0, mine = (n + ROWS - 1) / ROWS;
+            const int before = begin + sum_before(n), block = blocks + sum_before(mine);
             if (e < E) {
-                l.start[e] = (uint16_t)(begin + sum - n);
+                l.start[e] = (uint16_t)before;
                 l.count[e] = (uint16_t)n;
             }
-            if (n > 0) l.active[actives + __popcll(some & ((1ull << tid) - 1ull))] = (uint16_t)e;
-            begin += __shfl(sum, 63);
-            actives += __popcll(some);
+            for (int k = 0; k < mine; ++k) {
+                l.expert[block + k] = (uint16_t)e;
+                l.begin[block + k] = (uint16_t)(ROWS * k);
+            }
+            begin = __shfl(before + n, 63);
+            blocks = __shfl(block + mine, 63);
         }
-        if (tid == 0) l.actives = actives;
+        if (tid == 0) l.blocks = blocks;
     }
     __syncthreads();
 #pragma unroll
@@ -456,63 +481,77 @@ __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E,
     __syncthreads();
 }
 
-// Eight waves' products of the same 16 MT rows, chunks c0 .. c1 - 1, each wave with NT tiles of weights of its own (from wc, ws on).  Rows reach all
-// waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  `from`: the row that this thread copies pieces of 8 k of (piece tid % 16 of a
-// chunk, row tid / 16; with 16 rows, half of the threads copy every other chunk).  Rows and weights of the next stage are asked for in this one, rows first:
-// they are needed first, and loads return in order.
+// A workgroup's piece of work: a block of an expert's slots with the eight waves' tiles of weights, two each, over a run of the reduction.
+struct Item {
+    const uint16_t* from;                       // the row that this thread copies pieces of 8 k of: piece tid % 16 of a chunk, row (tid / 16) % (16 MT)
+    const uint8_t *wc[2], *ws[2];               // the wave's tiles
+    int c0, c1;                                 // chunks
+    bool two;                                   // rows behind the first 16 are in use
+};
+
+// Items of a launch in turn.  Rows reach all waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  (With 16 rows half of the threads copy
+// every other chunk.)  Rows and weights of the next stage, or of the next item's first, are asked for in this one, rows first: they are needed first, and
+// loads return in order.  take(n): the n-th; store(n, sums).
 constexpr int kStage = 4;
 template <int MT>
-constexpr int kRowBytes = kStage * MT * 4096;       // of a buffer
+constexpr int kRowBytes = kStage * MT * 4096;   // of a buffer
 
-template <int B, int MT, int NT>
-__device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>& of, const uint8_t* const (&wc)[NT], const uint8_t* const (&ws)[NT], int K, int c0, int c1,
-                                              uint8_t* lds, float4v (&acc)[MT][NT]) {
-    constexpr int G = kStage, PER = 2 * MT;         // pieces of a thread
+template <int B, int MT, typename Take, typename Store>
+__device__ __forceinline__ void stream_items(int begin, int end, int stride, const Row<B>& of, int K, uint8_t* lds, const Take& take, const Store& store) {
+    constexpr int G = kStage, PER = 2 * MT, NT = 2; // pieces of a thread
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
-    const int piece = tid & 15, copy_row = (tid >> 4) & (16 * MT - 1), pieces = K >> 3, blocks = of.blocks;
+    const int piece = tid & 15, pieces = K >> 3, blocks = of.blocks;
     auto chunk_of = [&](int k) { return MT == 2 ? k : 2 * k + (tid >> 8); };
     auto unit = [](int p, int r) { return 16 * (256 * (r >> 4) + 16 * p + ((r & 15) ^ p)); };
-    const int to = unit(piece, copy_row);
-    if (c0 >= c1) return;
-    if (blocks < of.SB) {                         // less than one chunk: too short to be moved back into
-        if (tid < 256 * MT) *reinterpret_cast<u32x4*>(lds + to) = piece < pieces ? *reinterpret_cast<const u32x4*>(from + 8 * piece) : u32x4{0, 0, 0, 0};
-        uint4 words[NT];
-        uint32_t sw[NT];
+    const int to = unit(piece, (tid >> 4) & (16 * MT - 1));
+    if (begin >= end) return;
+    if (blocks < of.SB) {                           // less than one chunk: too short to be moved back into
+        for (int item = begin; item < end; item += stride) {
+            const Item now = take(item);
+            if (tid < 256 * MT) *reinterpret_cast<u32x4*>(lds + to) = piece < pieces ? *reinterpret_cast<const u32x4*>(now.from + 8 * piece) : u32x4{0, 0, 0, 0};
+            uint4 words[NT];
+            uint32_t sw[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            u32x4 v = {0, 0, 0, 0};
-            uint64_t s = 0;
-            if constexpr (B == 16) {
-                if (2 * q < blocks) {
-                    const uint2 w = load8_a8(wc[t] + of.code);
-                    v[0] = w.x, v[1] = w.y;
+            for (int t = 0; t < NT; ++t) {
+                u32x4 v = {0, 0, 0, 0};
+                uint64_t s = 0;
+                if constexpr (B == 16) {
+                    if (2 * q < blocks) {
+                        const uint2 w = load8_a8(now.wc[t] + of.code);
+                        v[0] = w.x, v[1] = w.y;
+                    }
+                    if (2 * q + 1 < blocks) {
+                        const uint2 w = load8_a8(now.wc[t] + of.code + 8);
+                        v[2] = w.x, v[3] = w.y;
+                    }
+                } else {
+                    if (q < blocks) v = *reinterpret_cast<const u32x4_a4*>(now.wc[t] + of.code);
                 }
-                if (2 * q + 1 < blocks) {
-                    const uint2 w = load8_a8(wc[t] + of.code + 8);
-                    v[2] = w.x, v[3] = w.y;
-                }
-            } else {
-                if (q < blocks) v = *reinterpret_cast<const u32x4_a4*>(wc[t] + of.code);
+                for (int k = 0; k < blocks; ++k) s |= (uint64_t)now.ws[t][of.scale + k] << (8 * k);
+                words[t] = make_uint4(v[0], v[1], v[2], v[3]);
+                sw[t] = of.of_lane(u32x2{(uint32_t)s, (uint32_t)(s >> 32)}, q);
             }
-            for (int k = 0; k < blocks; ++k) s |= (uint64_t)ws[t][of.scale + k] << (8 * k);
-            words[t] = make_uint4(v[0], v[1], v[2], v[3]);
-            sw[t] = of.of_lane(u32x2{(uint32_t)s, (uint32_t)(s >> 32)}, q);
+            __syncthreads();
+            half8 xf[MT][4];
+            float4v acc[MT][NT];
+            clear<MT, NT>(acc);
+#pragma unroll
+            for (int r = 0; r < MT; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
+            multiply_folded<B, MT, NT>(xf, words, sw, acc);
+            store(item, acc);
+            __syncthreads();
         }
-        __syncthreads();
-        half8 xf[MT][4];
-#pragma unroll
-        for (int r = 0; r < MT; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
-        multiply_folded<B, MT, NT>(xf, words, sw, acc);
-        __syncthreads();
         return;
     }
     u32x4 rows[PER], cw[G][NT];
     u32x2 sc[NT];
+    Item ahead = take(begin);                       // whose loads are asked for next
     auto ask_rows = [&](int c) {                    // (past the end: the last chunk again)
 #pragma unroll
-        for (int k = 0; k < PER; ++k) rows[k] = *reinterpret_cast<const u32x4*>(from + 8 * min(16 * min(c + chunk_of(k), c1 - 1) + piece, pieces - 1));
+        for (int k = 0; k < PER; ++k)
+            rows[k] = *reinterpret_cast<const u32x4*>(ahead.from + 8 * min(16 * min(c + chunk_of(k), ahead.c1 - 1) + piece, pieces - 1));
     };
     auto put_rows = [&](int c, int buffer) {
 #pragma unroll
@@ -523,148 +562,174 @@ __device__ __forceinline__ void multiply_rows(const uint16_t* from, const Row<B>
     };
     auto ask_scales = [&](int c) {                  // lane group q: of chunk c + q
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sc[t] = of.scales(ws[t], min(c + q, c1 - 1));
+        for (int t = 0; t < NT; ++t) sc[t] = of.scales(ahead.ws[t], min(c + q, ahead.c1 - 1));
     };
     auto ask_codes = [&](int d, int c) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) cw[d][t] = of.codes(wc[t], min(c + d, c1 - 1));
+        for (int t = 0; t < NT; ++t) cw[d][t] = of.codes(ahead.wc[t], min(c + d, ahead.c1 - 1));
     };
-    ask_rows(c0);
-    ask_scales(c0);
+    ask_rows(ahead.c0);
+    ask_scales(ahead.c0);
 #pragma unroll
-    for (int d = 0; d < G; ++d) ask_codes(d, c0);
-    put_rows(c0, 0);
+    for (int d = 0; d < G; ++d) ask_codes(d, ahead.c0);
+    put_rows(ahead.c0, 0);
     wait_lgkmcnt0();
     wg_barrier();
     int buffer = 0;
-    for (int c = c0; c < c1; c += G) {
-        ask_rows(c + G);
-        uint32_t sw[4][NT];
+    for (int item = begin; item < end; item += stride) {
+        const int c0 = ahead.c0, c1 = ahead.c1;
+        const bool two = ahead.two;
+        float4v acc[MT][NT];
+        clear<MT, NT>(acc);
+        for (int c = c0; c < c1; c += G) {
+            uint32_t sw[4][NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const u32x2 v = of.whole(sc[t], min(c + q, c1 - 1));
-            uint32_t one[4];
-            scales_of_group<B>(make_uint2(v[0], v[1]), one);
+            for (int t = 0; t < NT; ++t) {
+                const u32x2 v = of.whole(sc[t], min(c + q, c1 - 1));
+                uint32_t one[4];
+                scales_of_group<B>(make_uint2(v[0], v[1]), one);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) sw[d][t] = one[d];
-        }
-        ask_scales(c + G);
-#pragma unroll
-        for (int d = 0; d < G; ++d) {
-            if (c + d < c1) {
-                half8 xf[MT][4];
-#pragma unroll
-                for (int r = 0; r < MT; ++r)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + buffer * kRowBytes<MT> + d * MT * 4096 + unit(4 * j + q, 16 * r + i));
-                uint4 words[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) words[t] = of.whole(cw[d][t], c + d);
-                multiply_folded<B, MT, NT>(xf, words, sw[d], acc);
+                for (int d = 0; d < 4; ++d) sw[d][t] = one[d];
             }
-            __builtin_amdgcn_sched_barrier(0);
-            ask_codes(d, c + G);
+            int next = c + G;
+            if (next >= c1) {
+                ahead = take(item + stride < end ? item + stride : item);
+                next = ahead.c0;
+            }
+            ask_rows(next);
+            ask_scales(next);
+#pragma unroll
+            for (int d = 0; d < G; ++d) {
+                if (c + d < c1) {
+                    const uint8_t* at = lds + buffer * kRowBytes<MT> + d * MT * 4096;
+                    half8 xf[MT][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(at + unit(4 * j + q, i));
+                    if (MT > 1 && two)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) xf[MT - 1][j] = *reinterpret_cast<const half8*>(at + unit(4 * j + q, 16 * (MT - 1) + i));
+                    uint4 words[NT];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) words[t] = of.whole(cw[d][t], c + d);
+                    multiply_folded<B, MT, NT>(xf, words, sw[d], acc, two);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                ask_codes(d, next);
+            }
+            buffer ^= 1;
+            put_rows(next, buffer);
+            wait_lgkmcnt0();
+            wg_barrier();                           // not __syncthreads(): loads stay in flight
         }
-        buffer ^= 1;
-        put_rows(c + G, buffer);                    // (behind the last stage: a buffer that nobody reads)
-        wait_lgkmcnt0();
-        wg_barrier();                               // not __syncthreads(): loads stay in flight
+        store(item, acc);
     }
 }
 
-// 128 columns of an expert a workgroup, 16 rows of G and of U for each wave; its tokens 16 or 32 at a time.
-template <int B>
+// Items of a workgroup: those of an expert are next to each other, and workgroups of one XCD, which share an L2, take a run of them in turn.
+struct Share {
+    int begin, end, stride;
+};
+__device__ __forceinline__ Share share_of(int all) {
+    constexpr int XCDS = 8;
+    const int wg = (int)blockIdx.x, wgs = (int)gridDim.x, x = wg % XCDS, of_xcd = (wgs - x + XCDS - 1) / XCDS;
+    const int x0 = (int)((int64_t)x * all / XCDS), x1 = (int)((int64_t)(x + 1) * all / XCDS);
+    if (wgs < XCDS) return {wg, all, wgs};
+    return {x0 + wg / XCDS, x1, of_xcd};
+}
+
+// An item: 128 columns of an expert for up to 16 MT of its tokens; a wave has 16 rows of G and of U.
+template <int B, int MT>
 __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    uint8_t* rows = lds;
-    Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<2>);
+    Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    lists_of<512>(a.ids, a.M, a.top, a.E, l);
-    const int groups = (a.tiles + 7) >> 3, nth = (int)(blockIdx.x / (uint32_t)groups);
-    if (nth >= l.actives) return;
-    const int tile = min(8 * (int)(blockIdx.x % (uint32_t)groups) + wave, a.tiles - 1), n = 16 * tile + i;      // (waves past the last tile repeat it)
+    lists_of<512, 16 * MT>(a.ids, a.M, a.top, a.E, l);
+    const int groups = (a.tiles + 7) >> 3, chunks = (a.K + 127) >> 7;
     const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
-    const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
-    const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
-    const uint8_t *wc[2], *ws[2];
+    auto tile_of = [&](int group) { return min(8 * group + wave, a.tiles - 1); };       // (waves past the last tile repeat it)
+    auto take = [&](int item) {
+        const int block = item / groups, tile = tile_of(item - block * groups);
+        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = __builtin_amdgcn_readfirstlane(l.begin[block]), left = __builtin_amdgcn_readfirstlane(l.count[e]) - r0;
+        Item v;
+        v.from = a.x + (int64_t)(l.slots[l.start[e] + r0 + min((tid >> 4) & (16 * MT - 1), left - 1)] / a.top) * a.ldx;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        wc[t] = codes_of(a.up, e, t * a.I + 16 * tile);
-        ws[t] = scales_of(a.up, e, t * a.I + 16 * tile);
-    }
-    auto tokens = [&](auto mt_tag, int r0) {
-        constexpr int MT = decltype(mt_tag)::value;
-        const int which = r0 + ((tid >> 4) & (16 * MT - 1));
-        const uint16_t* from = a.x + (int64_t)(l.slots[first + min(which, count - 1)] / a.top) * a.ldx;
-        float4v acc[MT][2];
-        clear<MT, 2>(acc);
-        multiply_rows<B, MT, 2>(from, of, wc, ws, a.K, 0, (a.K + 127) >> 7, rows, acc);
+        for (int t = 0; t < 2; ++t) {
+            v.wc[t] = codes_of(a.up, e, t * a.I + 16 * tile);
+            v.ws[t] = scales_of(a.up, e, t * a.I + 16 * tile);
+        }
+        v.c0 = 0, v.c1 = chunks;
+        v.two = left > 16;
+        return v;
+    };
+    auto store = [&](int item, const float4v (&acc)[MT][2]) {
+        const int block = item / groups, tile = tile_of(item - block * groups);
+        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = l.begin[block], left = l.count[e] - r0, first = l.start[e] + r0;
+        const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int at = r0 + 16 * r + 4 * q + k;
-                if (at >= count) continue;
+                const int at = 16 * r + 4 * q + k;
+                if (at >= left) continue;
                 const int slot = l.slots[first + at];
                 float weight = a.weights[slot];
                 for (int s = slot + 1; s % a.top != 0; ++s)             // the same expert again
                     if (l.id[s] == e) weight += a.weights[s];
-                store_h(a, slot, n, acc[r][0][k] * alpha, acc[r][1][k] * alpha, weight);
+                store_h(a, slot, 16 * tile + i, acc[r][0][k] * alpha, acc[r][1][k] * alpha, weight);
             }
     };
-    for (int r0 = 0; r0 < count; r0 += 32) {
-        if (count - r0 <= 16) tokens(std::integral_constant<int, 1>{}, r0);
-        else tokens(std::integral_constant<int, 2>{}, r0);
-    }
+    const Share mine = share_of(l.blocks * groups);
+    stream_items<B, MT>(mine.begin, mine.end, mine.stride, of, a.K, lds, take, store);
 }
 
-// Results of every slot by itself, in fp32: 32 columns a wave of an expert, 256 a workgroup, over one of `splits` runs of I; its tokens 8, 16 or 32 at a time.
-template <int B, typename OutT>
+// Results of every slot by itself, in fp32.  An item: 256 columns of an expert over one of `splits` runs of I, for up to 8 MT of its tokens; a wave has 32 columns.
+template <int B, int MT, typename OutT>
 __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    uint8_t* rows = lds;
-    Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<2>);
+    Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    lists_of<512>(a.ids, a.M, a.top, a.E, l);
-    const uint32_t item = blockIdx.x / (uint32_t)a.groups;
-    const int nth = (int)(item / (uint32_t)a.splits), split = (int)(item % (uint32_t)a.splits);
-    if (nth >= l.actives) return;
-    // two tiles of 16 columns; those past the last one begin at the last whole 16, which are another's, and are not stored
-    const int n0 = 32 * (8 * (int)(blockIdx.x % (uint32_t)a.groups) + wave), last = a.N < 16 ? 0 : a.N - 16;
+    lists_of<512, 8 * MT>(a.ids, a.M, a.top, a.E, l);
+    const int chunks = (a.I + 127) >> 7, pieces = a.groups * a.splits, last = a.N < 16 ? 0 : a.N - 16;
     const Row<B> of(min(i, a.N - 1), q, a.I, a.down.code_pitch, a.down.scale_pitch);
-    const int e = __builtin_amdgcn_readfirstlane(l.active[nth]), count = __builtin_amdgcn_readfirstlane(l.count[e]), first = __builtin_amdgcn_readfirstlane(l.start[e]);
-    const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
-    const int at0 = min(n0, last), at1 = min(n0 + 16, last);
-    const uint8_t* const wc[2] = {codes_of(a.down, e, at0), codes_of(a.down, e, at1)};
-    const uint8_t* const ws[2] = {scales_of(a.down, e, at0), scales_of(a.down, e, at1)};
-    const int chunks = (a.I + 127) >> 7, c0 = split * chunks / a.splits, c1 = (split + 1) * chunks / a.splits;
-    float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
-    auto tokens = [&](auto mt_tag, int r0) {
-        constexpr int MT = decltype(mt_tag)::value;
-        const int copy = (tid >> 4) & (16 * MT - 1), which = r0 + 8 * (copy >> 4) + (copy & 7);
-        const uint16_t* from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[first + min(which, count - 1)] * a.pitch;
-        float4v acc[MT][2];
-        clear<MT, 2>(acc);
-        multiply_rows<B, MT, 2>(from, of, wc, ws, a.I, c0, c1, rows, acc);
+    auto col_of = [&](int group) { return 32 * (8 * group + wave); };
+    // item: block, then run, then group
+    auto take = [&](int item) {
+        const int block = item / pieces, rest = item - block * pieces, split = rest / a.groups, n0 = col_of(rest - split * a.groups);
+        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = __builtin_amdgcn_readfirstlane(l.begin[block]), left = __builtin_amdgcn_readfirstlane(l.count[e]) - r0;
+        const int copy = (tid >> 4) & (16 * MT - 1), which = 8 * (copy >> 4) + (copy & 7);
+        Item v;
+        v.from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[l.start[e] + r0 + min(which, left - 1)] * a.pitch;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {               // tiles past the last column begin 16 before it; what an earlier tile has, too, is not stored
+            v.wc[t] = codes_of(a.down, e, min(n0 + 16 * t, last));
+            v.ws[t] = scales_of(a.down, e, min(n0 + 16 * t, last));
+        }
+        v.c0 = split * chunks / a.splits, v.c1 = (split + 1) * chunks / a.splits;
+        v.two = left > 8;
+        return v;
+    };
+    auto store = [&](int item, const float4v (&acc)[MT][2]) {
+        const int block = item / pieces, rest = item - block * pieces, split = rest / a.groups, n0 = col_of(rest - split * a.groups);
+        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = l.begin[block], left = l.count[e] - r0, first = l.start[e] + r0;
+        const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
+        float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int at = r0 + 8 * r + 4 * (q & 1) + k;
-                float* to = out + (int64_t)l.slots[first + min(at, count - 1)] * a.N;
+                const int at = 8 * r + 4 * (q & 1) + k;
+                float* to = out + (int64_t)l.slots[first + min(at, left - 1)] * a.N;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[r][t][k]), __float_as_uint(acc[r][t][k]), false, false);
                     const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
-                    const int n = (t == 0 ? at0 : at1) + i;             // a column that an earlier tile has, too, is that one's
-                    if (lane < 32 && at < count && n >= n0 + 16 * t && n < a.N) to[n] = v * alpha;
+                    const int n = min(n0 + 16 * t, last) + i;
+                    if (lane < 32 && at < left && n >= n0 + 16 * t && n < a.N) to[n] = v * alpha;
                 }
             }
     };
-    for (int r0 = 0; r0 < count; r0 += 16) {
-        if (count - r0 <= 8) tokens(std::integral_constant<int, 1>{}, r0);
-        else tokens(std::integral_constant<int, 2>{}, r0);
-    }
+    const Share mine = share_of(l.blocks * pieces);
+    stream_items<B, MT>(mine.begin, mine.end, mine.stride, of, a.I, lds, take, store);
 }
 
 // y of a token: its slots' results, each over its runs, in their order, and the residual.
@@ -689,8 +754,6 @@ constexpr int64_t kUpRows = 80 << 10;               // LDS of a workgroup of up_
 int64_t up_row_bytes(int64_t M, int64_t K) { return (M == 1 ? 1 : M <= 4 ? 4 : 16) * ((K + 127) / 128) * 256; }
 bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 64 && K >= 256 && up_row_bytes(M, K) <= kUpRows - 33 * 1024; }
 bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
-
-constexpr size_t kManyLds = 2 * kRowBytes<2> + sizeof(Lists);
 
 // Runs of I for down_many_kernel.
 int down_splits(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
@@ -733,6 +796,24 @@ arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
     return check_launch("down_few_kernel");
 }
 
+// items: as many as there can be.
+template <int B, int MT>
+arcq_status launch_up_many(const UpArgs& u, int64_t items, hipStream_t stream) {
+    auto kern = up_many_kernel<B, MT>;
+    static std::atomic<uint64_t> lds_raised{0};
+    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu())), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, u);
+    return check_launch("up_many_kernel");
+}
+template <int B, int MT, typename OutT>
+arcq_status launch_down_many(const DownArgs<OutT>& d, int64_t items, hipStream_t stream) {
+    auto kern = down_many_kernel<B, MT, OutT>;
+    static std::atomic<uint64_t> lds_raised{0};
+    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu())), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, d);
+    return check_launch("down_many_kernel");
+}
+
 template <int B, typename OutT>
 arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     const MoeWorkspace w = workspace_of(std::min<int64_t>(p.M, kMostTokens), p.top, p.K, p.I, p.N, p.E, p.perm != nullptr);
@@ -761,22 +842,16 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
                                          : launch_up_few<B, 8>(u, items, cus, p.stream);
         if (st) return st;
     } else {
-        auto kern = up_many_kernel<B>;
-        static std::atomic<uint64_t> lds_raised{0};
-        if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(most * ((tiles + 7) / 8))), dim3(512), kManyLds, p.stream, u);
-        if (arcq_status st = check_launch("up_many_kernel")) return st;
+        const int64_t groups = (tiles + 7) / 8;
+        if (arcq_status st = M <= 16 ? launch_up_many<B, 1>(u, M * p.top * groups, p.stream) : launch_up_many<B, 2>(u, M * p.top * groups, p.stream)) return st;
     }
     DownArgs<OutT> d = {high, low, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
                         static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 255) / 256), 1};
     if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2>(d, p.stream) : M <= 4 ? launch_down_few<B, 4>(d, p.stream) : launch_down_few<B, 8>(d, p.stream);
     // (a last launch of fewer tokens has the runs of the first: there is room for those)
     d.splits = down_splits(std::min<int64_t>(p.M, kMostTokens), p.top, p.E, p.I, p.N);
-    auto kern = down_many_kernel<B, OutT>;
-    static std::atomic<uint64_t> lds_raised{0};
-    if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(most * d.splits * d.groups)), dim3(512), kManyLds, p.stream, d);
-    if (arcq_status st = check_launch("down_many_kernel")) return st;
+    const int64_t items = M * p.top * d.splits * d.groups;
+    if (arcq_status st = M <= 8 ? launch_down_many<B, 1>(d, items, p.stream) : launch_down_many<B, 2>(d, items, p.stream)) return st;
     const unsigned parts = (unsigned)((p.N + 255) / 256);
     hipLaunchKernelGGL((join_kernel<OutT>), dim3(parts * (unsigned)M), dim3(256), 0, p.stream, d, parts);
     return check_launch("join_kernel");

@@ -73,8 +73,9 @@ __device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (
 template <int B>
 constexpr float kFolded = B == 32 ? 256.0f : 1.0f;
 
+// all: whether the tiles of rows behind the first one are wanted.
 template <int B, int MT, int NT>
-__device__ __forceinline__ void multiply_folded(const half8 (&xf)[MT][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[MT][NT]) {
+__device__ __forceinline__ void multiply_folded(const half8 (&xf)[MT][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[MT][NT], bool all = true) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         transpose_words(cw[t]);
@@ -95,7 +96,10 @@ __device__ __forceinline__ void multiply_folded(const half8 (&xf)[MT][4], uint4 
                 w[j] = half8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
             }
         }
-        if (!block_by_block) {
+        if (!block_by_block && MT > 1 && !all) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[0][j], w[j], acc[0][t], 0, 0, 0);
+        } else if (!block_by_block) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -106,6 +110,7 @@ __device__ __forceinline__ void multiply_folded(const half8 (&xf)[MT][4], uint4 
                 const float s = power_of(sw[t] >> (8 * j) & 0xFFu);
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
+                    if (r > 0 && !all) break;
                     const float4v sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[r][t][e] = __builtin_fmaf(sum[e] * kFolded<B>, s, acc[r][t][e]);
