@@ -112,7 +112,7 @@ struct Row {                                        // the lane's
     // the chunk's scale bytes in their places; of a whole chunk nothing changes
     __device__ u32x2 whole(u32x2 s, int c) const {
         const int off = 8 * max(SB * c - (blocks - SB), 0);
-        if constexpr (B == 32) return u32x2{s[0] >> off, 0u};
+        if constexpr (B == 32) return u32x2{s[0] >> off | (0x70707070u & ~(0xFFFFFFFFu >> off)), 0u};       // (bytes past the end that fold)
         const uint64_t v = ((uint64_t)s[1] << 32 | s[0]) >> off;
         return u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
     }
@@ -130,6 +130,26 @@ struct Row {                                        // the lane's
 // Where a tile starts whose first row is `row` of expert e (uniform).
 __device__ __forceinline__ const uint8_t* codes_of(const Experts& w, int e, int64_t row) { return w.codes + ((int64_t)e * w.rows + row) * w.code_pitch; }
 __device__ __forceinline__ const uint8_t* scales_of(const Experts& w, int e, int64_t row) { return w.scales + ((int64_t)e * w.rows + row) * w.scale_pitch; }
+
+// `count` chunks whose scales do not all fold, asked for only here, one at a time: rows(d, fragments), codes(d, tile).
+template <int B, int MT, int NT, typename Rows, typename Codes>
+__device__ __forceinline__ void block_by_block(int count, const uint32_t (&sw)[4][NT], const Rows& rows, const Codes& codes, float4v (&acc)[MT][NT]) {
+    if constexpr (B == 32) {
+#pragma unroll 1
+        for (int d = 0; d < count; ++d) {
+            half8 xf[MT][4];
+            rows(d, xf);
+            uint4 words[NT];
+            uint32_t one[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                words[t] = codes(d, t);
+                one[t] = d == 0 ? sw[0][t] : d == 1 ? sw[1][t] : d == 2 ? sw[2][t] : sw[3][t];
+            }
+            multiply_folded<B, false, MT>(xf, words, one, acc);
+        }
+    }
+}
 
 template <int MT, int NT>
 __device__ __forceinline__ void clear(float4v (&acc)[MT][NT]) {
@@ -163,7 +183,7 @@ __device__ __forceinline__ int checked_id(const int32_t* ids, int t, int slots, 
 // workgroups take one such tile for each of their 8 / KW teams after the other, and ask for the next one's weights while they multiply and add up this one's.
 // ROWS: places for tokens in LDS.
 template <int B, int KW, int ROWS>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) void up_few_kernel(UpArgs a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) void up_few_kernel(UpArgs a) {
     constexpr int TEAMS = 8 / KW, G = 4;            // chunks in flight
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     float(&red)[2][8][2][4][64] = *reinterpret_cast<float(*)[2][8][2][4][64]>(lds);     // wave, G or U, element, lane
@@ -234,21 +254,30 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 #pragma unroll
                 for (int d = 0; d < 4; ++d) sw[d][t] = s[d];
             }
+            auto rows_of = [&](int d, half8 (&xf)[1][4]) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(x_lane + 256 * ROWS * (c + d) + 64 * ROWS * j);
+            };
+            const bool fold = folds<B>(sw);
+            if (!fold) block_by_block<B, 1>(count, sw, rows_of, [&](int d, int t) { return of.whole(of.codes(wc[t], c + d), c + d); }, acc);
             if (over) take(min(item + stride, all - 1));
             ask_scales(next);
+            if (fold) {
 #pragma unroll
-            for (int d = 0; d < G; ++d) {
-                if (d < count) {
-                    half8 xf[1][4];
+                for (int d = 0; d < G; ++d) {
+                    if (d < count) {                // (rows past the wave's last chunk are another's)
+                        half8 xf[1][4];
+                        rows_of(d, xf);
+                        uint4 words[2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(x_lane + 256 * ROWS * c + 16 * ROWS * (16 * d + 4 * j));
-                    uint4 words[2];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) words[t] = of.whole(cw[d][t], c + d);
-                    multiply_folded<B, 1, 2>(xf, words, sw[d], acc);
+                        for (int t = 0; t < 2; ++t) words[t] = of.whole(cw[d][t], c + d);
+                        multiply_folded<B, true, 1>(xf, words, sw[d], acc);
+                    }
+                    ask_codes(next, d);
                 }
-                __builtin_amdgcn_sched_barrier(0);  // (the next chunk's rows are not read from LDS before: registers)
-                ask_codes(next, d);
+            } else {
+#pragma unroll
+                for (int d = 0; d < G; ++d) ask_codes(next, d);
             }
         }
         float(&part)[8][2][4][64] = red[round & 1];
@@ -285,7 +314,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
 // Rows of h reach a wave's registers through a slice of LDS of its own, so that a chunk on its way takes TOKENS / 2 registers of 16 bytes and not four.
 template <int B, int TOKENS, int WAVES, typename OutT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4))) void down_few_kernel(DownArgs<OutT> a) {
-    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2, G = TOKENS == 8 ? 3 : 4;      // (as registers allow)
+    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2, G = TOKENS < 8 ? 4 : B == 16 ? 3 : 2;      // (as registers allow)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     float(&sums)[WAVES][8][16] = *reinterpret_cast<float(*)[WAVES][8][16]>(lds);
     int* ids_of = reinterpret_cast<int*>(lds + sizeof(sums));
@@ -328,10 +357,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     u32x4 cw[G], rows[G][LOADS];
     u32x2 sc;
     auto ask_scales = [&](int g) { sc = of.scales(ws, min(G * g + q, per - 1)); };
+    auto load_rows = [&](int c, u32x4 (&to)[LOADS]) {
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) to[l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + 128u * (uint32_t)c));
+    };
     auto ask_chunk = [&](int g, int d) {
         const int c = min(G * g + d, per - 1);
-#pragma unroll
-        for (int l = 0; l < LOADS; ++l) rows[d][l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + 128u * (uint32_t)c));
+        load_rows(c, rows[d]);
         cw[d] = of.codes(wc, c);
     };
     if (s0 < s1) {
@@ -347,24 +379,40 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
             const bool over = g + 1 == groups, end = s + 1 == s1;
             const int next = end ? g : over ? 0 : g + 1;        // (behind the last one: itself again)
             const u32x2 v = of.whole(sc, min(G * g + q, per - 1));
-            uint32_t sw[4];
-            scales_of_group<B>(make_uint2(v[0], v[1]), sw);
+            uint32_t one[4], sw[4][1];
+            scales_of_group<B>(make_uint2(v[0], v[1]), one);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) sw[d][0] = one[d];
+            auto rows_of = [&](const u32x4 (&from)[LOADS], half8 (&xf)[1][4]) {     // (LDS operations of a wave complete in order)
+#pragma unroll
+                for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4*>(slice + unit(i, 4 * l + q)) = from[l];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(slice + unit(4 * j + q, 2 * (i & (TOKENS - 1)) + (i >> 3)));
+            };
+            const bool fold = folds<B>(sw);
+            if (!fold)
+                block_by_block<B, 1>(count, sw, [&](int d, half8 (&xf)[1][4]) {
+                    u32x4 from[LOADS];
+                    load_rows(G * g + d, from);
+                    rows_of(from, xf);
+                }, [&](int d, int) { return of.whole(of.codes(wc, G * g + d), G * g + d); }, acc);
             if (over && !end) take(nth + 1);
             ask_scales(next);
+            if (fold) {
 #pragma unroll
-            for (int d = 0; d < G; ++d) {
-                if (d < count) {
-#pragma unroll
-                    for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4*>(slice + unit(i, 4 * l + q)) = rows[d][l];
-                    half8 xf[1][4];                 // (LDS operations of a wave complete in order)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(slice + unit(4 * j + q, 2 * (i & (TOKENS - 1)) + (i >> 3)));
-                    uint4 words[1] = {of.whole(cw[d], G * g + d)};
-                    const uint32_t one[1] = {sw[d]};
-                    multiply_folded<B, 1, 1>(xf, words, one, acc);
+                for (int d = 0; d < G; ++d) {
+                    if (d < count) {
+                        half8 xf[1][4];
+                        rows_of(rows[d], xf);
+                        uint4 words[1] = {of.whole(cw[d], G * g + d)};
+                        multiply_folded<B, true, 1>(xf, words, sw[d], acc);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    ask_chunk(next, d);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                ask_chunk(next, d);
+            } else {
+#pragma unroll
+                for (int d = 0; d < G; ++d) ask_chunk(next, d);
             }
             if (over || end) {
                 const float alpha = B == 16 ? a.down.tensor_scales[__builtin_amdgcn_readlane(active, nth)] * kUnit : kUnit / kFolded<B>;
@@ -539,7 +587,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
             for (int r = 0; r < MT; ++r)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
-            multiply_folded<B, MT, NT>(xf, words, sw, acc);
+            multiply_folded<B, B == 16, MT>(xf, words, sw, acc);
             store(item, acc);
             __syncthreads();
         }
@@ -556,7 +604,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
     auto put_rows = [&](int c, int buffer) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const bool in = 16 * (c + chunk_of(k)) + piece < pieces;
+            const bool in = c + chunk_of(k) < ahead.c1 && 16 * (c + chunk_of(k)) + piece < pieces;      // (all four chunks are multiplied)
             *reinterpret_cast<u32x4*>(lds + buffer * kRowBytes<MT> + chunk_of(k) * MT * 4096 + to) = in ? rows[k] : u32x4{0, 0, 0, 0};
         }
     };
@@ -591,6 +639,18 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
 #pragma unroll
                 for (int d = 0; d < 4; ++d) sw[d][t] = one[d];
             }
+            auto rows_of = [&](int d, auto& xf, auto tiles) {
+                const uint8_t* at = lds + buffer * kRowBytes<MT> + d * MT * 4096;
+#pragma unroll
+                for (int r = 0; r < decltype(tiles)::value; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(at + unit(4 * j + q, 16 * r + i));
+            };
+            using All = std::integral_constant<int, MT>;
+            const bool fold = folds<B>(sw);
+            if (!fold)
+                block_by_block<B, MT>(min(G, c1 - c), sw, [&](int d, half8 (&xf)[MT][4]) { rows_of(d, xf, All{}); },
+                                      [&](int d, int t) { return of.whole(of.codes(ahead.wc[t], c + d), c + d); }, acc);
             int next = c + G;
             if (next >= c1) {
                 ahead = take(item + stride < end ? item + stride : item);
@@ -598,23 +658,25 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
             }
             ask_rows(next);
             ask_scales(next);
+            auto multiply = [&](auto tiles) {
 #pragma unroll
-            for (int d = 0; d < G; ++d) {
-                if (c + d < c1) {
-                    const uint8_t* at = lds + buffer * kRowBytes<MT> + d * MT * 4096;
+                for (int d = 0; d < G; ++d) {
                     half8 xf[MT][4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(at + unit(4 * j + q, i));
-                    if (MT > 1 && two)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) xf[MT - 1][j] = *reinterpret_cast<const half8*>(at + unit(4 * j + q, 16 * (MT - 1) + i));
+                    rows_of(d, xf, tiles);
                     uint4 words[NT];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) words[t] = of.whole(cw[d][t], c + d);
-                    multiply_folded<B, MT, NT>(xf, words, sw[d], acc, two);
+                    multiply_folded<B, true, decltype(tiles)::value>(xf, words, sw[d], acc);
+                    ask_codes(d, next);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                ask_codes(d, next);
+            };
+            if (!fold) {
+#pragma unroll
+                for (int d = 0; d < G; ++d) ask_codes(d, next);
+            } else if (MT > 1 && !two) {
+                multiply(std::integral_constant<int, 1>{});
+            } else {
+                multiply(All{});
             }
             buffer ^= 1;
             put_rows(next, buffer);

@@ -68,38 +68,45 @@ __device__ __forceinline__ void multiply_chunk(const half8 (&xf)[MT][4], uint4 (
 }
 
 // The same sums kFolded<B> times as large, with every scale in the weights' fp16 numbers.  MXFP4: code x 2^(byte - 127 + 8) is exact in fp16 for bytes from 96 to
-// 127, from the smallest subnormal to 1536, which is where weights have theirs; a tile with another one among a chunk's goes the way above, block by block.
-// That saves 28 of 59 vector instructions for 2048 weights and a tile of rows.
+// 127, from the smallest subnormal to 1536, which is where weights have theirs: folds() tells whether all of a wave's are.  Chunks with others go block by
+// block as above (FOLD: false).  Folding saves 28 of 59 vector instructions for 2048 weights and a tile of rows.
 template <int B>
 constexpr float kFolded = B == 32 ? 256.0f : 1.0f;
 
-// all: whether the tiles of rows behind the first one are wanted.
-template <int B, int MT, int NT>
-__device__ __forceinline__ void multiply_folded(const half8 (&xf)[MT][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[MT][NT], bool all = true) {
+template <int B, int N, int NT>
+__device__ __forceinline__ bool folds(const uint32_t (&sw)[N][NT]) {
+    if constexpr (B == 16) return true;
+    uint32_t off = 0;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) off |= sw[d][t] ^ 0x60606060u;
+    return __ballot((off & 0xE0E0E0E0u) != 0) == 0;
+}
+
+// Tiles of rows 0 .. MT - 1.
+template <int B, bool FOLD, int MT, int NT, int ROWS>
+__device__ __forceinline__ void multiply_folded(const half8 (&xf)[ROWS][4], uint4 (&cw)[NT], const uint32_t (&sw)[NT], float4v (&acc)[ROWS][NT]) {
+    static_assert(MT <= ROWS && (FOLD || B == 32), "NVFP4's scales always fold");
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         transpose_words(cw[t]);
         const uint32_t word[4] = {cw[t].x, cw[t].y, cw[t].z, cw[t].w};
         half8 w[4];
-        bool block_by_block = false;
         if constexpr (B == 16) {
             const uint32_t s01 = scale_halves(sw[t], 0x0C010C00), s23 = scale_halves(sw[t], 0x0C030C02);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = decode8_half(word[j], j < 2 ? s01 : s23, j & 1);
         } else {
-            block_by_block = __ballot((sw[t] & 0xE0E0E0E0u) != 0x60606060u) != 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float f = block_by_block ? 1.0f : __uint_as_float(((sw[t] >> (8 * j) & 0xFFu) + 8u) << 23);
+                const float f = FOLD ? __uint_as_float(((sw[t] >> (8 * j) & 0xFFu) + 8u) << 23) : 1.0f;
                 const half2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word[j], f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word[j], f, 1),
                              p2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word[j], f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word[j], f, 3);
                 w[j] = half8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
             }
         }
-        if (!block_by_block && MT > 1 && !all) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[0][j], w[j], acc[0][t], 0, 0, 0);
-        } else if (!block_by_block) {
+        if constexpr (FOLD) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -110,7 +117,6 @@ __device__ __forceinline__ void multiply_folded(const half8 (&xf)[MT][4], uint4 
                 const float s = power_of(sw[t] >> (8 * j) & 0xFFu);
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
-                    if (r > 0 && !all) break;
                     const float4v sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(xf[r][j], w[j], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[r][t][e] = __builtin_fmaf(sum[e] * kFolded<B>, s, acc[r][t][e]);

@@ -261,17 +261,18 @@ def test_unaligned_weights_and_scales():
         assert_within(call(fmt, dev(x), None, ids, w, *moved, out_dtype=torch.float32), want, off)
 
 
-def test_every_scale_byte():
-    """Exponents of MXFP4 and all scales of NVFP4, on either side of the activation."""
-    say("moe, scale bytes")
+@pytest.mark.parametrize("M", [2, 7, 12, 40])
+def test_every_scale_byte(M):
+    """Exponents of MXFP4 and all scales of NVFP4, on either side of the activation; tokens as one tile of rows and gathered."""
+    say("moe, scale bytes", M)
     rng = np.random.default_rng(2)
     for fmt, bytes_, block in (("mx", np.arange(90, 150), 32), ("nvfp4", np.arange(0, 0x7F), 16)):
-        M, K, N = 2, 2 * block, len(bytes_)
-        I = (len(bytes_) + 31) // 32 * 32
+        K, N = 8 * block, len(bytes_)
+        I = (len(bytes_) + 31) // 32 * 32 + 128
         x = (rng.standard_normal((M, K)) * 0.5).astype(np.float16)
         ids, w = np.zeros((M, 1), dtype=np.int32), np.ones((M, 1), dtype=np.float32)
         flat = np.ones(1, dtype=np.float32) if fmt == "nvfp4" else None
-        up = rng.integers(0, 256, (1, 2 * I, K // 2), dtype=np.uint8), np.full((1, 2 * I, 2), 120 if fmt == "mx" else 0x30, dtype=np.uint8), flat
+        up = rng.integers(0, 256, (1, 2 * I, K // 2), dtype=np.uint8), np.full((1, 2 * I, 8), 120 if fmt == "mx" else 0x30, dtype=np.uint8), flat
         down = rng.integers(0, 256, (1, N, I // 2), dtype=np.uint8), np.repeat(bytes_[None, :, None], I // block, 2).astype(np.uint8), flat
         want, off = L.experts(x, None, ids, w, up, down, "none")
         assert_within(call(fmt, dev(x), None, ids, w, up, down, activation=B.ACT_NONE, out_dtype=torch.float32), want, off)
