@@ -178,42 +178,77 @@ __device__ __forceinline__ int checked_id(const int32_t* ids, int t, int slots, 
     return e >= 0 && e < E ? e : -1;
 }
 
+// The same for up to 256 slots, all threads of a workgroup of 512: the experts to `found`.
+__device__ __forceinline__ int distinct(const int16_t* ids, int slots, int16_t* found, int (&counts)[8]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int e = tid < slots ? ids[tid] : -1;
+    bool first = e >= 0;
+    for (int g = 0; g <= min(tid | 63, slots - 1) >> 3; ++g) {      // eight ids a read
+        const u32x4 v = *reinterpret_cast<const u32x4*>(ids + 8 * g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) first = first && !((int16_t)(k & 1 ? v[k >> 1] >> 16 : v[k >> 1]) == e && 8 * g + k < tid);
+    }
+    const uint64_t firsts = __ballot(first);
+    if (lane == 0) counts[wave] = __popcll(firsts);
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < 8; ++w) {
+        before += w < wave ? counts[w] : 0;
+        all += counts[w];
+    }
+    if (first) found[before + __popcll(firsts & ((1ull << lane) - 1ull))] = (int16_t)e;
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(all);
+}
+
 // All tokens are rows of one tile, for every expert, so no list of an expert's tokens is needed: what comes out for one that does not choose it is passed over.
-// They lie in LDS, eight k of all tokens after the other.  A tile of 16 columns of an expert, that is 16 rows of G and of U, is for KW waves, which split K;
-// workgroups take one such tile for each of their 8 / KW teams after the other, and ask for the next one's weights while they multiply and add up this one's.
-// ROWS: places for tokens in LDS.
-template <int B, int KW, int ROWS>
+// They lie in LDS.  A tile of 16 columns of an expert, that is 16 rows of G and of U, is for KW waves, which split K; workgroups, one on a compute unit, take
+// such a tile for each of their 8 / KW teams after the other, and ask for the next one's weights while they multiply and add up this one's.
+// G: chunks in flight.  SLOTS: most slots, 64 (experts in a wave's lanes) or 256 (in LDS).
+struct UpFewLds {
+    float sums[8][2][4][64];                        // wave, G or U, element, lane
+    float weights[256];
+    __attribute__((aligned(16))) int16_t ids[256];
+    int16_t active[256];
+    int counts[8];
+};
+template <int B, int KW, int G, int SLOTS>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) void up_few_kernel(UpArgs a) {
-    constexpr int TEAMS = 8 / KW, G = 4;            // chunks in flight
+    constexpr int TEAMS = 8 / KW;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    float(&red)[2][8][2][4][64] = *reinterpret_cast<float(*)[2][8][2][4][64]>(lds);     // wave, G or U, element, lane
-    int* ids_of = reinterpret_cast<int*>(lds + sizeof(red));
-    float* weights_of = reinterpret_cast<float*>(lds + sizeof(red) + 256);
-    uint8_t* xs = lds + sizeof(red) + 512;
+    UpFewLds& l = *reinterpret_cast<UpFewLds*>(lds);
+    uint8_t* xs = lds + sizeof(UpFewLds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     const int kw = wave % KW, team = wave / KW, slots = a.M * a.top;
-    const int id = checked_id(a.ids, lane, slots, a.E);
-    const float weight_of = lane < slots ? a.weights[lane] : 0.0f;
-    const int chunks = (a.K + 127) >> 7, pieces = a.K >> 3;
+    const int mine = SLOTS == 64 ? lane : tid;      // of the slots
+    const int id = checked_id(a.ids, mine, slots, a.E);
+    const float weight_of = mine < slots ? a.weights[mine] : 0.0f;
+    const int chunks = (a.K + 127) >> 7, pieces = a.K >> 3, pitch = 256 * chunks + 16;      // (16 bytes more than whole chunks: rows spread over the banks)
     for (int u = tid; u < 16 * chunks * a.M; u += 512) {                // (pieces past the end are zeros)
         const int m = a.M == 1 ? 0 : u / (16 * chunks), p = u - m * 16 * chunks;
         u32x4 v = {0, 0, 0, 0};
         if (p < pieces) v = *reinterpret_cast<const u32x4*>(a.x + m * a.ldx + 8 * p);
-        *reinterpret_cast<u32x4*>(xs + 16 * (p * ROWS + m)) = v;
+        *reinterpret_cast<u32x4*>(xs + m * pitch + 16 * p) = v;
     }
-    if (wave == 0) {
-        ids_of[lane] = id;
-        weights_of[lane] = weight_of;
+    if (tid < SLOTS) {
+        l.ids[tid] = (int16_t)id;
+        l.weights[tid] = weight_of;
     }
-    int actives;
-    const int active = distinct(id, actives);
+    int actives, active = -1;
+    if constexpr (SLOTS == 64) {
+        active = distinct(id, actives);
+    } else {
+        __syncthreads();
+        actives = distinct(l.ids, slots, l.active, l.counts);
+    }
+    auto expert_of = [&](int nth) { return SLOTS == 64 ? __builtin_amdgcn_readlane(active, nth) : __builtin_amdgcn_readfirstlane(l.active[nth]); };
     const int all = actives * a.tiles, stride = (int)gridDim.x * TEAMS;
     const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
-    const uint8_t* x_lane = xs + 16 * (q * ROWS + min(i, a.M - 1));
+    const uint8_t* x_lane = xs + min(i, a.M - 1) * pitch + 16 * q;
     const int c0 = kw * chunks / KW, n = (kw + 1) * chunks / KW - c0, groups = (n + G - 1) / G;     // n >= 1
     const uint8_t *wc[2], *ws[2];
     auto take = [&](int item) {                     // the item whose weights are asked for next
-        const int nth = item / a.tiles, e = __builtin_amdgcn_readlane(active, nth);
+        const int nth = item / a.tiles, e = expert_of(nth);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {               // (I is a multiple of 16)
             wc[t] = codes_of(a.up, e, t * a.I + 16 * (item - nth * a.tiles));
@@ -256,7 +291,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
             }
             auto rows_of = [&](int d, half8 (&xf)[1][4]) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(x_lane + 256 * ROWS * (c + d) + 64 * ROWS * j);
+                for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(x_lane + 256 * (c + d) + 64 * j);
             };
             const bool fold = folds<B>(sw);
             if (!fold) block_by_block<B, 1>(count, sw, rows_of, [&](int d, int t) { return of.whole(of.codes(wc[t], c + d), c + d); }, acc);
@@ -280,32 +315,33 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
                 for (int d = 0; d < G; ++d) ask_codes(next, d);
             }
         }
-        float(&part)[8][2][4][64] = red[round & 1];
+        if (round > 0) wg_barrier();                // (the sums of the round before have been read)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) part[wave][t][k][lane] = acc[0][t][k];
+            for (int k = 0; k < 4; ++k) l.sums[wave][t][k][lane] = acc[0][t][k];
         wait_lgkmcnt0();
         wg_barrier();
         if (item < all) {
-            const int nth = item / a.tiles, e = __builtin_amdgcn_readlane(active, nth), n0 = 16 * (item - nth * a.tiles);
+            const int nth = item / a.tiles, e = expert_of(nth), n0 = 16 * (item - nth * a.tiles);
             const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
             for (int idx = kw * 64 + lane; idx < 16 * a.M; idx += 64 * KW) {
                 const int m = idx >> 4, at = 16 * (m >> 2) + (idx & 15), k = m & 3;
                 int slot = -1;
                 float weight = 0.0f;
                 for (int j = 0; j < a.top; ++j)
-                    if (ids_of[m * a.top + j] == e) {
+                    if (l.ids[m * a.top + j] == e) {
                         slot = slot < 0 ? m * a.top + j : slot;
-                        weight += weights_of[m * a.top + j];
+                        weight += l.weights[m * a.top + j];
                     }
                 if (slot < 0) continue;
                 float g = 0.f, u = 0.f;
 #pragma unroll
-                for (int w = 0; w < KW; ++w) g += part[team * KW + w][0][k][at], u += part[team * KW + w][1][k][at];
+                for (int w = 0; w < KW; ++w) g += l.sums[team * KW + w][0][k][at], u += l.sums[team * KW + w][1][k][at];
                 store_h(a, slot, n0 + (idx & 15), g * alpha, u * alpha, weight);
             }
         }
+        wait_lgkmcnt0();                            // (reads of the sums have come back before the next barrier)
     }
 }
 
@@ -699,9 +735,21 @@ __device__ __forceinline__ Share share_of(int all) {
     return {x0 + wg / XCDS, x1, of_xcd};
 }
 
+// Where an item is: blocks of an expert over the same weights are next to each other, so that those come from memory once.
+struct Place {
+    int expert, first, left, piece;             // the first of the expert's slots in the list, and how many from there on; which of `pieces` pieces of its weights
+};
+template <int ROWS>
+__device__ __forceinline__ Place place_of(const Lists& l, int item, int pieces) {
+    const int some = item / pieces, e = __builtin_amdgcn_readfirstlane(l.expert[some]), begin = __builtin_amdgcn_readfirstlane(l.begin[some]);
+    const int count = __builtin_amdgcn_readfirstlane(l.count[e]), start = __builtin_amdgcn_readfirstlane(l.start[e]);
+    const int blocks = (count + ROWS - 1) / ROWS, local = item - (some - begin / ROWS) * pieces, piece = local / blocks, r0 = (local - piece * blocks) * ROWS;
+    return {e, start + r0, count - r0, piece};
+}
+
 // An item: 128 columns of an expert for up to 16 MT of its tokens; a wave has 16 rows of G and of U.
 template <int B, int MT>
-__global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4 : 2, 4))) void up_many_kernel(UpArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
@@ -710,10 +758,10 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
     const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
     auto tile_of = [&](int group) { return min(8 * group + wave, a.tiles - 1); };       // (waves past the last tile repeat it)
     auto take = [&](int item) {
-        const int block = item / groups, tile = tile_of(item - block * groups);
-        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = __builtin_amdgcn_readfirstlane(l.begin[block]), left = __builtin_amdgcn_readfirstlane(l.count[e]) - r0;
+        const Place at = place_of<16 * MT>(l, item, groups);
+        const int e = at.expert, left = at.left, tile = tile_of(at.piece);
         Item v;
-        v.from = a.x + (int64_t)(l.slots[l.start[e] + r0 + min((tid >> 4) & (16 * MT - 1), left - 1)] / a.top) * a.ldx;
+        v.from = a.x + (int64_t)(l.slots[at.first + min((tid >> 4) & (16 * MT - 1), left - 1)] / a.top) * a.ldx;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             v.wc[t] = codes_of(a.up, e, t * a.I + 16 * tile);
@@ -724,8 +772,8 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
         return v;
     };
     auto store = [&](int item, const float4v (&acc)[MT][2]) {
-        const int block = item / groups, tile = tile_of(item - block * groups);
-        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = l.begin[block], left = l.count[e] - r0, first = l.start[e] + r0;
+        const Place place = place_of<16 * MT>(l, item, groups);
+        const int e = place.expert, left = place.left, first = place.first, tile = tile_of(place.piece);
         const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
@@ -746,7 +794,7 @@ __global__ __launch_bounds__(512) void up_many_kernel(UpArgs a) {
 
 // Results of every slot by itself, in fp32.  An item: 256 columns of an expert over one of `splits` runs of I, for up to 8 MT of its tokens; a wave has 32 columns.
 template <int B, int MT, typename OutT>
-__global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4 : 2, 4))) void down_many_kernel(DownArgs<OutT> a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
@@ -754,13 +802,12 @@ __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
     const int chunks = (a.I + 127) >> 7, pieces = a.groups * a.splits, last = a.N < 16 ? 0 : a.N - 16;
     const Row<B> of(min(i, a.N - 1), q, a.I, a.down.code_pitch, a.down.scale_pitch);
     auto col_of = [&](int group) { return 32 * (8 * group + wave); };
-    // item: block, then run, then group
     auto take = [&](int item) {
-        const int block = item / pieces, rest = item - block * pieces, split = rest / a.groups, n0 = col_of(rest - split * a.groups);
-        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = __builtin_amdgcn_readfirstlane(l.begin[block]), left = __builtin_amdgcn_readfirstlane(l.count[e]) - r0;
+        const Place at = place_of<8 * MT>(l, item, pieces);
+        const int e = at.expert, left = at.left, split = at.piece / a.groups, n0 = col_of(at.piece - split * a.groups);
         const int copy = (tid >> 4) & (16 * MT - 1), which = 8 * (copy >> 4) + (copy & 7);
         Item v;
-        v.from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[l.start[e] + r0 + min(which, left - 1)] * a.pitch;
+        v.from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[at.first + min(which, left - 1)] * a.pitch;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {               // tiles past the last column begin 16 before it; what an earlier tile has, too, is not stored
             v.wc[t] = codes_of(a.down, e, min(n0 + 16 * t, last));
@@ -771,8 +818,8 @@ __global__ __launch_bounds__(512) void down_many_kernel(DownArgs<OutT> a) {
         return v;
     };
     auto store = [&](int item, const float4v (&acc)[MT][2]) {
-        const int block = item / pieces, rest = item - block * pieces, split = rest / a.groups, n0 = col_of(rest - split * a.groups);
-        const int e = __builtin_amdgcn_readfirstlane(l.expert[block]), r0 = l.begin[block], left = l.count[e] - r0, first = l.start[e] + r0;
+        const Place place = place_of<8 * MT>(l, item, pieces);
+        const int e = place.expert, left = place.left, first = place.first, split = place.piece / a.groups, n0 = col_of(place.piece - split * a.groups);
         const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
         float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
 #pragma unroll
@@ -812,10 +859,17 @@ __global__ __launch_bounds__(256) void join_kernel(DownArgs<OutT> a, uint32_t pa
 }
 
 // Whether a launch's tokens go as rows of one tile.
-constexpr int64_t kUpRows = 80 << 10;               // LDS of a workgroup of up_few_kernel, two on a compute unit
-int64_t up_row_bytes(int64_t M, int64_t K) { return (M == 1 ? 1 : M <= 4 ? 4 : 16) * ((K + 127) / 128) * 256; }
-bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 64 && K >= 256 && up_row_bytes(M, K) <= kUpRows - 33 * 1024; }
+size_t up_few_lds(int64_t M, int64_t K) { return sizeof(UpFewLds) + (size_t)M * (size_t)((K + 127) / 128 * 256 + 16); }
+bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 256 && K >= 256 && up_few_lds(M, K) <= kMaxLdsBytes; }
 bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
+
+// Waves that split K in up_few_kernel: as many as have four chunks each.  And how many chunks go together, so that few are asked for in vain where a wave's are
+// not a multiple of that.
+int waves_of(int chunks) { return chunks >= 32 ? 8 : chunks >= 16 ? 4 : 2; }
+int group_of(int chunks, int waves) {
+    const int most = (chunks + waves - 1) / waves;
+    return (most + 2) / 3 * 3 < (most + 3) / 4 * 4 ? 3 : 4;
+}
 
 // Runs of I for down_many_kernel.
 int down_splits(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
@@ -834,28 +888,36 @@ MoeWorkspace workspace_of(int64_t M, int64_t top, int64_t K, int64_t I, int64_t 
     return {reorder ? whole(M * K * 2) : 0, whole(M * top * pitch_of(I) * 2), down_few(M, top, I) ? 0 : whole((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4)};
 }
 
-template <int B, int KW, int ROWS>
-arcq_status launch_up_rows(const UpArgs& u, int64_t items, int cus, hipStream_t stream) {
-    auto kern = up_few_kernel<B, KW, ROWS>;
+template <int B, int KW, int G, int SLOTS>
+arcq_status launch_up_slots(const UpArgs& u, int64_t items, hipStream_t stream) {
+    auto kern = up_few_kernel<B, KW, G, SLOTS>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     const int64_t teams = 8 / KW;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>((items + teams - 1) / teams, cus)), dim3(512), 2 * 16384 + 512 + (size_t)up_row_bytes(u.M, u.K), stream, u);
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>((items + teams - 1) / teams, num_cu())), dim3(512), up_few_lds(u.M, u.K), stream, u);
     return check_launch("up_few_kernel");
 }
 template <int B, int KW>
-arcq_status launch_up_few(const UpArgs& u, int64_t items, int cus, hipStream_t stream) {
-    return u.M == 1 ? launch_up_rows<B, KW, 1>(u, items, cus, stream) : u.M <= 4 ? launch_up_rows<B, KW, 4>(u, items, cus, stream) : launch_up_rows<B, KW, 16>(u, items, cus, stream);
+arcq_status launch_up_few(const UpArgs& u, int64_t items, hipStream_t stream) {
+    const bool few = u.M * u.top <= 64;
+    if (group_of((u.K + 127) / 128, KW) == 3) return few ? launch_up_slots<B, KW, 3, 64>(u, items, stream) : launch_up_slots<B, KW, 3, 256>(u, items, stream);
+    return few ? launch_up_slots<B, KW, 4, 64>(u, items, stream) : launch_up_slots<B, KW, 4, 256>(u, items, stream);
 }
 
-template <int B, int TOKENS, typename OutT>
-arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
-    constexpr int WAVES = 16;
+template <int B, int TOKENS, int WAVES, typename OutT>
+arcq_status launch_down_waves(const DownArgs<OutT>& d, hipStream_t stream) {
     auto kern = down_few_kernel<B, TOKENS, WAVES, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
     hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256 + 512, stream, d);
     return check_launch("down_few_kernel");
+}
+
+// 16 waves a workgroup, one on a compute unit; where a last round of those would leave a quarter of the compute units' time idle, 8, of which two fit.
+template <int B, int TOKENS, typename OutT>
+arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
+    const int64_t tiles = (d.N + 15) / 16, cus = num_cu(), rounds = (tiles + cus - 1) / cus;
+    return tiles > cus && 4 * tiles < 3 * rounds * cus ? launch_down_waves<B, TOKENS, 8>(d, stream) : launch_down_waves<B, TOKENS, 16>(d, stream);
 }
 
 // items: as many as there can be.
@@ -864,7 +926,7 @@ arcq_status launch_up_many(const UpArgs& u, int64_t items, hipStream_t stream) {
     auto kern = up_many_kernel<B, MT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu())), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, u);
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu() * (MT == 1 ? 2 : 1))), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, u);
     return check_launch("up_many_kernel");
 }
 template <int B, int MT, typename OutT>
@@ -872,7 +934,7 @@ arcq_status launch_down_many(const DownArgs<OutT>& d, int64_t items, hipStream_t
     auto kern = down_many_kernel<B, MT, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu())), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, d);
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu() * (MT == 1 ? 2 : 1))), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, d);
     return check_launch("down_many_kernel");
 }
 
@@ -894,14 +956,13 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     const Experts up = {p.up_codes, p.up_scales, p.up_tensor_scales, (p.K + p.S_up) / 2, (p.K + p.S_up) / B, (int)(2 * p.I)};
     const Experts down = {p.down_codes, p.down_scales, p.down_tensor_scales, (p.I + p.S_down) / 2, (p.I + p.S_down) / B, (int)p.N};
     const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, high, low, (int)pitch_of(p.I), tiles};
-    const int cus = num_cu();
     if (up_few(M, p.top, p.K)) {
         const int64_t items = most * tiles;
         const int chunks = (int)((p.K + 127) / 128);
-        const int kw = chunks >= 32 ? 8 : chunks >= 16 ? 4 : 2;
-        const arcq_status st = kw == 2   ? launch_up_few<B, 2>(u, items, cus, p.stream)
-                               : kw == 4 ? launch_up_few<B, 4>(u, items, cus, p.stream)
-                                         : launch_up_few<B, 8>(u, items, cus, p.stream);
+        const int kw = waves_of(chunks);
+        const arcq_status st = kw == 2   ? launch_up_few<B, 2>(u, items, p.stream)
+                               : kw == 4 ? launch_up_few<B, 4>(u, items, p.stream)
+                                         : launch_up_few<B, 8>(u, items, p.stream);
         if (st) return st;
     } else {
         const int64_t groups = (tiles + 7) / 8;
