@@ -1,6 +1,10 @@
 // The router of a mixture of experts: scores of all experts for a token, its best ones and their weights.
 //   l[m, e] = sum_k x[m, k] r[e, k];   s = softmax(l) or 1 / (1 + exp(-l));   best by s (+ bias);   weights: their s, or their shares of those
 // Which experts are best is decided by sums in 64 bits of exact products, so near ties fall as the definition has it and not as an order of fp32 sums does.
+//
+// One launch where a workgroup a token gets through the router's weights quickly; otherwise scores_kernel, on v_mfma_f64_16x16x4_f64, leaves sums of runs of K
+// in the workspace and choose_kernel adds them up in their order.  Bound by two launches for a few tokens, by the 64-bit matrix rate for many (2 M K E of
+// 78 * 10^12 a second).
 #include "internal.h"
 
 #include <algorithm>
@@ -10,7 +14,7 @@ namespace arcq {
 namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-constexpr int kPerLane = ARCQ_MOE_MAX_EXPERTS / 64;
+typedef double double4v __attribute__((ext_vector_type(4)));
 
 struct RouteArgs {
     const _Float16 *x, *router;
@@ -20,58 +24,82 @@ struct RouteArgs {
     uint32_t flags;
     int32_t* ids;
     float* weights;
+    double* sums;                               // [splits][M][E]
+    int splits;
 };
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+// A value's neighbour by a data-parallel move (row shifts, then the last lane of a row, of two rows, to the next): lanes without one get `none`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v, double none) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v), o = __builtin_bit_cast(uint64_t, none);
+    const uint32_t lo = __builtin_amdgcn_update_dpp((int)(uint32_t)o, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp((int)(uint32_t)(o >> 32), (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+__device__ __forceinline__ double last_lane(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, 63), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <typename Op>
+__device__ __forceinline__ double over_wave(double v, double none, const Op& op) {
+    v = op(v, moved<0x111, 0xF>(v, none));      // row_shr 1, 2, 4, 8
+    v = op(v, moved<0x112, 0xF>(v, none));
+    v = op(v, moved<0x114, 0xF>(v, none));
+    v = op(v, moved<0x118, 0xF>(v, none));
+    v = op(v, moved<0x142, 0xA>(v, none));      // row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
+    v = op(v, moved<0x143, 0xC>(v, none));
+    return last_lane(v);
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    return over_wave(v, 0.0, [](double a, double b) { return a + b; });
+}
+// (what is not a number is passed over)
 __device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmax(v, __shfl_xor(v, d));
-    return v;
+    return over_wave(v, -INFINITY, [](double a, double b) { return fmax(a, b); });
 }
 
-// One wave: the best experts of a token by its scores, in LDS.
-__device__ void choose(const double* logits, const RouteArgs& a, int64_t m) {
+// One wave: the best experts of token m by its scores; logits[j]: of expert 64 j + lane, not a number past the last one.
+template <int PER>
+__device__ __forceinline__ void choose(const double (&logits)[PER], const RouteArgs& a, int64_t m) {
     const int lane = threadIdx.x & 63;
     const bool sigmoid = (a.flags & ARCQ_MOE_SIGMOID) != 0;
-    double score[kPerLane], rank[kPerLane];
+    double score[PER], rank[PER];
     double most = -INFINITY;
-    for (int j = 0; j < kPerLane; ++j) {
-        const int e = 64 * j + lane;
-        score[j] = e < a.E ? logits[e] : __builtin_nan("");
-        most = fmax(most, score[j]);
-    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) most = fmax(most, logits[j]);
     most = wave_max(most);
     double sum = 0.0;
-    for (int j = 0; j < kPerLane; ++j) {
-        rank[j] = score[j];
-        if (64 * j + lane < a.E) {
-            score[j] = sigmoid ? 1.0 / (1.0 + exp(-score[j])) : exp(score[j] - most);
-            sum += score[j];
-        }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        score[j] = sigmoid ? 1.0 / (1.0 + exp(-logits[j])) : exp(logits[j] - most);
+        if (64 * j + lane < a.E) sum += score[j];
     }
     sum = sigmoid ? 1.0 : wave_sum(sum);
-    for (int j = 0; j < kPerLane; ++j) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int e = 64 * j + lane;
         score[j] /= sum;
-        if (a.bias && 64 * j + lane < a.E) rank[j] = score[j] + (double)a.bias[64 * j + lane];
+        rank[j] = a.bias && e < a.E ? score[j] + (double)a.bias[e] : logits[j];
     }
     double chosen = 0.0, mine = 0.0;
     int32_t id = -1;
     for (int t = 0; t < a.top; ++t) {
         double best = -INFINITY;
-        for (int j = 0; j < kPerLane; ++j) best = fmax(best, rank[j]);     // (fmax passes over what is not a number: taken, or no expert)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) best = fmax(best, rank[j]);       // (passes over what is taken)
         best = wave_max(best);
         int e = -1;
         double s = 0.0;
-        for (int j = 0; j < kPerLane; ++j) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
             const uint64_t equal = __ballot(rank[j] == best);
             if (e < 0 && equal != 0) {
-                const int at = __builtin_ctzll(equal);
+                const int at = (int)__builtin_ctzll(equal);
+                const uint64_t b = __builtin_bit_cast(uint64_t, score[j]);
+                const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, at), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), at);
                 e = 64 * j + at;
-                s = __shfl(score[j], at);
+                s = __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
                 if (lane == at) rank[j] = __builtin_nan("");
             }
         }
@@ -84,36 +112,155 @@ __device__ void choose(const double* logits, const RouteArgs& a, int64_t m) {
     }
 }
 
-// A workgroup a token.
-__global__ __launch_bounds__(1024) void route_token_kernel(RouteArgs a) {
-    __shared__ double logits[ARCQ_MOE_MAX_EXPERTS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// A workgroup a token, its 16 waves in teams of `team` for an expert.
+template <int PER>
+__global__ __launch_bounds__(1024) void route_token_kernel(RouteArgs a, int team) {
+    __shared__ double part[16][64 * PER];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), run = wave % team;
     const int64_t m = blockIdx.x;
     const _Float16* x = a.x + m * a.ldx;
-    for (int e = wave; e < a.E; e += 16) {
+    for (int e = wave / team; e < a.E; e += 16 / team) {
         const _Float16* r = a.router + e * a.ldr;
         double sum = 0.0;
-        for (int k = 8 * lane; k < a.K; k += 512) {
+        for (int k = 8 * (64 * run + lane); k < a.K; k += 512 * team) {
             const half8 u = *reinterpret_cast<const half8*>(x + k), v = *reinterpret_cast<const half8*>(r + k);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += (double)((float)u[i] * (float)v[i]);
         }
         sum = wave_sum(sum);
-        if (lane == 0) logits[e] = sum;
+        if (lane == 0) part[run][e] = sum;
     }
     __syncthreads();
-    if (wave == 0) choose(logits, a, m);
+    if (wave != 0) return;
+    double logits[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int e = 64 * j + lane;
+        logits[j] = __builtin_nan("");
+        if (e < a.E) {
+            logits[j] = part[0][e];
+            for (int w = 1; w < team; ++w) logits[j] += part[w][e];
+        }
+    }
+    choose<PER>(logits, a, m);
+}
+
+// 16 tokens by 16 experts, one of `splits` runs of K, in four waves.  Lane (i, q) brings k = 32 c + 8 q .. + 7 of token i and of expert i: the s-th of
+// these of the four lane groups are a step of the matrix instruction.
+__global__ __launch_bounds__(256) void scores_kernel(RouteArgs a, uint32_t tiles_e, uint32_t tiles_m) {
+    __shared__ double part[4][256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    const uint32_t tile = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x % (uint32_t)a.splits;
+    const int m0 = 16 * (int)(tile / tiles_e), e0 = 16 * (int)(tile % tiles_e);
+    const _Float16* x = a.x + (int64_t)min(m0 + i, a.M - 1) * a.ldx;
+    const _Float16* r = a.router + (int64_t)min(e0 + i, a.E - 1) * a.ldr;
+    const int chunks = (a.K + 31) >> 5, runs = 4 * a.splits, run = 4 * (int)split + wave;
+    const int c0 = (int)((int64_t)run * chunks / runs), c1 = (int)((int64_t)(run + 1) * chunks / runs);
+    double4v acc = {0.0, 0.0, 0.0, 0.0};
+    constexpr int G = 4;                            // chunks asked for at once
+    for (int c = c0; c < c1; c += G) {
+        half8 u[G], v[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {               // (past the end: the last chunk again; pieces past the end of a row, its last one: counted as zeros)
+            const int k = min(32 * min(c + g, c1 - 1) + 8 * q, a.K - 8);
+            u[g] = *reinterpret_cast<const half8*>(x + k);
+            v[g] = *reinterpret_cast<const half8*>(r + k);
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (c + g >= c1) break;
+            if (32 * (c + g) + 8 * q >= a.K) u[g] = half8{0, 0, 0, 0, 0, 0, 0, 0}, v[g] = u[g];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(float)u[g][s], (double)(float)v[g][s], acc, 0, 0, 0);
+        }
+    }
+    // a lane has the sums of expert i and tokens q, q + 4, q + 8, q + 12
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[wave][16 * (4 * k + q) + i] = acc[k];
+    __syncthreads();
+    const int m = m0 + (tid >> 4), e = e0 + (tid & 15);
+    if (m < a.M && e < a.E) a.sums[((int64_t)split * a.M + m) * a.E + e] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+}
+
+// A wave a token.
+template <int PER>
+__global__ __launch_bounds__(256) void choose_kernel(RouteArgs a) {
+    const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (m >= a.M) return;
+    const int lane = threadIdx.x & 63;
+    double logits[PER];
+    constexpr int G = PER < 4 ? 8 : PER < 16 ? 4 : 2;       // runs asked for at once
+    const double* at = a.sums + m * a.E;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) logits[j] = 0.0;
+    for (int s = 0; s < a.splits; s += G) {
+        double v[G][PER];
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) v[g][j] = at[(int64_t)min(s + g, a.splits - 1) * a.M * a.E + min(64 * j + lane, a.E - 1)];
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) logits[j] += s + g < a.splits ? v[g][j] : 0.0;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (64 * j + lane >= a.E) logits[j] = __builtin_nan("");
+    choose<PER>(logits, a, m);
+}
+
+// Tokens of a launch: the workspace and grids stay within bounds for any number of them.
+constexpr int64_t kMostTokens = 4096;
+
+// Whether a workgroup a token is quickest: it reads all of the router's weights by itself.
+bool by_token(int64_t K, int64_t E) { return E <= 64 && K * E <= 65536; }
+
+// Runs of K: two workgroups a compute unit, with four chunks of 32 for each wave.
+int splits_of(int64_t M, int64_t K, int64_t E) {
+    const int64_t tiles = (M + 15) / 16 * ((E + 15) / 16);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(2 * 256 / tiles, K / 512));
+}
+
+template <int PER>
+arcq_status launch_choose(const RouteArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL(choose_kernel<PER>, dim3((unsigned)((a.M + 3) / 4)), dim3(256), 0, stream, a);
+    return check_launch("choose_kernel");
 }
 
 }  // namespace
 
-size_t moe_route_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t moe_route_workspace_bytes(int64_t M, int64_t K, int64_t E) {
+    if (by_token(K, E)) return 0;
+    M = std::min(M, kMostTokens);
+    return (size_t)splits_of(M, K, E) * (size_t)M * (size_t)E * sizeof(double);
+}
 
 arcq_status launch_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, const void* router, int64_t ldr, int64_t E, const float* bias, int64_t top,
-                             uint32_t flags, int32_t* ids, float* weights, void*, hipStream_t stream) {
-    const RouteArgs a = {static_cast<const _Float16*>(x), static_cast<const _Float16*>(router), ldx, ldr, bias, (int)M, (int)K, (int)E, (int)top, flags, ids, weights};
-    hipLaunchKernelGGL(route_token_kernel, dim3((unsigned)M), dim3(1024), 0, stream, a);
-    return check_launch("route_token_kernel");
+                             uint32_t flags, int32_t* ids, float* weights, void* workspace, hipStream_t stream) {
+    const int splits = splits_of(std::min(M, kMostTokens), K, E);       // (a last launch of fewer tokens has the runs of the first: there is room for those)
+    for (int64_t m = 0; m < M; m += kMostTokens) {
+        const int64_t rows = std::min(M - m, kMostTokens);
+        const RouteArgs a = {static_cast<const _Float16*>(x) + m * ldx, static_cast<const _Float16*>(router), ldx, ldr, bias, (int)rows, (int)K, (int)E, (int)top, flags,
+                             ids + m * top, weights + m * top, static_cast<double*>(workspace), splits};
+        if (by_token(K, E)) {
+            int team = 1;
+            while (2 * team * E <= 16 && 1024 * team <= K) team *= 2;
+            hipLaunchKernelGGL(route_token_kernel<1>, dim3((unsigned)rows), dim3(1024), 0, stream, a, team);
+            if (arcq_status st = check_launch("route_token_kernel")) return st;
+            continue;
+        }
+        const unsigned tiles_e = (unsigned)((E + 15) / 16), tiles_m = (unsigned)((rows + 15) / 16);
+        hipLaunchKernelGGL(scores_kernel, dim3(tiles_e * tiles_m * (unsigned)splits), dim3(256), 0, stream, a, tiles_e, tiles_m);
+        if (arcq_status st = check_launch("scores_kernel")) return st;
+        const arcq_status st = E <= 64    ? launch_choose<1>(a, stream)
+                               : E <= 128 ? launch_choose<2>(a, stream)
+                               : E <= 256 ? launch_choose<4>(a, stream)
+                               : E <= 512 ? launch_choose<8>(a, stream)
+                                          : launch_choose<16>(a, stream);
+        if (st) return st;
+    }
+    return ARCQ_OK;
 }
 
 }  // namespace arcq
