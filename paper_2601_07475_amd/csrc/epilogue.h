@@ -78,6 +78,27 @@ __device__ __forceinline__ float finish(const Epilogue<OutT>& e, float sum, int6
     return e.residual ? v[0] + r : v[0];
 }
 
+// The same in two steps: what it reads, early, and the rest.
+template <typename Ep>
+struct Operands {                                   // of NoEpilogue
+    __device__ __forceinline__ void ask(const Ep&, int64_t, int64_t) {}
+    __device__ __forceinline__ float finish(const Ep&, float sum) const { return sum; }
+};
+template <typename OutT>
+struct Operands<Epilogue<OutT>> {
+    _Float16 bias = (_Float16)0.0f;
+    OutT residual = (OutT)0.0f;
+    __device__ __forceinline__ void ask(const Epilogue<OutT>& e, int64_t m, int64_t n) {
+        if (e.bias) bias = e.bias[n];
+        if (e.residual) residual = e.residual[m * e.ldr + n];
+    }
+    __device__ __forceinline__ float finish(const Epilogue<OutT>& e, float sum) const {
+        float v[1] = {e.bias ? sum + (float)bias : sum};
+        activate(v, e.activation);
+        return e.residual ? v[0] + (float)residual : v[0];
+    }
+};
+
 // A wave's tile of 32 WM x 32 WN sums (accumulator layout as in store_tile_swapped), a fragment row of 32 at a time through the wave's region of LDS in
 // fp32: the bias on the way in, where a lane holds four columns side by side; the activation in place, in a loop whose body is there four times (unrolled over
 // the accumulator registers, four activations would fill the instruction cache); the residual on the way out, where a wave's loads and stores are

@@ -200,7 +200,20 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS
     // multiplied and added up.
     float* red = reinterpret_cast<float*>(lds + (X == WHOLE ? (uint32_t)rows * (uint32_t)K * 4u : (uint32_t)(WAVES * slice_bytes(ROWS, NT, WAVES))));
     uint32_t turn_red = 0;
+    // What the epilogue reads is asked for at the start of a tile: behind the next tile's weights it would wait for those.
+    constexpr int OUTS = (MT * NT * 256 + THREADS - 1) / THREADS;      // outputs of a thread
+    auto output = [&](int tile, int it, int& m, int& n) {
+        const int idx = tid + it * THREADS, rt = idx >> 8;
+        m = m0 + 16 * (rt / NT) + 4 * ((idx & 63) >> 4) + (idx >> 6 & 3), n = (tile * NT + rt % NT) * 16 + (idx & 15);
+        return idx < MT * NT * 256 && m < min(M, m0 + ROWS) && n < N;
+    };
     for (int tile = tile0; tile < tiles_n; tile += (int)stride) {
+        Operands<Ep> ends[OUTS];
+#pragma unroll
+        for (int it = 0; it < OUTS; ++it) {
+            int m, n;
+            if (output(tile, it, m, n)) ends[it].ask(ep, m, n);
+        }
         float4v acc[CH][MT][NT];
 #pragma unroll
         for (int c = 0; c < CH; ++c)
@@ -300,13 +313,15 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS
                     part[((wave * MT * NT + r * NT + t) * 4 + e) * 64 + lane] = CH == 2 ? acc[0][r][t][e] + acc[CH - 1][r][t][e] : acc[0][r][t][e];
         wait_lgkmcnt0();
         wg_barrier();                                   // not __syncthreads(): the next tile's weights stay in flight
-        for (int idx = tid; idx < MT * NT * 4 * 64; idx += THREADS) {
-            const int rt = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
+#pragma unroll
+        for (int it = 0; it < OUTS; ++it) {
+            int m, n;
+            const int idx = tid + it * THREADS, rt = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
+            if (!output(tile, it, m, n)) continue;
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) sum += part[(w * MT * NT * 4 + rt * 4 + e) * 64 + l];
-            const int m = m0 + 16 * (rt / NT) + 4 * (l >> 4) + e, n = (tile * NT + rt % NT) * 16 + (l & 15);
-            if (m < min(M, m0 + ROWS) && n < N) store_out(y + (int64_t)m * ldy + n, finish<OutT>(ep, sum * alpha, m, n));
+            store_out(y + (int64_t)m * ldy + n, ends[it].finish(ep, sum * alpha));
         }
     }
 }
