@@ -378,16 +378,17 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     // pieces of a chunk: rows r = 2 token + (0: high, 1: low), four a load, 16 lanes a row
     auto unit = [](int piece, int r) { return 16 * (2 * TOKENS * piece + (r ^ (piece & (2 * TOKENS - 1)))); };
     const uint8_t *wc = nullptr, *ws = nullptr;
-    uint32_t row[LOADS];                            // offsets from a.high
+    uint32_t row[LOADS], chunk[LOADS];              // offsets from a.high, and what a chunk adds to them
     const uint32_t low = (uint32_t)(a.low - a.high);
     auto take = [&](int nth) {                      // the expert whose weights are asked for next
         const int e = __builtin_amdgcn_readlane(active, nth);
         wc = codes_of(a.down, e, n0);
         ws = scales_of(a.down, e, n0);
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) {           // (rows of a token that does not choose it are some slot's: passed over)
+        for (int l = 0; l < LOADS; ++l) {           // (the row of a token that does not choose it is passed over: the same piece all the time)
             const int r = 4 * l + q, slot = slot_of[nth][r >> 1];
-            row[l] = ((r & 1) == 0 ? 0u : low) + (uint32_t)max(slot, 0) * (uint32_t)a.pitch + 8u * i;
+            row[l] = slot < 0 ? 0u : ((r & 1) == 0 ? 0u : low) + (uint32_t)slot * (uint32_t)a.pitch + 8u * i;
+            chunk[l] = slot < 0 ? 0u : 128u;
         }
     };
     u32x4 cw[G], rows[G][LOADS];
@@ -395,7 +396,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     auto ask_scales = [&](int g) { sc = of.scales(ws, min(G * g + q, per - 1)); };
     auto load_rows = [&](int c, u32x4 (&to)[LOADS]) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) to[l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + 128u * (uint32_t)c));
+        for (int l = 0; l < LOADS; ++l) to[l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + chunk[l] * (uint32_t)c));
     };
     auto ask_chunk = [&](int g, int d) {
         const int c = min(G * g + d, per - 1);
