@@ -132,8 +132,8 @@ __device__ __forceinline__ const uint8_t* codes_of(const Experts& w, int e, int6
 __device__ __forceinline__ const uint8_t* scales_of(const Experts& w, int e, int64_t row) { return w.scales + ((int64_t)e * w.rows + row) * w.scale_pitch; }
 
 // `count` chunks whose scales do not all fold, asked for only here, one at a time: rows(d, fragments), codes(d, tile).
-template <int B, int MT, int NT, typename Rows, typename Codes>
-__device__ __forceinline__ void block_by_block(int count, const uint32_t (&sw)[4][NT], const Rows& rows, const Codes& codes, float4v (&acc)[MT][NT]) {
+template <int B, int MT, int N, int NT, typename Rows, typename Codes>
+__device__ __forceinline__ void block_by_block(int count, const uint32_t (&sw)[N][NT], const Rows& rows, const Codes& codes, float4v (&acc)[MT][NT]) {
     if constexpr (B == 32) {
 #pragma unroll 1
         for (int d = 0; d < count; ++d) {
@@ -144,7 +144,7 @@ __device__ __forceinline__ void block_by_block(int count, const uint32_t (&sw)[4
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 words[t] = codes(d, t);
-                one[t] = d == 0 ? sw[0][t] : d == 1 ? sw[1][t] : d == 2 ? sw[2][t] : sw[3][t];
+                one[t] = d == 0 ? sw[0][t] : d == 1 ? sw[1][t] : d == 2 ? sw[2][t] : d == 3 ? sw[3][t] : sw[N - 1][t];
             }
             multiply_folded<B, false, MT>(xf, words, one, acc);
         }
@@ -256,10 +256,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
         }
     };
     u32x4 cw[G][2];
-    u32x2 sc[2];
-    auto ask_scales = [&](int g) {                  // lane group q: of the q-th chunk of the group
+    u32x2 sc[2], fifth[2];
+    auto ask_scales = [&](int g) {                  // lane group q: of the q-th chunk of the group; all lanes: of a fifth one
 #pragma unroll
-        for (int t = 0; t < 2; ++t) sc[t] = of.scales(ws[t], c0 + min(G * g + q, n - 1));
+        for (int t = 0; t < 2; ++t) {
+            sc[t] = of.scales(ws[t], c0 + min(G * g + q, n - 1));
+            if (G == 5) fifth[t] = of.scales(ws[t], c0 + min(G * g + 4, n - 1));
+        }
     };
     auto ask_codes = [&](int g, int d) {
 #pragma unroll
@@ -280,7 +283,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
         for (int g = 0; g < groups; ++g) {
             const bool over = g + 1 == groups;
             const int count = min(G, n - G * g), next = over ? 0 : g + 1, c = c0 + G * g;
-            uint32_t sw[4][2];
+            uint32_t sw[G < 4 ? 4 : G][2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const u32x2 v = of.whole(sc[t], c0 + min(G * g + q, n - 1));
@@ -288,6 +291,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
                 scales_of_group<B>(make_uint2(v[0], v[1]), s);
 #pragma unroll
                 for (int d = 0; d < 4; ++d) sw[d][t] = s[d];
+                if constexpr (G == 5) sw[4][t] = of.of_lane(of.whole(fifth[t], c0 + min(G * g + 4, n - 1)), q);
             }
             auto rows_of = [&](int d, half8 (&xf)[1][4]) {
 #pragma unroll
@@ -869,7 +873,10 @@ bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 6
 int waves_of(int chunks) { return chunks >= 32 ? 8 : chunks >= 16 ? 4 : 2; }
 int group_of(int chunks, int waves) {
     const int most = (chunks + waves - 1) / waves;
-    return (most + 2) / 3 * 3 < (most + 3) / 4 * 4 ? 3 : 4;
+    int best = 5;
+    for (const int g : {4, 3})
+        if ((most + g - 1) / g * g < (most + best - 1) / best * best) best = g;
+    return best;
 }
 
 // Runs of I for down_many_kernel.
@@ -901,8 +908,11 @@ arcq_status launch_up_slots(const UpArgs& u, int64_t items, hipStream_t stream) 
 template <int B, int KW>
 arcq_status launch_up_few(const UpArgs& u, int64_t items, hipStream_t stream) {
     const bool few = u.M * u.top <= 64;
-    if (group_of((u.K + 127) / 128, KW) == 3) return few ? launch_up_slots<B, KW, 3, 64>(u, items, stream) : launch_up_slots<B, KW, 3, 256>(u, items, stream);
-    return few ? launch_up_slots<B, KW, 4, 64>(u, items, stream) : launch_up_slots<B, KW, 4, 256>(u, items, stream);
+    switch (group_of((u.K + 127) / 128, KW)) {
+        case 3: return few ? launch_up_slots<B, KW, 3, 64>(u, items, stream) : launch_up_slots<B, KW, 3, 256>(u, items, stream);
+        case 4: return few ? launch_up_slots<B, KW, 4, 64>(u, items, stream) : launch_up_slots<B, KW, 4, 256>(u, items, stream);
+        default: return few ? launch_up_slots<B, KW, 5, 64>(u, items, stream) : launch_up_slots<B, KW, 5, 256>(u, items, stream);
+    }
 }
 
 template <int B, int TOKENS, int WAVES, typename OutT>
