@@ -207,7 +207,7 @@ __device__ __forceinline__ int distinct(const int16_t* ids, int slots, int16_t* 
 // G: chunks in flight.  SLOTS: most slots, 64 (experts in a wave's lanes) or 256 (in LDS).
 struct UpFewLds {
     float sums[8][2][4][64];                        // wave, G or U, element, lane
-    float weights[256];
+    float weights[256], scales[256];                // of a slot: its weight, and the tensor scale of its expert
     __attribute__((aligned(16))) int16_t ids[256];
     int16_t active[256];
     int counts[8];
@@ -224,15 +224,26 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     const int id = checked_id(a.ids, mine, slots, a.E);
     const float weight_of = mine < slots ? a.weights[mine] : 0.0f;
     const int chunks = (a.K + 127) >> 7, pieces = a.K >> 3, pitch = 256 * chunks + 16;      // (16 bytes more than whole chunks: rows spread over the banks)
-    for (int u = tid; u < 16 * chunks * a.M; u += 512) {                // (pieces past the end are zeros)
-        const int m = a.M == 1 ? 0 : u / (16 * chunks), p = u - m * 16 * chunks;
-        u32x4 v = {0, 0, 0, 0};
-        if (p < pieces) v = *reinterpret_cast<const u32x4*>(a.x + m * a.ldx + 8 * p);
-        *reinterpret_cast<u32x4*>(xs + m * pitch + 16 * p) = v;
+    const float scale_of = B == 16 && id >= 0 ? a.up.tensor_scales[id] : 1.0f / kFolded<B>;
+    constexpr int AT_ONCE = 8;                      // pieces of a thread on their way
+    const int per_row = 16 * chunks, all_pieces = per_row * a.M;
+    for (int u0 = tid; u0 < all_pieces; u0 += 512 * AT_ONCE) {          // (pieces past the end are zeros)
+        u32x4 v[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int u = min(u0 + 512 * k, all_pieces - 1), m = u / per_row, p = u - m * per_row;
+            v[k] = *reinterpret_cast<const u32x4*>(a.x + m * a.ldx + 8 * min(p, pieces - 1));
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int u = u0 + 512 * k, m = u / per_row, p = u - m * per_row;
+            if (u < all_pieces) *reinterpret_cast<u32x4*>(xs + m * pitch + 16 * p) = p < pieces ? v[k] : u32x4{0, 0, 0, 0};
+        }
     }
     if (tid < SLOTS) {
         l.ids[tid] = (int16_t)id;
         l.weights[tid] = weight_of;
+        l.scales[tid] = scale_of;
     }
     int actives, active = -1;
     if constexpr (SLOTS == 64) {
@@ -328,7 +339,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
         wg_barrier();
         if (item < all) {
             const int nth = item / a.tiles, e = expert_of(nth), n0 = 16 * (item - nth * a.tiles);
-            const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
             for (int idx = kw * 64 + lane; idx < 16 * a.M; idx += 64 * KW) {
                 const int m = idx >> 4, at = 16 * (m >> 2) + (idx & 15), k = m & 3;
                 int slot = -1;
@@ -342,6 +352,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
                 float g = 0.f, u = 0.f;
 #pragma unroll
                 for (int w = 0; w < KW; ++w) g += l.sums[team * KW + w][0][k][at], u += l.sums[team * KW + w][1][k][at];
+                const float alpha = l.scales[slot];
                 store_h(a, slot, n0 + (idx & 15), g * alpha, u * alpha, weight);
             }
         }
@@ -360,9 +371,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     int* ids_of = reinterpret_cast<int*>(lds + sizeof(sums));
     int8_t(&slot_of)[64][8] = *reinterpret_cast<int8_t(*)[64][8]>(lds + sizeof(sums) + 256);       // of an active expert and a token; -1: it does not choose it
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    uint8_t* slice = lds + sizeof(sums) + 256 + 512 + wave * TOKENS * 512;
+    float* scales_of_slots = reinterpret_cast<float*>(lds + sizeof(sums) + 256 + 512);
+    uint8_t* slice = lds + sizeof(sums) + 256 + 512 + 256 + wave * TOKENS * 512;
     const int slots = a.M * a.top, id = checked_id(a.ids, lane, slots, a.E);
-    if (wave == 0) ids_of[lane] = id;
+    if (wave == 0) {
+        ids_of[lane] = id;
+        scales_of_slots[lane] = B == 16 && id >= 0 ? a.down.tensor_scales[id] * kUnit : kUnit / kFolded<B>;
+    }
     for (int k = lane; k < 128; k += 64) (&sums[wave][0][0])[k] = 0.0f;
     int actives;
     const int active = distinct(id, actives);
@@ -456,13 +471,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
                 for (int d = 0; d < G; ++d) ask_chunk(next, d);
             }
             if (over || end) {
-                const float alpha = B == 16 ? a.down.tensor_scales[__builtin_amdgcn_readlane(active, nth)] * kUnit : kUnit / kFolded<B>;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     // lanes of the first half hold sums of high numbers, those of the second of low ones of the same rows
                     const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][0][k]), __float_as_uint(acc[0][0][k]), false, false);
                     const float sum = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
-                    if (lane < 32 && slot_of[nth][4 * q + k] >= 0) sums[wave][4 * q + k][i] += sum * alpha;
+                    const int slot = lane < 32 ? slot_of[nth][4 * q + k] : -1;
+                    if (slot >= 0) sums[wave][4 * q + k][i] += sum * scales_of_slots[slot];
                 }
                 clear<1, 1>(acc);
                 ++nth;
@@ -574,13 +589,14 @@ __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E,
 struct Item {
     const uint16_t* from;                       // the row that this thread copies pieces of 8 k of: piece tid % 16 of a chunk, row (tid / 16) % (16 MT)
     const uint8_t *wc[2], *ws[2];               // the wave's tiles
+    float scale;                                // of the weights
     int c0, c1;                                 // chunks
     bool two;                                   // rows behind the first 16 are in use
 };
 
 // Items of a launch in turn.  Rows reach all waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  (With 16 rows half of the threads copy
 // every other chunk.)  Rows and weights of the next stage, or of the next item's first, are asked for in this one, rows first: they are needed first, and
-// loads return in order.  take(n): the n-th; store(n, sums).
+// loads return in order.  take(n): the n-th; store(n, its scale, sums).
 constexpr int kStage = 4;
 template <int MT>
 constexpr int kRowBytes = kStage * MT * 4096;   // of a buffer
@@ -629,7 +645,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
             multiply_folded<B, B == 16, MT>(xf, words, sw, acc);
-            store(item, acc);
+            store(item, now.scale, acc);
             __syncthreads();
         }
         return;
@@ -668,6 +684,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
     for (int item = begin; item < end; item += stride) {
         const int c0 = ahead.c0, c1 = ahead.c1;
         const bool two = ahead.two;
+        const float scale = ahead.scale;
         float4v acc[MT][NT];
         clear<MT, NT>(acc);
         for (int c = c0; c < c1; c += G) {
@@ -724,7 +741,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
             wait_lgkmcnt0();
             wg_barrier();                           // not __syncthreads(): loads stay in flight
         }
-        store(item, acc);
+        store(item, scale, acc);
     }
 }
 
@@ -772,14 +789,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
             v.wc[t] = codes_of(a.up, e, t * a.I + 16 * tile);
             v.ws[t] = scales_of(a.up, e, t * a.I + 16 * tile);
         }
+        v.scale = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
         v.c0 = 0, v.c1 = chunks;
         v.two = left > 16;
         return v;
     };
-    auto store = [&](int item, const float4v (&acc)[MT][2]) {
+    auto store = [&](int item, float alpha, const float4v (&acc)[MT][2]) {
         const Place place = place_of<16 * MT>(l, item, groups);
         const int e = place.expert, left = place.left, first = place.first, tile = tile_of(place.piece);
-        const float alpha = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
@@ -819,13 +836,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
             v.ws[t] = scales_of(a.down, e, min(n0 + 16 * t, last));
         }
         v.c0 = split * chunks / a.splits, v.c1 = (split + 1) * chunks / a.splits;
+        v.scale = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
         v.two = left > 8;
         return v;
     };
-    auto store = [&](int item, const float4v (&acc)[MT][2]) {
+    auto store = [&](int item, float alpha, const float4v (&acc)[MT][2]) {
         const Place place = place_of<8 * MT>(l, item, pieces);
-        const int e = place.expert, left = place.left, first = place.first, split = place.piece / a.groups, n0 = col_of(place.piece - split * a.groups);
-        const float alpha = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
+        const int left = place.left, first = place.first, split = place.piece / a.groups, n0 = col_of(place.piece - split * a.groups);
         float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
 #pragma unroll
         for (int r = 0; r < MT; ++r)
@@ -920,7 +937,7 @@ arcq_status launch_down_waves(const DownArgs<OutT>& d, hipStream_t stream) {
     auto kern = down_few_kernel<B, TOKENS, WAVES, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256 + 512, stream, d);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256 + 512 + 256, stream, d);
     return check_launch("down_few_kernel");
 }
 

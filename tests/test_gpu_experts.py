@@ -48,6 +48,13 @@ def test_router(M, K, E, top):
             check_route(x, r, top, b, flags, extra=flags)
 
 
+@pytest.mark.parametrize("M,K,E,top", [(5000, 32, 8, 2), (4099, 64, 70, 3)])
+def test_router_of_many_tokens(M, K, E, top):
+    say(f"router M={M} K={K} E={E}")
+    rng = np.random.default_rng(M)
+    check_route(rng.standard_normal((M, K)).astype(np.float16), rng.standard_normal((E, K)).astype(np.float16), top, None, B.MOE_RENORMALIZE)
+
+
 def test_router_ties():
     """Sums that are equal exactly: the lower index first, among many and among all."""
     say("router, ties")
@@ -176,6 +183,58 @@ def test_experts(fmt, M, K, I, N, E, top):
     check(fmt, M, K, I, N, E, top, S=block * (which % 3 % (K // block + 1)), S2=block * (which % 2), act=L.NAMES[which % 5], residual=which % 2 == 0,
           dtype=torch.float16 if which % 4 < 2 else torch.float32, in_place=which % 4 == 2)
     check(fmt, M, K, I, N, E, top, act="silu", residual=which % 2 == 1, reorder=True, drop=True, dtype=torch.float32 if which % 4 < 2 else torch.float16, seed=1)
+
+
+# up to 64 and up to 256 choices of up to 16 tokens, K in two, four and eight parts of whole and broken groups of three, four and five chunks; too many tokens for that
+@pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
+@pytest.mark.parametrize("K", [256, 1024, 1184, 1280, 1760, 2048, 2304, 2816, 3552, 4096, 4640, 6144, 8160])
+@pytest.mark.parametrize("M,top", [(3, 2), (9, 8)])
+def test_long_rows(fmt, K, M, top):
+    check(fmt, M, K, 48 if fmt == "nvfp4" else 64, 17, 10, top, S=32 * (K % 3), act="gelu", dtype=torch.float32, drop=True)
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
+@pytest.mark.parametrize("M,K,I,N,E,top", [(16, 4608, 160, 40, 4, 2), (14, 128, 32, 40, 4, 2), (16, 256, 128, 33, 20, 16),       # gathered, 16 rows at a time; 256 choices
+                                           (1, 64, 160, 4112, 3, 2), (3, 64, 416, 5000, 2, 2), (7, 64, 544, 4112, 2, 1),        # columns for half as many waves a workgroup
+                                           (5, 256, 2080, 40, 20, 16), (2, 128, 96, 40, 3, 2), (8, 64, 1056, 300, 2, 2),        # slots by themselves, in runs of I and not
+                                           (40, 64, 4128, 33, 3, 1), (20, 96, 2080, 600, 2, 2),
+                                           (67, 288, 160, 40, 4, 2), (81, 512, 288, 40, 4, 4), (129, 256, 1056, 24, 3, 2)])     # last tokens of another kind than the first
+def test_kinds(fmt, M, K, I, N, E, top):
+    check(fmt, M, K, I, N, E, top, S=32, S2=32, residual=True, dtype=torch.float32, in_place=True)
+    check(fmt, M, K, I, N, E, top, reorder=True, drop=True, residual=True)
+
+
+@pytest.mark.parametrize("M,K,I,N,E,top", [(2, 1184, 288, 40, 3, 2), (3, 2304, 672, 20, 2, 2), (7, 4640, 1056, 20, 2, 1), (9, 2816, 160, 20, 9, 8), (16, 4608, 288, 20, 2, 1), (12, 160, 544, 20, 2, 2),
+                                           (40, 672, 1184, 40, 3, 2), (5, 416, 2080, 24, 20, 16)])
+def test_scales_far_apart(M, K, I, N, E, top):
+    """MXFP4 blocks that no 16-bit code can take the scale of, here and there and in a row's last blocks."""
+    rng = np.random.default_rng(K)
+    say(f"moe, scales far apart {M} {K} {I}")
+    x = rng.standard_normal((M, K)).astype(np.float16)
+    up, down = random_experts("mx", E, 2 * I, K, 32, rng), random_experts("mx", E, N, I, 0, rng)
+    for s in (up[1], down[1]):
+        s[rng.random(s.shape) < 0.02] = 80
+        s[rng.random(s.shape) < 0.01] = 128
+        s[:, ::3, -2:] = 94
+        s[0, 1::4] = np.maximum(s[0, 1::4], 97)
+    ids, w = choices(rng, M, E, top, False)
+    want, off = L.experts(x, None, ids, w, up, down)
+    assert_within(call("mx", dev(x), None, ids, w, up, down, out_dtype=torch.float32), want, off)
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
+def test_tokens_that_are_not_finite(fmt):
+    """A token with NaN or infinities in it changes no other token's result."""
+    say("moe, inf and nan", fmt)
+    rng = np.random.default_rng(8)
+    for M, K, I, top in ((2, 512, 160, 2), (7, 1024, 288, 1), (12, 512, 96, 2), (40, 256, 288, 2)):
+        up, down = ([dev(t) if t is not None else None for t in random_experts(fmt, 3, r, k, 0, rng)] for r, k in ((2 * I, K), (40, I)))
+        x = dev(rng.standard_normal((M, K)).astype(np.float16))
+        ids, w = (dev(t) for t in choices(rng, M, 3, top, False))
+        want = call(fmt, x, None, ids, w, up, down, out_dtype=torch.float32)
+        x[0, 5], x[0, 9], x[0, K - 1] = float("nan"), float("inf"), float("-inf")
+        got = call(fmt, x, None, ids, w, up, down, out_dtype=torch.float32)
+        assert torch.equal(got[1:], want[1:]) and not bool(torch.isfinite(got[0]).any())
 
 
 @pytest.mark.parametrize("fmt", ["nvfp4", "mx"])
