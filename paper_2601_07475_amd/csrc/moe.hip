@@ -1,20 +1,25 @@
-// The experts of a mixture for a few tokens, on packed 4-bit weights, as two kernels:
-//   h[m, j] = w[m, j] act(x[m] G_e^T) (x[m] U_e^T)        e = ids[m, j]            up_kernel
-//   y[m]    = sum_j h[m, j] D_e^T + residual[m]                                    down_kernel
+// The experts of a mixture for a few tokens, on packed 4-bit weights:
+//   h[m, j] = w[m, j] act(x[m] G_e^T) (x[m] U_e^T)        e = ids[m, j]            up_few_kernel or up_many_kernel
+//   y[m]    = sum_j h[m, j] D_e^T + residual[m]                                    down_few_kernel, or down_many_kernel and join_kernel
 // x fp16, G over U the 2 I rows of an expert's first operand, D its second; NVFP4 (B = 16) or MXFP4 (B = 32).
 //
-// Bound by reading the chosen experts' weights once (3 K I weights each, 9/16 or 17/32 byte a weight).  Tokens are a row tile of v_mfma_f32_16x16x32_f16, so
-// up to 16 (8 behind the activation) cost what one does.
+// Bound by reading the chosen experts' weights once (3 K I weights each, 9/16 or 17/32 byte a weight).  Tokens are rows of v_mfma_f32_16x16x32_f16's tile, so
+// up to 16 (8 behind the activation) cost what one does.  Two launches, because every column of h depends on all of x and every column of y on all of h; what
+// a launch that waits for another costs by itself, start, choices and the first trip to memory, is 5 to 6 us, and with few bytes that is most of the time.
 //
-// Every workgroup finds out by itself which tokens choose an expert (lists_of): no kernel in front, and none that waits for the host.  An expert that a token
-// names twice counts once, with both weights: lists then hold a token once, and sums do not depend on the order of a list.
+// Every workgroup finds out by itself which tokens choose an expert: no kernel in front, and none that waits for the host.  An expert that a token
+// names twice counts once, with both weights: a token is then in a list once, and sums do not depend on the order of a list.
 //
 // h is held as two fp16 numbers, h / 16 rounded and 2^11 times what that leaves: 22 bits of h down to 2^-10, 2^-32 below it, up to 2^20.  (One fp16 number would put
 // its rounding, 2^-12, behind an fp32 y.)  The two are rows i and i + 8 of one row tile, so the second costs no more matrix instructions than the tile's
 // free rows; the halves of a wave hold the sums of either and are put together when a wave is done with an expert.
 //
-// down_kernel's reduction runs over all chosen experts' channels one after the other, in equal shares for the waves of a workgroup; a wave adds what it has of an
-// expert to its own sums of all tokens in LDS, and the waves' sums are added in their order at the end.  No atomics: the same inputs give the same bits.
+// No atomics on results, and every sum in an order that the sizes and choices fix: the same inputs give the same bits.
+//
+// Measured (weights not in cache; us of the two products, and TB/s of the chosen experts' weights over both, where a plain read of as many bytes reaches 6.2):
+//   one token, eight of 64, 2048 x 1024, MXFP4      10 +   9   1.6       one token, two of eight, 4096 x 14336, NVFP4    30 +  22   3.9
+//   four, eight of 128, 4096 x 1792, MXFP4          52 +  37   4.0       13, four of 30, 5120 x 1392, NVFP4, fp32 y      57 +  35   2.9
+//   64, two of eight, 4096 x 14336, MXFP4          129 +  95   3.5
 #include "epilogue.h"
 #include "internal.h"
 #include "lds_dma.h"
@@ -204,7 +209,7 @@ __device__ __forceinline__ int distinct(const int16_t* ids, int slots, int16_t* 
 // All tokens are rows of one tile, for every expert, so no list of an expert's tokens is needed: what comes out for one that does not choose it is passed over.
 // They lie in LDS.  A tile of 16 columns of an expert, that is 16 rows of G and of U, is for KW waves, which split K; workgroups, one on a compute unit, take
 // such a tile for each of their 8 / KW teams after the other, and ask for the next one's weights while they multiply and add up this one's.
-// G: chunks in flight.  SLOTS: most slots, 64 (experts in a wave's lanes) or 256 (in LDS).
+// G: chunks in flight (a ring of two such groups was no faster).  SLOTS: most slots, 64 (experts in a wave's lanes) or 256 (in LDS).
 struct UpFewLds {
     float sums[8][2][4][64];                        // wave, G or U, element, lane
     float weights[256], scales[256];                // of a slot: its weight, and the tensor scale of its expert
@@ -597,6 +602,8 @@ struct Item {
 // Items of a launch in turn.  Rows reach all waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  (With 16 rows half of the threads copy
 // every other chunk.)  Rows and weights of the next stage, or of the next item's first, are asked for in this one, rows first: they are needed first, and
 // loads return in order.  take(n): the n-th; store(n, its scale, sums).
+// 32 rows an item (16 slots behind the activation): with 16, two workgroups a compute unit, 64 tokens of eight of 64 experts took 113 us and not 104; with 64,
+// 64 tokens of two of eight 1.5 % less, 32 tokens 2 % more, since the rows' matrix work and reads of LDS are what an item's time is then.
 constexpr int kStage = 4;
 template <int MT>
 constexpr int kRowBytes = kStage * MT * 4096;   // of a buffer
