@@ -16,10 +16,12 @@
 //
 // No atomics on results, and every sum in an order that the sizes and choices fix: the same inputs give the same bits.
 //
-// Measured (weights not in cache; us of the two products, and TB/s of the chosen experts' weights over both, where a plain read of as many bytes reaches 6.2):
-//   one token, eight of 64, 2048 x 1024, MXFP4      10 +   9   1.6       one token, two of eight, 4096 x 14336, NVFP4    30 +  22   3.9
-//   four, eight of 128, 4096 x 1792, MXFP4          52 +  37   4.0       13, four of 30, 5120 x 1392, NVFP4, fp32 y      57 +  35   2.9
-//   64, two of eight, 4096 x 14336, MXFP4          129 +  95   3.5
+// Measured (us of a call whose weights are not in cache, TB/s of the chosen experts' weights, where a plain read reaches 6.2, and us of the two products alone):
+//   one token, eight of 64, 2048 x 1024, MXFP4              17   1.6     9 +   9
+//   one token, two of eight, 4096 x 14336, NVFP4            51   3.9    25 +  18 (weights in part cached)
+//   four tokens, eight of 128, 4096 x 1792, MXFP4           84   3.5    49 +  36
+//   13 tokens, four of 30, 5120 x 1392, NVFP4, fp32 y       91   2.8    54 +  34, reordering 2 to 4, joining 4
+//   64 tokens, two of eight, 4096 x 14336, MXFP4           209   3.6   125 + 100, joining 4
 #include "epilogue.h"
 #include "internal.h"
 #include "lds_dma.h"
