@@ -514,6 +514,7 @@ struct Lists {
     __attribute__((aligned(16))) int16_t first[kMostSlots];      // the same without a token's later choices of an expert: those count with the first
     uint16_t expert[kMostSlots], begin[kMostSlots];     // of a block: its expert, and the first of that expert's slots
     uint32_t fill[kMostExperts];
+    float weight[kMostSlots];                   // by slot, where asked for: all that a token's choices of an expert weigh, at the first
     int blocks;
 };
 
@@ -529,9 +530,9 @@ __device__ __forceinline__ int sum_before(int n) {
     return sum - n;
 }
 
-// All threads of the workgroup.  An expert's slots are in ascending order: every workgroup has the same blocks.
+// All threads of the workgroup.  An expert's slots are in ascending order: every workgroup has the same blocks.  weights: or null
 template <int THREADS, int ROWS>
-__device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E, Lists& l) {
+__device__ void lists_of(const int32_t* __restrict__ ids, const float* __restrict__ weights, int M, int top, int E, Lists& l) {
     const int tid = threadIdx.x, slots = M * top;
     constexpr int PER = (kMostSlots + THREADS - 1) / THREADS;
     int id[PER], at[PER];
@@ -550,6 +551,12 @@ __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E,
             if (l.id[u] == id[p]) id[p] = -1;
         if (t < kMostSlots) l.first[t] = (int16_t)id[p];
         if (id[p] >= 0) atomicAdd(&l.fill[id[p]], 1u);
+        if (id[p] >= 0 && weights) {
+            float weight = weights[t];
+            for (int u = t + 1; u < t - t % top + top; ++u)
+                if (l.id[u] == id[p]) weight += weights[u];
+            l.weight[t] = weight;
+        }
     }
     __syncthreads();
     // a slot's place: how many before it have its expert, eight ids a read
@@ -592,6 +599,18 @@ __device__ void lists_of(const int32_t* __restrict__ ids, int M, int top, int E,
     __syncthreads();
 }
 
+// Where an item is: blocks of an expert over the same weights are next to each other, so that those come from memory once.
+struct Place {
+    int expert, first, left, piece;             // the first of the expert's slots in the list, and how many from there on; which of `pieces` pieces of its weights
+};
+template <int ROWS>
+__device__ __forceinline__ Place place_of(const Lists& l, int item, int pieces) {
+    const int some = item / pieces, e = __builtin_amdgcn_readfirstlane(l.expert[some]), begin = __builtin_amdgcn_readfirstlane(l.begin[some]);
+    const int count = __builtin_amdgcn_readfirstlane(l.count[e]), start = __builtin_amdgcn_readfirstlane(l.start[e]);
+    const int blocks = (count + ROWS - 1) / ROWS, local = item - (some - begin / ROWS) * pieces, piece = local / blocks, r0 = (local - piece * blocks) * ROWS;
+    return {e, start + r0, count - r0, piece};
+}
+
 // A workgroup's piece of work: a block of an expert's slots with the eight waves' tiles of weights, two each, over a run of the reduction.
 struct Item {
     const uint16_t* from;                       // the row that this thread copies pieces of 8 k of: piece tid % 16 of a chunk, row (tid / 16) % (16 MT)
@@ -599,11 +618,12 @@ struct Item {
     float scale;                                // of the weights
     int c0, c1;                                 // chunks
     bool two;                                   // rows behind the first 16 are in use
+    Place place;
 };
 
 // Items of a launch in turn.  Rows reach all waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  (With 16 rows half of the threads copy
 // every other chunk.)  Rows and weights of the next stage, or of the next item's first, are asked for in this one, rows first: they are needed first, and
-// loads return in order.  take(n): the n-th; store(n, its scale, sums).
+// loads return in order.  take(n): the n-th; store(its place, its scale, sums).
 // 32 rows an item (16 slots behind the activation): with 16, two workgroups a compute unit, 64 tokens of eight of 64 experts took 113 us and not 104; with 64,
 // 64 tokens of two of eight 1.5 % less, 32 tokens 2 % more, since the rows' matrix work and reads of LDS are what an item's time is then.
 constexpr int kStage = 4;
@@ -654,7 +674,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
             multiply_folded<B, B == 16, MT>(xf, words, sw, acc);
-            store(item, now.scale, acc);
+            store(now.place, now.scale, acc);
             __syncthreads();
         }
         return;
@@ -694,6 +714,9 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
         const int c0 = ahead.c0, c1 = ahead.c1;
         const bool two = ahead.two;
         const float scale = ahead.scale;
+        const Place place = ahead.place;
+        Item after;                                 // found out where loads are on their way, not where some are to be asked for
+        bool known = false;
         float4v acc[MT][NT];
         clear<MT, NT>(acc);
         for (int c = c0; c < c1; c += G) {
@@ -720,11 +743,15 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
                                       [&](int d, int t) { return of.whole(of.codes(ahead.wc[t], c + d), c + d); }, acc);
             int next = c + G;
             if (next >= c1) {
-                ahead = take(item + stride < end ? item + stride : item);
+                ahead = known ? after : take(item + stride < end ? item + stride : item);
                 next = ahead.c0;
             }
             ask_rows(next);
             ask_scales(next);
+            if (MT > 1 && c == c0 && c + G < c1) {      // (with MT = 1 registers do not allow it)
+                after = take(item + stride < end ? item + stride : item);
+                known = true;
+            }
             auto multiply = [&](auto tiles) {
 #pragma unroll
                 for (int d = 0; d < G; ++d) {
@@ -750,7 +777,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
             wait_lgkmcnt0();
             wg_barrier();                           // not __syncthreads(): loads stay in flight
         }
-        store(item, scale, acc);
+        store(place, scale, acc);
     }
 }
 
@@ -766,25 +793,13 @@ __device__ __forceinline__ Share share_of(int all) {
     return {x0 + wg / XCDS, x1, of_xcd};
 }
 
-// Where an item is: blocks of an expert over the same weights are next to each other, so that those come from memory once.
-struct Place {
-    int expert, first, left, piece;             // the first of the expert's slots in the list, and how many from there on; which of `pieces` pieces of its weights
-};
-template <int ROWS>
-__device__ __forceinline__ Place place_of(const Lists& l, int item, int pieces) {
-    const int some = item / pieces, e = __builtin_amdgcn_readfirstlane(l.expert[some]), begin = __builtin_amdgcn_readfirstlane(l.begin[some]);
-    const int count = __builtin_amdgcn_readfirstlane(l.count[e]), start = __builtin_amdgcn_readfirstlane(l.start[e]);
-    const int blocks = (count + ROWS - 1) / ROWS, local = item - (some - begin / ROWS) * pieces, piece = local / blocks, r0 = (local - piece * blocks) * ROWS;
-    return {e, start + r0, count - r0, piece};
-}
-
 // An item: 128 columns of an expert for up to 16 MT of its tokens; a wave has 16 rows of G and of U.
 template <int B, int MT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4 : 2, 4))) void up_many_kernel(UpArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    lists_of<512, 16 * MT>(a.ids, a.M, a.top, a.E, l);
+    lists_of<512, 16 * MT>(a.ids, a.weights, a.M, a.top, a.E, l);
     const int groups = (a.tiles + 7) >> 3, chunks = (a.K + 127) >> 7;
     const Row<B> of(i, q, a.K, a.up.code_pitch, a.up.scale_pitch);
     auto tile_of = [&](int group) { return min(8 * group + wave, a.tiles - 1); };       // (waves past the last tile repeat it)
@@ -801,11 +816,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
         v.scale = B == 16 ? a.up.tensor_scales[e] : 1.0f / kFolded<B>;
         v.c0 = 0, v.c1 = chunks;
         v.two = left > 16;
+        v.place = at;
         return v;
     };
-    auto store = [&](int item, float alpha, const float4v (&acc)[MT][2]) {
-        const Place place = place_of<16 * MT>(l, item, groups);
-        const int e = place.expert, left = place.left, first = place.first, tile = tile_of(place.piece);
+    auto store = [&](const Place& place, float alpha, const float4v (&acc)[MT][2]) {
+        const int left = place.left, first = place.first, tile = tile_of(place.piece);
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
@@ -813,10 +828,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
                 const int at = 16 * r + 4 * q + k;
                 if (at >= left) continue;
                 const int slot = l.slots[first + at];
-                float weight = a.weights[slot];
-                for (int s = slot + 1; s % a.top != 0; ++s)             // the same expert again
-                    if (l.id[s] == e) weight += a.weights[s];
-                store_h(a, slot, 16 * tile + i, acc[r][0][k] * alpha, acc[r][1][k] * alpha, weight);
+                store_h(a, slot, 16 * tile + i, acc[r][0][k] * alpha, acc[r][1][k] * alpha, l.weight[slot]);
             }
     };
     const Share mine = share_of(l.blocks * groups);
@@ -829,7 +841,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    lists_of<512, 8 * MT>(a.ids, a.M, a.top, a.E, l);
+    lists_of<512, 8 * MT>(a.ids, nullptr, a.M, a.top, a.E, l);
     const int chunks = (a.I + 127) >> 7, pieces = a.groups * a.splits, last = a.N < 16 ? 0 : a.N - 16;
     const Row<B> of(min(i, a.N - 1), q, a.I, a.down.code_pitch, a.down.scale_pitch);
     auto col_of = [&](int group) { return 32 * (8 * group + wave); };
@@ -847,10 +859,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
         v.c0 = split * chunks / a.splits, v.c1 = (split + 1) * chunks / a.splits;
         v.scale = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
         v.two = left > 8;
+        v.place = at;
         return v;
     };
-    auto store = [&](int item, float alpha, const float4v (&acc)[MT][2]) {
-        const Place place = place_of<8 * MT>(l, item, pieces);
+    auto store = [&](const Place& place, float alpha, const float4v (&acc)[MT][2]) {
         const int left = place.left, first = place.first, split = place.piece / a.groups, n0 = col_of(place.piece - split * a.groups);
         float* out = a.partial + (int64_t)split * a.M * a.top * a.N;
 #pragma unroll
