@@ -214,9 +214,10 @@ __device__ __forceinline__ int distinct(const int16_t* ids, int slots, int16_t* 
 // G: chunks in flight (a ring of two such groups was no faster).  SLOTS: most slots, 64 (experts in a wave's lanes) or 256 (in LDS).
 struct UpFewLds {
     float sums[8][2][4][64];                        // wave, G or U, element, lane
-    float weights[256], scales[256];                // of a slot: its weight, and the tensor scale of its expert
+    float weights[256], scales[256];                // of a slot: its weight (a token's first choice of an expert: all of them), and the tensor scale of its expert
     __attribute__((aligned(16))) int16_t ids[256];
     int16_t active[256];
+    int8_t choice[256][16];                         // of an active expert and a token: the first of its choices that is this expert, -1 for none
     int counts[8];
 };
 template <int B, int KW, int G, int SLOTS>
@@ -295,6 +296,22 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     for (int d = 0; d < G; ++d) ask_codes(0, d);
     wait_lgkmcnt0();
     wg_barrier();                                   // not __syncthreads(): the weights stay in flight
+    // which token chooses which expert, once and not for every tile; what is written here is read behind the first round's barriers
+    for (int k0 = 64 * wave; k0 < 16 * actives; k0 += 512) {
+        const int nth = (k0 + lane) >> 4, m = lane & 15;
+        const int e = SLOTS == 64 ? __shfl(active, nth & 63) : l.active[min(nth, actives - 1)];        // (every lane takes part)
+        int choice = -1;
+        float weight = 0.0f;
+        if (m < a.M && nth < actives) {
+            for (int j = 0; j < a.top; ++j)
+                if (l.ids[m * a.top + j] == e) {
+                    choice = choice < 0 ? j : choice;
+                    weight += l.weights[m * a.top + j];
+                }
+            if (choice >= 0) l.weights[m * a.top + choice] = weight;
+        }
+        if (nth < actives) l.choice[nth][m] = (int8_t)choice;
+    }
     for (int round = 0; round < rounds; ++round, item += stride) {
         float4v acc[1][2];
         clear<1, 2>(acc);
@@ -345,22 +362,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
         wait_lgkmcnt0();
         wg_barrier();
         if (item < all) {
-            const int nth = item / a.tiles, e = expert_of(nth), n0 = 16 * (item - nth * a.tiles);
+            const int nth = item / a.tiles, n0 = 16 * (item - nth * a.tiles);
             for (int idx = kw * 64 + lane; idx < 16 * a.M; idx += 64 * KW) {
                 const int m = idx >> 4, at = 16 * (m >> 2) + (idx & 15), k = m & 3;
-                int slot = -1;
-                float weight = 0.0f;
-                for (int j = 0; j < a.top; ++j)
-                    if (l.ids[m * a.top + j] == e) {
-                        slot = slot < 0 ? m * a.top + j : slot;
-                        weight += l.weights[m * a.top + j];
-                    }
-                if (slot < 0) continue;
+                const int choice = l.choice[nth][m], slot = m * a.top + choice;
+                if (choice < 0) continue;
                 float g = 0.f, u = 0.f;
 #pragma unroll
                 for (int w = 0; w < KW; ++w) g += l.sums[team * KW + w][0][k][at], u += l.sums[team * KW + w][1][k][at];
                 const float alpha = l.scales[slot];
-                store_h(a, slot, n0 + (idx & 15), g * alpha, u * alpha, weight);
+                store_h(a, slot, n0 + (idx & 15), g * alpha, u * alpha, l.weights[slot]);
             }
         }
         wait_lgkmcnt0();                            // (reads of the sums have come back before the next barrier)
