@@ -18,10 +18,10 @@
 //
 // Measured (us of a call whose weights are not in cache, TB/s of the chosen experts' weights, where a plain read reaches 6.2, and us of the two products alone):
 //   one token, eight of 64, 2048 x 1024, MXFP4              17   1.6     9 +   9
-//   one token, two of eight, 4096 x 14336, NVFP4            51   3.9    25 +  18 (weights in part cached)
+//   one token, two of eight, 4096 x 14336, NVFP4            51   3.9    24 +  18 (weights in part cached)
 //   four tokens, eight of 128, 4096 x 1792, MXFP4           84   3.5    49 +  36
-//   13 tokens, four of 30, 5120 x 1392, NVFP4, fp32 y       91   2.8    54 +  34, reordering 2 to 4, joining 4
-//   64 tokens, two of eight, 4096 x 14336, MXFP4           209   3.6   125 + 100, joining 4
+//   13 tokens, four of 30, 5120 x 1392, NVFP4, fp32 y       89   2.8    54 +  34, reordering 2 to 4, joining 4
+//   64 tokens, two of eight, 4096 x 14336, MXFP4           201   3.7   118 + 102, joining 4
 #include "epilogue.h"
 #include "internal.h"
 #include "lds_dma.h"
@@ -635,7 +635,7 @@ struct Item {
 // Items of a launch in turn.  Rows reach all waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  (With 16 rows half of the threads copy
 // every other chunk.)  Rows and weights of the next stage, or of the next item's first, are asked for in this one, rows first: they are needed first, and
 // loads return in order.  take(n): the n-th; store(its place, its scale, sums).
-// 32 rows an item (16 slots behind the activation): with 16, two workgroups a compute unit, 64 tokens of eight of 64 experts took 113 us and not 104; with 64,
+// 32 rows an item (16 slots behind the activation): with 16, two workgroups a compute unit, 64 tokens of eight of 64 experts took 113 us and not 100; with 64,
 // 64 tokens of two of eight 1.5 % less, 32 tokens 2 % more, since the rows' matrix work and reads of LDS are what an item's time is then.
 constexpr int kStage = 4;
 template <int MT>
