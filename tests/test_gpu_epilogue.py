@@ -161,6 +161,13 @@ def test_more_rows_than_a_launch_takes():
     check(p, "gelu_tanh", True, True, torch.float16)
 
 
+def test_more_mx8_rows_than_a_launch_takes():
+    say("mx8_gemm_epilogue, 70000 rows")
+    p = Product("mx8", 70000, 24, 64, 32, 9)
+    check(p, "silu", True, True, torch.float32)
+    check(p, "none", True, True, torch.float16, in_place=True, workspace=False)
+
+
 def test_other_streams_and_graphs():
     """Captured on a stream of its own, replayed with other inputs between eager calls; two graphs with one workspace, one after the other."""
     say("epilogues in graphs")

@@ -467,6 +467,48 @@ def test_two_graphs_share_a_workspace():
             assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("fmt,M", [("nvfp4", 2), ("mx", 12), ("nvfp4", 48), ("mx", 100)])
+def test_replayed_and_at_the_same_time(fmt, M):
+    """Each kind of kernel in a graph, replayed with other tokens and choices; two calls at once on streams and workspaces of their own."""
+    say("moe, graphs and two streams", fmt, M)
+    rng = np.random.default_rng(M)
+    K, I, N, E, top = 512, 288, 272, 7, 3
+    up, down = ([dev(t) if t is not None else None for t in random_experts(fmt, E, r, k, 0, rng)] for r, k in ((2 * I, K), (N, I)))
+    parts = (*up, *down) if fmt == "nvfp4" else (*up[:2], *down[:2])
+    prepare, eager = (B.prepare_moe, B.arcq_moe) if fmt == "nvfp4" else (B.prepare_mx_moe, B.arcq_mx_moe)
+    perm = dev(rng.permutation(K).astype(np.int32))
+
+    def tokens():
+        return (dev(rng.standard_normal((M, K)).astype(np.float16)), *(dev(t) for t in choices(rng, M, E, top, True)))
+
+    x, ids, w = tokens()
+    need = B.arcq_moe_workspace_size(M, top, E, K, I, N, True)
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    y, r = torch.empty((M, N), device="cuda"), torch.randn((M, N), device="cuda")
+    eager(x, perm, ids, w, *parts, residual=r, y=y, workspace=ws[0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        prepare(x, perm, ids, w, *parts, y, ws[0], residual=r)()
+    for _ in range(4):
+        for to, t in zip((x, ids, w), tokens()):
+            to.copy_(t)
+        ws[0].fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager(x, perm, ids, w, *parts, residual=r))
+    sets, streams = [tokens() for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    want = [eager(a, perm, b, c, *parts, out_dtype=torch.float32) for a, b, c in sets]
+    ys = [torch.zeros((M, N), device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (a, b, c), stream, out, scratch in zip(sets, streams, ys, ws):
+            with torch.cuda.stream(stream):
+                eager(a, perm, b, c, *parts, y=out, workspace=scratch)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ys, want))
+
+
 def test_operands_that_do_not_fit():
     """Refused before the library sees their addresses."""
     perm, up, down, host, router, x, hidden, top, I = layer("mx")
