@@ -55,6 +55,7 @@ struct UpArgs {
     uint16_t *high, *low;                       // [M top, pitch]
     int pitch;                                  // I in whole chunks, zeros behind
     int tiles;                                  // of 16 columns
+    const int32_t* perm;                        // of up_few_kernel: the order that x is taken in, or null
 };
 
 template <typename OutT>
@@ -212,6 +213,7 @@ __device__ __forceinline__ int distinct(const int16_t* ids, int slots, int16_t* 
 // They lie in LDS.  A tile of 16 columns of an expert, that is 16 rows of G and of U, is for KW waves, which split K; workgroups, one on a compute unit, take
 // such a tile for each of their 8 / KW teams after the other, and ask for the next one's weights while they multiply and add up this one's.
 // G: chunks in flight (a ring of two such groups was no faster).  SLOTS: most slots, 64 (experts in a wave's lanes) or 256 (in LDS).
+constexpr int kGathered = 2;                        // pieces of 8 values a thread, at most, where it puts x in order
 struct UpFewLds {
     float sums[8][2][4][64];                        // wave, G or U, element, lane
     float weights[256], scales[256];                // of a slot: its weight (a token's first choice of an expert: all of them), and the tensor scale of its expert
@@ -235,7 +237,24 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     const float scale_of = B == 16 && id >= 0 ? a.up.tensor_scales[id] : 1.0f / kFolded<B>;
     constexpr int AT_ONCE = 8;                      // pieces of a thread on their way
     const int per_row = 16 * chunks, all_pieces = per_row * a.M;
-    for (int u0 = tid; u0 < all_pieces; u0 += 512 * AT_ONCE) {          // (pieces past the end are zeros)
+    // few enough values are put in order here: asked for before the weights and written to LDS behind them
+    u32x4 order[kGathered][2];
+    uint16_t gathered[kGathered][8];
+    if (a.perm) {
+#pragma unroll
+        for (int k = 0; k < kGathered; ++k) {
+            const int p = min(tid + 512 * k, all_pieces - 1) % per_row;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) order[k][h] = *reinterpret_cast<const u32x4*>(a.perm + 8 * min(p, pieces - 1) + 4 * h);
+        }
+#pragma unroll
+        for (int k = 0; k < kGathered; ++k) {
+            const uint16_t* row = a.x + min(tid + 512 * k, all_pieces - 1) / per_row * a.ldx;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) gathered[k][v] = row[min(order[k][v >> 2][v & 3], (uint32_t)a.K - 1u)];        // (an unchecked perm may point outside)
+        }
+    }
+    for (int u0 = a.perm ? all_pieces : tid; u0 < all_pieces; u0 += 512 * AT_ONCE) {    // (pieces past the end are zeros)
         u32x4 v[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
@@ -294,6 +313,17 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     ask_scales(0);
 #pragma unroll
     for (int d = 0; d < G; ++d) ask_codes(0, d);
+    if (a.perm) {
+#pragma unroll
+        for (int k = 0; k < kGathered; ++k) {
+            const int u = tid + 512 * k, m = u / per_row, p = u - m * per_row;
+            u32x4 v = {0, 0, 0, 0};
+            if (p < pieces)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) v[h] = (uint32_t)gathered[k][2 * h] | (uint32_t)gathered[k][2 * h + 1] << 16;
+            if (u < all_pieces) *reinterpret_cast<u32x4*>(xs + m * pitch + 16 * p) = v;
+        }
+    }
     wait_lgkmcnt0();
     wg_barrier();                                   // not __syncthreads(): the weights stay in flight
     // which token chooses which expert, once and not for every tile; what is written here is read behind the first round's barriers
@@ -914,6 +944,8 @@ __global__ __launch_bounds__(256) void join_kernel(DownArgs<OutT> a, uint32_t pa
 
 // Whether a launch's tokens go as rows of one tile.
 size_t up_few_lds(int64_t M, int64_t K) { return sizeof(UpFewLds) + (size_t)M * (size_t)((K + 127) / 128 * 256 + 16); }
+// Up to 8192 values that have to be put in order are so by up_few_kernel itself: one token of 2048 through eight of 64 18.2 us, behind a launch that does
+// it 20.6, and 18.0 with nothing to put in order; with up to 16384 the two ways differ by 1 us to either side.
 bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 256 && K >= 256 && up_few_lds(M, K) <= kMaxLdsBytes; }
 bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
 
@@ -1006,7 +1038,8 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     float* partial = reinterpret_cast<float*>(at + w.reordered + 2 * w.half);
     const uint16_t* x = static_cast<const uint16_t*>(p.x) + m0 * p.ldx;
     int64_t ldx = p.ldx;
-    if (p.perm) {
+    const bool gather = p.perm && up_few(M, p.top, p.K) && M * pitch_of(p.K) <= 8 * 512 * kGathered;
+    if (p.perm && !gather) {
         if (arcq_status st = launch_reorder_rows(x, M, p.K, p.ldx, p.perm, reordered, p.stream)) return st;
         x = reordered, ldx = p.K;
     }
@@ -1015,7 +1048,7 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     const int tiles = (int)(p.I / 16);
     const Experts up = {p.up_codes, p.up_scales, p.up_tensor_scales, (p.K + p.S_up) / 2, (p.K + p.S_up) / B, (int)(2 * p.I)};
     const Experts down = {p.down_codes, p.down_scales, p.down_tensor_scales, (p.I + p.S_down) / 2, (p.I + p.S_down) / B, (int)p.N};
-    const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, high, low, (int)pitch_of(p.I), tiles};
+    const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, high, low, (int)pitch_of(p.I), tiles, gather ? p.perm : nullptr};
     if (up_few(M, p.top, p.K)) {
         const int64_t items = most * tiles;
         const int chunks = (int)((p.K + 127) / 128);
