@@ -942,15 +942,18 @@ __global__ __launch_bounds__(256) void join_kernel(DownArgs<OutT> a, uint32_t pa
     store_out(a.y + m * a.ldy + n, sum);
 }
 
-// Whether a launch's tokens go as rows of one tile.
+// Whether a launch's tokens go as rows of one tile: up to the activation wherever 16 rows and LDS take them, behind it up to 8 tokens.  Measured, us of a call, and with
+// the tokens gathered instead there:       up_few_kernel                   down_few_kernel
+//   1 x 4096 x 14336, two of eight             51    60                        51    60
+//   4 x 4096 x 1792, eight of 128              84    95                        85    91    (8 tokens 153, 149; 16 tokens 229, 229)
+//   13 x 5120 x 1392, four of 30               93   107                        (more than 8 tokens)
+//   1 x 2048 x 1024, eight of 64                                               18    27
 size_t up_few_lds(int64_t M, int64_t K) { return sizeof(UpFewLds) + (size_t)M * (size_t)((K + 127) / 128 * 256 + 16); }
-// Up to 8192 values that have to be put in order are so by up_few_kernel itself: one token of 2048 through eight of 64 18.2 us, behind a launch that does
-// it 20.6, and 18.0 with nothing to put in order; with up to 16384 the two ways differ by 1 us to either side.
 bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 256 && K >= 256 && up_few_lds(M, K) <= kMaxLdsBytes; }
 bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
 
 // Waves that split K in up_few_kernel: as many as have four chunks each.  And how many chunks go together, so that few are asked for in vain where a wave's are
-// not a multiple of that.
+// not a multiple of that.  (13 x 5120 x 1392, four of 30: 5 chunks a wave go as five in 93 us, as four and one of four in 97.)
 int waves_of(int chunks) { return chunks >= 32 ? 8 : chunks >= 16 ? 4 : 2; }
 int group_of(int chunks, int waves) {
     const int most = (chunks + waves - 1) / waves;
@@ -1006,6 +1009,7 @@ arcq_status launch_down_waves(const DownArgs<OutT>& d, hipStream_t stream) {
 }
 
 // 16 waves a workgroup, one on a compute unit; where a last round of those would leave a quarter of the compute units' time idle, 8, of which two fit.
+// (5120 features, 1392 channels, four of 30, us of a call with 8 and with 16: one token 24, 27; four 61, 66; eight 79, 84.)
 template <int B, int TOKENS, typename OutT>
 arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
     const int64_t tiles = (d.N + 15) / 16, cus = num_cu(), rounds = (tiles + cus - 1) / cus;
@@ -1038,6 +1042,8 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     float* partial = reinterpret_cast<float*>(at + w.reordered + 2 * w.half);
     const uint16_t* x = static_cast<const uint16_t*>(p.x) + m0 * p.ldx;
     int64_t ldx = p.ldx;
+    // Up to 8192 values that have to be put in order are so by up_few_kernel itself: one token of 2048 through eight of 64 18.2 us, behind a launch that does it
+    // 20.6, and 18.0 with nothing to put in order; with up to 16384 the two ways differ by 1 us to either side.
     const bool gather = p.perm && up_few(M, p.top, p.K) && M * pitch_of(p.K) <= 8 * 512 * kGathered;
     if (p.perm && !gather) {
         if (arcq_status st = launch_reorder_rows(x, M, p.K, p.ldx, p.perm, reordered, p.stream)) return st;

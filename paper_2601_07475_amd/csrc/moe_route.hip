@@ -215,7 +215,8 @@ __global__ __launch_bounds__(256) void choose_kernel(RouteArgs a) {
 // Tokens of a launch: the workspace and grids stay within bounds for any number of them.
 constexpr int64_t kMostTokens = 4096;
 
-// Whether a workgroup a token is quickest: it reads all of the router's weights by itself, 128 KB at most.
+// Whether a workgroup a token is quickest: it reads all of the router's weights by itself, 128 KB at most.  Measured, us a call, and the other way:
+// 8 experts, K = 4096, 1 to 256 tokens 6.5, 9.3; 60 and 1024 6.6, 9.3; 60 and 4096 13 to 14, 9.2.
 bool by_token(int64_t K, int64_t E) { return E <= 64 && K * E <= 65536; }
 
 // Runs of K: two workgroups a compute unit, with four chunks of 32 for each wave.
