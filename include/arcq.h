@@ -394,7 +394,8 @@ arcq_status arcq_mx_gemv_epilogue(const void* x, int64_t M, int64_t K, int64_t l
  * bias    fp32 [E], 4-byte aligned, or NULL: none
  * 1 <= top_k <= E <= ARCQ_MOE_MAX_EXPERTS, top_k <= ARCQ_MOE_MAX_TOP_K
  * ids     out, int32 [M, top_k];  weights  out, fp32 [M, top_k], both dense and 4-byte aligned
- * workspace  256-byte aligned, at least arcq_moe_route_workspace_size bytes (may be NULL when that is 0).  Calls that share one must not overlap.
+ * workspace  256-byte aligned, at least arcq_moe_route_workspace_size bytes (may be NULL when that is 0), which are enough for fewer tokens, too.
+ *            Calls that share one must not overlap.
  * Where scores are not finite, ids hold experts once each, or -1 (no expert) with a weight of 0 or NaN.
  */
 #define ARCQ_MOE_SIGMOID     1u

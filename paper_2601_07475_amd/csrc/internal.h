@@ -145,7 +145,7 @@ struct MoeArgs {
 };
 size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t E, int64_t K, int64_t I, int64_t N, bool reorder);
 arcq_status launch_moe(int block, const MoeArgs& p);
-// The router
+// The router; enough for any number of tokens up to M
 size_t moe_route_workspace_bytes(int64_t M, int64_t K, int64_t E);
 arcq_status launch_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, const void* router, int64_t ldr, int64_t E, const float* bias, int64_t top,
                              uint32_t flags, int32_t* ids, float* weights, void* workspace, hipStream_t stream);

@@ -220,9 +220,10 @@ constexpr int64_t kMostTokens = 4096;
 bool by_token(int64_t K, int64_t E) { return E <= 64 && K * E <= 65536; }
 
 // Runs of K: two workgroups a compute unit, with four chunks of 32 for each wave.
+constexpr int64_t kRunWorkgroups = 2 * 256, kRunK = 512;
 int splits_of(int64_t M, int64_t K, int64_t E) {
     const int64_t tiles = (M + 15) / 16 * ((E + 15) / 16);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(2 * 256 / tiles, K / 512));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kRunWorkgroups / tiles, K / kRunK));
 }
 
 template <int PER>
@@ -233,10 +234,15 @@ arcq_status launch_choose(const RouteArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// Fewer tokens may go in more runs and need more room than more tokens do, so this is the most that any number of them up to M needs: for every number of
+// runs, as many tokens as still go in that many.
 size_t moe_route_workspace_bytes(int64_t M, int64_t K, int64_t E) {
     if (by_token(K, E)) return 0;
     M = std::min(M, kMostTokens);
-    return (size_t)splits_of(M, K, E) * (size_t)M * (size_t)E * sizeof(double);
+    const int64_t tiles_e = (E + 15) / 16;
+    int64_t rows = M;                               // in one run
+    for (int64_t runs = 2; runs <= K / kRunK && runs * tiles_e <= kRunWorkgroups; ++runs) rows = std::max(rows, runs * std::min(M, kRunWorkgroups / (runs * tiles_e) * 16));
+    return (size_t)rows * (size_t)E * sizeof(double);
 }
 
 arcq_status launch_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, const void* router, int64_t ldr, int64_t E, const float* bias, int64_t top,
