@@ -349,7 +349,8 @@ arcq_status arcq_mx8_gemm(const uint8_t* a_codes, const uint8_t* a_scales,
  * w_*   packed weights [N, K + S] in the plain layout (not ARCQ_LAYOUT_INTERLEAVED with S > 0), codes 8-byte aligned; the S columns that
  *       repeat the outliers' weights are passed over.  K, S as in the packer.
  * y     as in arcq_gemm.
- * workspace  256-byte aligned, at least arcq_gemv_workspace_size / arcq_mx_gemv_workspace_size bytes (may be NULL when that is 0).
+ * workspace  256-byte aligned, at least arcq_gemv_workspace_size / arcq_mx_gemv_workspace_size bytes (may be NULL when that is 0).  Fewer rows may need more
+ *       of it than more rows do: one workspace for several numbers of rows has the largest of their sizes.
  *       Calls that share a workspace must not overlap.
  */
 arcq_status arcq_gemv_workspace_size(int64_t M, int64_t N, int64_t K, int with_perm, size_t* bytes);
@@ -421,7 +422,8 @@ arcq_status arcq_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, con
  *          weights are passed over.  Codes 8-byte aligned.  K, S_up and I, S_down as in the packer.
  * activation  an ARCQ_ACT_;  residual, y  as in the calls with an epilogue: residual may be NULL or y
  * 1 <= top_k <= ARCQ_MOE_MAX_TOP_K, 1 <= E <= ARCQ_MOE_MAX_EXPERTS, N <= 2^24
- * workspace  256-byte aligned, at least arcq_moe_workspace_size bytes (for either format).  Calls that share one must not overlap.
+ * workspace  256-byte aligned, at least arcq_moe_workspace_size bytes (for either format), which are enough for fewer tokens, too.  Calls that share one must
+ *            not overlap.
  */
 arcq_status arcq_moe_workspace_size(int64_t M, int64_t top_k, int64_t E, int64_t K, int64_t I, int64_t N, int with_perm, size_t* bytes);
 arcq_status arcq_moe(const void* x, int64_t M, int64_t K, int64_t ldx, const int32_t* perm,

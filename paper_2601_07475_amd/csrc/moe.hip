@@ -963,10 +963,12 @@ int group_of(int chunks, int waves) {
     return best;
 }
 
-// Runs of I for down_many_kernel.
+// Runs of I for down_many_kernel: two items a compute unit, eight chunks in each at least.
+constexpr int64_t kRunItems = 512;
+int64_t most_runs(int64_t I) { return std::min<int64_t>((I + 127) / 128 / 8, 8); }
 int down_splits(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
-    const int64_t groups = (N + 255) / 256 * std::min<int64_t>(E, M * top), chunks = (I + 127) / 128;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(groups, 1), chunks / 8, 8}));
+    const int64_t groups = (N + 255) / 256 * std::min<int64_t>(E, M * top);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kRunItems / std::max<int64_t>(groups, 1), most_runs(I)));
 }
 
 int64_t pitch_of(int64_t I) { return (I + 127) / 128 * 128; }
@@ -975,9 +977,12 @@ int64_t pitch_of(int64_t I) { return (I + 127) / 128 * 128; }
 struct MoeWorkspace {
     size_t reordered, half, partial;            // rows in the weights' order; one of the two numbers of h; slots' results
 };
+size_t whole_lines(int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; }
+size_t partial_bytes(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
+    return M == 0 || down_few(M, top, I) ? 0 : whole_lines((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4);
+}
 MoeWorkspace workspace_of(int64_t M, int64_t top, int64_t K, int64_t I, int64_t N, int64_t E, bool reorder) {
-    auto whole = [](int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; };
-    return {reorder ? whole(M * K * 2) : 0, whole(M * top * pitch_of(I) * 2), down_few(M, top, I) ? 0 : whole((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4)};
+    return {reorder ? whole_lines(M * K * 2) : 0, whole_lines(M * top * pitch_of(I) * 2), partial_bytes(M, top, E, I, N)};
 }
 
 template <int B, int KW, int G, int SLOTS>
@@ -1081,9 +1086,18 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
 
 }  // namespace
 
+// Enough for any number of tokens up to M: fewer may go in more runs of I and need more room for slots' results than more tokens do, so those are counted for as
+// many tokens as still go in each number of runs.
 size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t E, int64_t K, int64_t I, int64_t N, bool reorder) {
-    const MoeWorkspace w = workspace_of(std::min<int64_t>(M, kMostTokens), top, K, I, N, E, reorder);
-    return w.reordered + 2 * w.half + w.partial;
+    M = std::min<int64_t>(M, kMostTokens);
+    const MoeWorkspace w = workspace_of(M, top, K, I, N, E, reorder);       // (whose other parts grow with the tokens)
+    const int64_t groups = (N + 255) / 256;
+    size_t partial = w.partial;
+    for (int64_t runs = 2; runs <= most_runs(I); ++runs) {
+        const int64_t experts = kRunItems / (groups * runs);        // that there may be work for
+        partial = std::max(partial, partial_bytes(E <= experts ? M : std::min(M, experts / top), top, E, I, N));
+    }
+    return w.reordered + 2 * w.half + partial;
 }
 
 // Tokens go kMostTokens at a time.

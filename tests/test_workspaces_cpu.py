@@ -36,3 +36,20 @@ def test_router_sums_fit():
             runs = max(1, min(512 // tiles, K // 512))
             if K * E > 65536 or E > 64:
                 assert B.arcq_moe_route_workspace_size(m, K, E) >= runs * m * E * 8
+
+
+@pytest.mark.parametrize("top,E,K,I,N", [(8, 256, 2048, 2048, 512), (2, 8, 4096, 14336, 4096), (8, 128, 4096, 1792, 4096), (4, 30, 5120, 1392, 5120), (1, 1024, 64, 8192, 1280),
+                                         (1, 1024, 64, 8192, 1), (16, 1024, 256, 65536, 300), (2, 2, 256, 4096, 256), (3, 7, 96, 96, 1000), (1, 1, 32, 1024, 100000), (5, 40, 32, 3136, 1800)])
+@pytest.mark.parametrize("reorder", [False, True])
+def test_experts(top, E, K, I, N, reorder):
+    got = sizes(lambda m: B.arcq_moe_workspace_size(m, top, E, K, I, N, reorder), 70)
+    assert got == sorted(got)
+    for m in range(1, 65):
+        # h of every slot in 32 bits, and results of every run, as the launch has them, where they are added up by a launch of their own
+        groups, runs = (N + 255) // 256 * min(E, m * top), 0
+        if m > 8 or m * top > 64 or I < 128:
+            runs = max(1, min(512 // groups, (I + 127) // 128 // 8, 8))
+        assert got[m - 1] >= 4 * m * top * ((I + 127) // 128 * 128) + 4 * runs * m * top * N + 2 * m * K * reorder
+        call = lambda ws, bytes_: B.lib().arcq_moe(FAKE, m, K, K, FAKE if reorder else None, FAKE, FAKE, top, E, FAKE, FAKE, FAKE, I, 0, FAKE, FAKE, FAKE, N, 0, 4,  # noqa: E731
+                                                   None, 0, FAKE, 0, N, ws, bytes_, None)
+        assert call(OFF16, got[m - 1]) == B.BAD_ALIGN and call(FAKE, got[m - 1] - 1) == B.WORKSPACE_TOO_SMALL
