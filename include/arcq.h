@@ -411,7 +411,8 @@ arcq_status arcq_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, con
 /*
  * The experts of a mixture for a few tokens (the decode step of such a layer), on packed NVFP4 (arcq_moe) or MXFP4 (arcq_mx_moe) weights:
  *   y[m, n] = sum_j weights[m, j] sum_{i<I} act(g[i]) u[i] D_e[n, i] + residual[m, n],   e = ids[m, j],   g = G_e x[m],  u = U_e x[m]
- * with fp32 accumulation; x is not rounded, weights[m, j] act(g) u is held to 22 bits (2^-32 at least) and must stay below 2^20.
+ * with fp32 accumulation; x is not rounded; h = weights[m, j] act(g[i]) u[i] is in fp32, of which 23 bits enter the second product (2^-38 of the largest h of
+ * that m and j at least), whatever size they are.
  * x        fp16 [M, K], pitch ldx, and perm as in arcq_gemv.  Any M; made for up to 64 tokens (more take the weights once for every 64).
  * ids      int32 [M, top_k], dense: outside 0 .. E - 1 (say -1) there is no expert, and the weight there is not read.  A token without any gets its
  *          residual, or zeros.  An expert twice in a token counts with both weights.

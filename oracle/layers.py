@@ -62,6 +62,13 @@ def sum_error(mag, K):
     return mag * (K / 16 + 64) * 2.0 ** -23
 
 
+def middle_error(h):
+    """What the values h [I] between the two products are off by on their way, whatever their size: three products in fp32 (four half steps), then two fp16
+    numbers.  The first leaves at most 2^-11 of its value, which the second rounds at half a step of its own, 2^-12 of that: 2^-23 in all.  Both count in units
+    that take the largest value of the row, or of some of its channels, to 2^13 at least, and fp16 has no steps below 2^-24, so half of one is 2^-38 of that value."""
+    return h * (4 * HALF + 2.0 ** -23) + 2.0 ** -38 * h.max(initial=0.0)
+
+
 def finish(total, mag, K, bias=None, act="none", residual=None):
     """total, mag: a product's sums and their magnitudes -> (y, how far an fp32 evaluation may be off, before y's own rounding)."""
     off = sum_error(mag, K)
@@ -115,9 +122,8 @@ def experts(x, perm, ids, weights, up, down, act="silu", residual=None):
             a = activation(act, g)
             da = (STEEPEST if act != "none" else 1.0) * dg + activation_slack(act, np.abs(g) + dg)
             h = w * a * u
-            # three products in fp32, then 22 bits of the result, 2^-32 at least
             dh = np.abs(w) * (da * (np.abs(u) + du) + np.abs(a) * du)
-            dh = dh + (np.abs(h) + dh) * (4 * HALF + 2.0 ** -22) + 2.0 ** -32
+            dh = dh + middle_error(np.abs(h) + dh)
             y[m] += D @ h
             mag[m] += np.abs(D) @ (np.abs(h) + dh)
             off[m] += np.abs(D) @ dh

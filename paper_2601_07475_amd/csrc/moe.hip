@@ -10,9 +10,11 @@
 // Every workgroup finds out by itself which tokens choose an expert: no kernel in front, and none that waits for the host.  An expert that a token
 // names twice counts once, with both weights: a token is then in a list once, and sums do not depend on the order of a list.
 //
-// h is held as two fp16 numbers, h / 16 rounded and 2^11 times what that leaves: 22 bits of h down to 2^-10, 2^-32 below it, up to 2^20.  (One fp16 number would put
-// its rounding, 2^-12, behind an fp32 y.)  The two are rows i and i + 8 of one row tile, so the second costs no more matrix instructions than the tile's
-// free rows; the halves of a wave hold the sums of either and are put together when a wave is done with an expert.
+// h goes through memory in fp32.  The second product takes it as two fp16 numbers, what rounds to fp16 and what that leaves, in a unit that goes by the largest value of
+// its row, or of its row so far: 23 bits of h, and 2^-38 of that largest value at least, whatever size the values are.  (One fp16 number would put its rounding,
+// 2^-12, behind an fp32 y; a fixed unit loses small values and has a largest one.)  Units are powers of two, and sums are taken back exactly.  The two numbers are rows i and
+// i + 8 of one row tile, so the second costs no more matrix instructions than the tile's free rows; the halves of a wave hold the sums of either and are put together
+// when a wave is done with an expert.
 //
 // No atomics on results, and every sum in an order that the sizes and choices fix: the same inputs give the same bits.
 //
@@ -35,8 +37,6 @@ namespace arcq {
 namespace {
 
 constexpr int kMostExperts = ARCQ_MOE_MAX_EXPERTS, kMostTokens = 64, kMostSlots = kMostTokens * ARCQ_MOE_MAX_TOP_K;     // of a launch
-constexpr float kLow = 0x1p-11f;                // what the second number of h counts
-constexpr float kUnit = 16.0f;                  // what the first one counts
 
 struct Experts {
     const uint8_t *codes, *scales;              // [E, rows, pitch]
@@ -52,15 +52,17 @@ struct UpArgs {
     const float* weights;
     int M, top, E, K, I, activation;
     Experts up;
-    uint16_t *high, *low;                       // [M top, pitch]
+    float* h;                                   // [M top, pitch]
     int pitch;                                  // I in whole chunks, zeros behind
+    uint8_t* exponents;                         // of the largest magnitude of every 16 of a row, [M top, exponents_pitch(tiles)], zeros behind; or null
     int tiles;                                  // of 16 columns
     const int32_t* perm;                        // of up_few_kernel: the order that x is taken in, or null
 };
 
 template <typename OutT>
 struct DownArgs {
-    const uint16_t *high, *low;
+    const float* h;
+    const uint8_t* exponents;
     const int32_t* ids;
     int M, top, E, I, pitch, N;
     Experts down;
@@ -72,17 +74,76 @@ struct DownArgs {
     int groups, splits;
 };
 
-// h of one slot and column.
+__host__ __device__ constexpr int exponents_pitch(int tiles) { return (tiles + 15) / 16 * 16; }
+
+// The largest over a row of 16 lanes, in all of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));        // its neighbour, the pair beside it, the other four, the other eight
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));
+}
+
+// h of one slot and column; the 16 lanes of a row have the columns of a tile.
 __device__ __forceinline__ void store_h(const UpArgs& a, int slot, int n, float g, float u, float weight) {
     float v[1] = {g};
     activate(v, a.activation);
-    const float h = v[0] * u * weight * (1.0f / kUnit);
-    const _Float16 high = (_Float16)h, low = (_Float16)((h - (float)high) * (1.0f / kLow));
-    const int64_t to = (int64_t)slot * a.pitch + n;
-    a.high[to] = __builtin_bit_cast(uint16_t, high);
-    a.low[to] = __builtin_bit_cast(uint16_t, low);
-    if (n >= a.I - 16)                          // whoever has the last tile clears what is left of the last chunk
-        for (int z = n + 16; z < a.pitch; z += 16) a.high[to + z - n] = a.low[to + z - n] = 0;
+    const float h = v[0] * u * weight;
+    float* to = a.h + ((int64_t)slot * a.pitch + n);
+    *to = h;
+    const bool last = n >= a.I - 16;
+    if (last)                                   // whoever has the last tile clears what is left of the last chunk
+        for (int z = 16; n + z < a.pitch; z += 16) to[z] = 0.0f;
+    if (a.exponents) {
+        const uint32_t most = row_max(__float_as_uint(h) & 0x7FFFFFFFu) >> 23;
+        uint8_t* row = a.exponents + slot * exponents_pitch(a.tiles);
+        const int tile = n >> 4, lane = n & 15;
+        if (lane == 0) row[tile] = (uint8_t)most;
+        if (last && tile + 1 + lane < exponents_pitch(a.tiles)) row[tile + 1 + lane] = 0;
+    }
+}
+
+// Values of h below 2^(most - 126) are multiplied by 2^(140 - most) = scale_to(most): the largest lie from 2^13 to 2^14, and those of infinity's neighbours, for which
+// `most` is at its end, below 2^16: all are numbers of fp16.  Sums are taken back by scale_from(most).  With kLeast what the two numbers leave is less than fp32 resolves.
+constexpr uint32_t kLeast = 14, kMost = 253;
+__device__ __forceinline__ float scale_to(uint32_t most) { return __uint_as_float((267u - most) << 23); }
+__device__ __forceinline__ float scale_from(uint32_t most) { return __uint_as_float((most - 13u) << 23); }
+
+// The largest magnitude of four values (or something that is not a number).
+__device__ __forceinline__ float magnitude(const u32x4& v) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_fabsf(__uint_as_float(v[0])), __builtin_fabsf(__uint_as_float(v[1]))),
+                                                                       __builtin_fabsf(__uint_as_float(v[2]))), __builtin_fabsf(__uint_as_float(v[3])));
+}
+// The largest over the 32 lanes of either half of a wave, in all of them.
+__device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
+    v = row_max(v);
+    const uint2v rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return max(rows[0], rows[1]);
+}
+// The largest of 16 bytes.
+__device__ __forceinline__ uint32_t largest_byte(const u32x4& v) {
+    typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+    ushort2v m = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2v, v[k] & 0x00FF00FFu));
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2v, v[k] >> 8 & 0x00FF00FFu));
+    }
+    return max((uint32_t)m[0], (uint32_t)m[1]);
+}
+// Four values times scale as fp16 numbers, to `high`, and as fp16 numbers what that leaves, to `low`.
+__device__ __forceinline__ void put_h(const u32x4& v, float scale, uint8_t* high, uint8_t* low) {
+    uint32_t h[2], l[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float a = __uint_as_float(v[2 * k]), b = __uint_as_float(v[2 * k + 1]);
+        h[k] = __builtin_bit_cast(uint32_t, half2v{(_Float16)(a * scale), (_Float16)(b * scale)});
+        asm("" : "+v"(h[k]));                       // (as it is: both halves are read from here, not rounded a second time)
+        const half2v first = __builtin_bit_cast(half2v, h[k]);
+        l[k] = __builtin_bit_cast(uint32_t, half2v{(_Float16)__builtin_fmaf(a, scale, -(float)first[0]), (_Float16)__builtin_fmaf(b, scale, -(float)first[1])});
+    }
+    *reinterpret_cast<uint2*>(high) = make_uint2(h[0], h[1]);
+    *reinterpret_cast<uint2*>(low) = make_uint2(l[0], l[1]);
 }
 
 // Chunks of 128 k of a tile of 16 rows of weights, the last of which may be a part.  Kernels ask for them some chunks ahead, every lane for every chunk alike
@@ -410,7 +471,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
 
 // Up to 8 tokens: 16 columns of y a workgroup.  The reduction runs over all chosen experts' channels one after the other, in equal shares for the waves, G
 // chunks at a time; a wave adds what it has of an expert to its own sums of all tokens, and the waves' sums are added in their order at the end.
-// Rows of h reach a wave's registers through a slice of LDS of its own, so that a chunk on its way takes TOKENS / 2 registers of 16 bytes and not four.
+// Rows of h reach a wave's registers through a slice of LDS of its own, so that a chunk on its way takes TOKENS / 2 registers of 16 bytes and not four.  A row
+// of h has one unit, by the exponents that came with it: looking for the largest values of a chunk on its arrival instead took 2 to 10 % of a call.
+constexpr int kFewTables = 256 + 512 + 256 + 256;      // bytes of its tables in LDS
 template <int B, int TOKENS, int WAVES, typename OutT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4))) void down_few_kernel(DownArgs<OutT> a) {
     constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2, G = TOKENS < 8 ? 4 : B == 16 ? 3 : 2;      // (as registers allow)
@@ -420,11 +483,15 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     int8_t(&slot_of)[64][8] = *reinterpret_cast<int8_t(*)[64][8]>(lds + sizeof(sums) + 256);       // of an active expert and a token; -1: it does not choose it
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     float* scales_of_slots = reinterpret_cast<float*>(lds + sizeof(sums) + 256 + 512);
-    uint8_t* slice = lds + sizeof(sums) + 256 + 512 + 256 + wave * TOKENS * 512;
+    uint32_t* exponents = reinterpret_cast<uint32_t*>(lds + sizeof(sums) + 256 + 512 + 256);
+    uint8_t* slice = lds + sizeof(sums) + kFewTables + wave * TOKENS * 512;
     const int slots = a.M * a.top, id = checked_id(a.ids, lane, slots, a.E);
+    const int row_bytes = exponents_pitch(a.I >> 4), exponent_pieces = slots * row_bytes >> 4;
+    const u32x4 some = *reinterpret_cast<const u32x4*>(a.exponents + 16 * min(tid, exponent_pieces - 1));
     if (wave == 0) {
+        exponents[lane] = kLeast;
         ids_of[lane] = id;
-        scales_of_slots[lane] = B == 16 && id >= 0 ? a.down.tensor_scales[id] * kUnit : kUnit / kFolded<B>;
+        scales_of_slots[lane] = B == 16 && id >= 0 ? a.down.tensor_scales[id] : 1.0f / kFolded<B>;
     }
     for (int k = lane; k < 128; k += 64) (&sums[wave][0][0])[k] = 0.0f;
     int actives;
@@ -442,19 +509,20 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     const Row<B> of(min(i, a.N - 1 - n0), q, a.I, a.down.code_pitch, a.down.scale_pitch);
     const int per = (a.I + 127) >> 7, groups = (per + G - 1) / G, all = actives * groups;
     const int s0 = wave * all / WAVES, s1 = (wave + 1) * all / WAVES;
-    // pieces of a chunk: rows r = 2 token + (0: high, 1: low), four a load, 16 lanes a row
+    // a load: a chunk of two tokens, 32 lanes each; in LDS rows r = 2 token + (0: first numbers, 1: second ones), in pieces of eight
+    const int part = lane & 31, half = lane >> 5;
     auto unit = [](int piece, int r) { return 16 * (2 * TOKENS * piece + (r ^ (piece & (2 * TOKENS - 1)))); };
+    const int to = unit(part >> 1, 2 * half) + 8 * (part & 1);
     const uint8_t *wc = nullptr, *ws = nullptr;
-    uint32_t row[LOADS], chunk[LOADS];              // offsets from a.high, and what a chunk adds to them
-    const uint32_t low = (uint32_t)(a.low - a.high);
+    uint32_t row[LOADS], chunk[LOADS];              // offsets from a.h, and what a chunk adds to them
     auto take = [&](int nth) {                      // the expert whose weights are asked for next
         const int e = __builtin_amdgcn_readlane(active, nth);
         wc = codes_of(a.down, e, n0);
         ws = scales_of(a.down, e, n0);
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {           // (the row of a token that does not choose it is passed over: the same piece all the time)
-            const int r = 4 * l + q, slot = slot_of[nth][r >> 1];
-            row[l] = slot < 0 ? 0u : ((r & 1) == 0 ? 0u : low) + (uint32_t)slot * (uint32_t)a.pitch + 8u * i;
+            const int slot = slot_of[nth][2 * l + half];
+            row[l] = slot < 0 ? 0u : (uint32_t)slot * (uint32_t)a.pitch + 4u * part;
             chunk[l] = slot < 0 ? 0u : 128u;
         }
     };
@@ -463,19 +531,33 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
     auto ask_scales = [&](int g) { sc = of.scales(ws, min(G * g + q, per - 1)); };
     auto load_rows = [&](int c, u32x4 (&to)[LOADS]) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) to[l] = *reinterpret_cast<const u32x4*>(a.high + (row[l] + chunk[l] * (uint32_t)c));
+        for (int l = 0; l < LOADS; ++l) to[l] = *reinterpret_cast<const u32x4*>(a.h + (row[l] + chunk[l] * (uint32_t)c));
     };
     auto ask_chunk = [&](int g, int d) {
         const int c = min(G * g + d, per - 1);
         load_rows(c, rows[d]);
         cw[d] = of.codes(wc, c);
     };
+    int nth = s0 / max(groups, 1), g = s0 - nth * groups;
     if (s0 < s1) {
-        int nth = s0 / groups, g = s0 - nth * groups;
         take(nth);
         ask_scales(g);
 #pragma unroll
         for (int d = 0; d < G; ++d) ask_chunk(g, d);
+    }
+    // the rows' units, while weights are on their way
+    auto count_exponents = [&](int u, const u32x4& v) { atomicMax(&exponents[(u << 4) / row_bytes], min(largest_byte(v), kMost)); };
+    if (tid < exponent_pieces) count_exponents(tid, some);
+    for (int u = tid + THREADS; u < exponent_pieces; u += THREADS) count_exponents(u, *reinterpret_cast<const u32x4*>(a.exponents + 16 * u));
+    wait_lgkmcnt0();
+    wg_barrier();
+    if (s0 < s1) {
+        float scale[LOADS];                         // to the rows' units
+        auto take_units = [&](int nth) {
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) scale[l] = scale_to(exponents[max((int)slot_of[nth][2 * l + half], 0)]);
+        };
+        take_units(nth);
         float4v acc[1][1];
         clear<1, 1>(acc);
         for (int s = s0; s < s1; ++s) {
@@ -489,7 +571,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
             for (int d = 0; d < 4; ++d) sw[d][0] = one[d];
             auto rows_of = [&](const u32x4 (&from)[LOADS], half8 (&xf)[1][4]) {     // (LDS operations of a wave complete in order)
 #pragma unroll
-                for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4*>(slice + unit(i, 4 * l + q)) = from[l];
+                for (int l = 0; l < LOADS; ++l) {   // (token 2 l and its second row by exclusive or: neither changes another bit of the place)
+                    const int at = to ^ 64 * l;
+                    put_h(from[l], scale[l], slice + at, slice + (at ^ 16));
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xf[0][j] = *reinterpret_cast<const half8*>(slice + unit(4 * j + q, 2 * (i & (TOKENS - 1)) + (i >> 3)));
             };
@@ -521,14 +606,15 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4
             if (over || end) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    // lanes of the first half hold sums of high numbers, those of the second of low ones of the same rows
+                    // lanes of the first half hold sums of first numbers, those of the second of second ones of the same rows
                     const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][0][k]), __float_as_uint(acc[0][0][k]), false, false);
-                    const float sum = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
+                    const float sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
                     const int slot = lane < 32 ? slot_of[nth][4 * q + k] : -1;
-                    if (slot >= 0) sums[wave][4 * q + k][i] += sum * scales_of_slots[slot];
+                    if (slot >= 0) sums[wave][4 * q + k][i] += sum * scale_from(exponents[slot]) * scales_of_slots[slot];
                 }
                 clear<1, 1>(acc);
                 ++nth;
+                if (!end) take_units(nth);
             }
             g = next;
         }
@@ -558,6 +644,7 @@ struct Lists {
     float weight[kMostSlots];                   // by slot, where asked for: all that a token's choices of an expert weigh, at the first
     int blocks;
 };
+constexpr size_t kListBytes = (sizeof(Lists) + 15) / 16 * 16;
 
 // Of a value a lane: the sum over the lanes before.
 __device__ __forceinline__ int sum_before(int n) {
@@ -653,8 +740,9 @@ __device__ __forceinline__ Place place_of(const Lists& l, int item, int pieces) 
 }
 
 // A workgroup's piece of work: a block of an expert's slots with the eight waves' tiles of weights, two each, over a run of the reduction.
+template <typename T>
 struct Item {
-    const uint16_t* from;                       // the row that this thread copies pieces of 8 k of: piece tid % 16 of a chunk, row (tid / 16) % (16 MT)
+    const T* from;                              // the row that this thread copies pieces of 16 bytes of
     const uint8_t *wc[2], *ws[2];               // the wave's tiles
     float scale;                                // of the weights
     int c0, c1;                                 // chunks
@@ -665,25 +753,77 @@ struct Item {
 // Items of a launch in turn.  Rows reach all waves through LDS, kStage chunks at a time in two buffers: a barrier a stage.  (With 16 rows half of the threads copy
 // every other chunk.)  Rows and weights of the next stage, or of the next item's first, are asked for in this one, rows first: they are needed first, and
 // loads return in order.  take(n): the n-th; store(its place, its scale, sums).
+// T: rows of fp16, 16 MT of them; or of fp32, 8 MT, each as two of fp16, rows r and r + 8 of a tile, in a unit that goes by the largest value so far.
 // 32 rows an item (16 slots behind the activation): with 16, two workgroups a compute unit, 64 tokens of eight of 64 experts took 113 us and not 100; with 64,
 // 64 tokens of two of eight 1.5 % less, 32 tokens 2 % more, since the rows' matrix work and reads of LDS are what an item's time is then.
 constexpr int kStage = 4;
 template <int MT>
 constexpr int kRowBytes = kStage * MT * 4096;   // of a buffer
 
-template <int B, int MT, typename Take, typename Store>
-__device__ __forceinline__ void stream_items(int begin, int end, int stride, const Row<B>& of, int K, uint8_t* lds, const Take& take, const Store& store) {
+// Which row a thread copies pieces of, and which of a chunk's pieces of 16 bytes: rows of fp32 have 32, so that half a wave has all of a row's.
+template <typename T, int MT>
+__device__ __forceinline__ int copied_row() {
+    return std::is_same<T, float>::value ? (int)threadIdx.x / (64 / MT) : (int)(threadIdx.x >> 4) & (16 * MT - 1);
+}
+
+template <int B, int MT, typename T, typename Take, typename Store>
+__device__ __forceinline__ void stream_items(int begin, int end, int stride, const Row<B>& of, int K, uint8_t* lds, float (*units)[2][8 * MT], const Take& take, const Store& store) {
+    constexpr bool SPLIT = std::is_same<T, float>::value;
     constexpr int G = kStage, PER = 2 * MT, NT = 2; // pieces of a thread
+    constexpr int OF_PIECE = 16 / (int)sizeof(T), PIECES = 128 / OF_PIECE;      // values of a piece, pieces of a chunk's row
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
-    const int piece = tid & 15, pieces = K >> 3, blocks = of.blocks;
-    auto chunk_of = [&](int k) { return MT == 2 ? k : 2 * k + (tid >> 8); };
+    const int piece = tid & (PIECES - 1), pieces = K / OF_PIECE, blocks = of.blocks, row = copied_row<T, MT>();
+    auto chunk_of = [&](int k) { return MT == 2 ? k : 2 * k + (SPLIT ? lane >> 5 : tid >> 8); };
     auto unit = [](int p, int r) { return 16 * (256 * (r >> 4) + 16 * p + ((r & 15) ^ p)); };
-    const int to = unit(piece, (tid >> 4) & (16 * MT - 1));
+    const int to = SPLIT ? unit(piece >> 1, 16 * (row >> 3) + (row & 7)) + 8 * (piece & 1) : unit(piece, row);
+    // N pieces of the thread's row, of chunks chunk_of(0 ..); all threads of a wave.  SPLIT: a row's unit only grows from the item's first stage on; left for whoever
+    // has the sums: what they are multiplied by before this stage's are added, and what takes them back.
+    uint32_t most = kLeast;
+    auto put = [&](auto& v, int buffer, bool first) {
+        constexpr int N = sizeof(v) / sizeof(v[0]);
+        uint8_t* at = lds + buffer * kRowBytes<MT>;
+        if constexpr (SPLIT) {
+            float largest = 0.0f;
+#pragma unroll
+            for (int k = 0; k < N; ++k) largest = __builtin_elementwise_maximum(largest, magnitude(v[k]));
+            uint32_t stage = half_wave_max(__float_as_uint(largest));
+            if constexpr (MT == 1) {                // (a wave has a row)
+                const uint2v halves = __builtin_amdgcn_permlane32_swap(stage, stage, false, false);
+                stage = max(halves[0], halves[1]);
+            }
+            stage = min(max(stage >> 23, kLeast), kMost);
+            const uint32_t before = first ? stage : most;
+            most = max(before, stage);
+            if (piece == 0) {
+                units[buffer][0][row] = most - before < 127 ? __uint_as_float((127 - (most - before)) << 23) : 0.0f;
+                units[buffer][1][row] = scale_from(most);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (N > 1 || chunk_of(k) == 0) put_h(v[k], scale_to(most), at + chunk_of(k) * MT * 4096 + to, at + chunk_of(k) * MT * 4096 + (to ^ 128));       // (eight rows on)
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (N > 1 || chunk_of(k) == 0) *reinterpret_cast<u32x4*>(at + chunk_of(k) * MT * 4096 + to) = v[k];
+        }
+    };
+    auto multiply_by = [&](const float (&scales)[8 * MT], float4v (&acc)[MT][NT]) {
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+            const float4v scale = *reinterpret_cast<const float4v*>(&scales[8 * r + 4 * (q & 1)]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[r][t][k] *= scale[k];
+        }
+    };
     if (begin >= end) return;
     if (blocks < of.SB) {                           // less than one chunk: too short to be moved back into
         for (int item = begin; item < end; item += stride) {
-            const Item now = take(item);
-            if (tid < 256 * MT) *reinterpret_cast<u32x4*>(lds + to) = piece < pieces ? *reinterpret_cast<const u32x4*>(now.from + 8 * piece) : u32x4{0, 0, 0, 0};
+            const Item<T> now = take(item);
+            u32x4 one[1] = {{0, 0, 0, 0}};
+            if (chunk_of(0) == 0 && piece < pieces) one[0] = *reinterpret_cast<const u32x4*>(now.from + OF_PIECE * piece);
+            put(one, 0, true);
             uint4 words[NT];
             uint32_t sw[NT];
 #pragma unroll
@@ -715,6 +855,7 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xf[r][j] = *reinterpret_cast<const half8*>(lds + unit(4 * j + q, 16 * r + i));
             multiply_folded<B, B == 16, MT>(xf, words, sw, acc);
+            if constexpr (SPLIT) multiply_by(units[0][1], acc);
             store(now.place, now.scale, acc);
             __syncthreads();
         }
@@ -722,18 +863,20 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
     }
     u32x4 rows[PER], cw[G][NT];
     u32x2 sc[NT];
-    Item ahead = take(begin);                       // whose loads are asked for next
+    Item<T> ahead = take(begin);                    // whose loads are asked for next
     auto ask_rows = [&](int c) {                    // (past the end: the last chunk again)
 #pragma unroll
         for (int k = 0; k < PER; ++k)
-            rows[k] = *reinterpret_cast<const u32x4*>(ahead.from + 8 * min(16 * min(c + chunk_of(k), ahead.c1 - 1) + piece, pieces - 1));
+            rows[k] = *reinterpret_cast<const u32x4*>(ahead.from + OF_PIECE * min(PIECES * min(c + chunk_of(k), ahead.c1 - 1) + piece, pieces - 1));
     };
     auto put_rows = [&](int c, int buffer) {
+        u32x4 v[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const bool in = c + chunk_of(k) < ahead.c1 && 16 * (c + chunk_of(k)) + piece < pieces;      // (all four chunks are multiplied)
-            *reinterpret_cast<u32x4*>(lds + buffer * kRowBytes<MT> + chunk_of(k) * MT * 4096 + to) = in ? rows[k] : u32x4{0, 0, 0, 0};
+            const bool in = c + chunk_of(k) < ahead.c1 && PIECES * (c + chunk_of(k)) + piece < pieces;      // (all four chunks are multiplied)
+            v[k] = in ? rows[k] : u32x4{0, 0, 0, 0};
         }
+        put(v, buffer, c == ahead.c0);
     };
     auto ask_scales = [&](int c) {                  // lane group q: of chunk c + q
 #pragma unroll
@@ -756,11 +899,13 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
         const bool two = ahead.two;
         const float scale = ahead.scale;
         const Place place = ahead.place;
-        Item after;                                 // found out where loads are on their way, not where some are to be asked for
+        Item<T> after;                              // found out where loads are on their way, not where some are to be asked for
         bool known = false;
         float4v acc[MT][NT];
         clear<MT, NT>(acc);
         for (int c = c0; c < c1; c += G) {
+            if constexpr (SPLIT)
+                if (c != c0) multiply_by(units[buffer][0], acc);
             uint32_t sw[4][NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -813,6 +958,8 @@ __device__ __forceinline__ void stream_items(int begin, int end, int stride, con
             } else {
                 multiply(All{});
             }
+            if constexpr (SPLIT)
+                if (c + G >= c1) multiply_by(units[buffer][1], acc);
             buffer ^= 1;
             put_rows(next, buffer);
             wait_lgkmcnt0();
@@ -847,8 +994,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
     auto take = [&](int item) {
         const Place at = place_of<16 * MT>(l, item, groups);
         const int e = at.expert, left = at.left, tile = tile_of(at.piece);
-        Item v;
-        v.from = a.x + (int64_t)(l.slots[at.first + min((tid >> 4) & (16 * MT - 1), left - 1)] / a.top) * a.ldx;
+        Item<uint16_t> v;
+        v.from = a.x + (int64_t)(l.slots[at.first + min(copied_row<uint16_t, MT>(), left - 1)] / a.top) * a.ldx;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             v.wc[t] = codes_of(a.up, e, t * a.I + 16 * tile);
@@ -873,7 +1020,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
             }
     };
     const Share mine = share_of(l.blocks * groups);
-    stream_items<B, MT>(mine.begin, mine.end, mine.stride, of, a.K, lds, take, store);
+    stream_items<B, MT, uint16_t>(mine.begin, mine.end, mine.stride, of, a.K, lds, nullptr, take, store);
 }
 
 // Results of every slot by itself, in fp32.  An item: 256 columns of an expert over one of `splits` runs of I, for up to 8 MT of its tokens; a wave has 32 columns.
@@ -882,6 +1029,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Lists& l = *reinterpret_cast<Lists*>(lds + 2 * kRowBytes<MT>);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    float(*units)[2][8 * MT] = reinterpret_cast<float(*)[2][8 * MT]>(lds + 2 * kRowBytes<MT> + kListBytes);
     lists_of<512, 8 * MT>(a.ids, nullptr, a.M, a.top, a.E, l);
     const int chunks = (a.I + 127) >> 7, pieces = a.groups * a.splits, last = a.N < 16 ? 0 : a.N - 16;
     const Row<B> of(min(i, a.N - 1), q, a.I, a.down.code_pitch, a.down.scale_pitch);
@@ -889,16 +1037,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
     auto take = [&](int item) {
         const Place at = place_of<8 * MT>(l, item, pieces);
         const int e = at.expert, left = at.left, split = at.piece / a.groups, n0 = col_of(at.piece - split * a.groups);
-        const int copy = (tid >> 4) & (16 * MT - 1), which = 8 * (copy >> 4) + (copy & 7);
-        Item v;
-        v.from = ((copy & 8) == 0 ? a.high : a.low) + (int64_t)l.slots[at.first + min(which, left - 1)] * a.pitch;
+        Item<float> v;
+        v.from = a.h + (int64_t)l.slots[at.first + min(copied_row<float, MT>(), left - 1)] * a.pitch;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {               // tiles past the last column begin 16 before it; what an earlier tile has, too, is not stored
             v.wc[t] = codes_of(a.down, e, min(n0 + 16 * t, last));
             v.ws[t] = scales_of(a.down, e, min(n0 + 16 * t, last));
         }
         v.c0 = split * chunks / a.splits, v.c1 = (split + 1) * chunks / a.splits;
-        v.scale = B == 16 ? a.down.tensor_scales[e] * kUnit : kUnit / kFolded<B>;
+        v.scale = B == 16 ? a.down.tensor_scales[e] : 1.0f / kFolded<B>;
         v.two = left > 8;
         v.place = at;
         return v;
@@ -915,14 +1062,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 4
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const uint2v both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[r][t][k]), __float_as_uint(acc[r][t][k]), false, false);
-                    const float v = __builtin_fmaf(__uint_as_float(both[1]), kLow, __uint_as_float(both[0]));
+                    const float v = __uint_as_float(both[0]) + __uint_as_float(both[1]);
                     const int n = min(n0 + 16 * t, last) + i;
                     if (lane < 32 && at < left && n >= n0 + 16 * t && n < a.N) to[n] = v * alpha;
                 }
             }
     };
     const Share mine = share_of(l.blocks * pieces);
-    stream_items<B, MT>(mine.begin, mine.end, mine.stride, of, a.I, lds, take, store);
+    stream_items<B, MT, float>(mine.begin, mine.end, mine.stride, of, a.I, lds, units, take, store);
 }
 
 // y of a token: its slots' results, each over its runs, in their order, and the residual.
@@ -975,14 +1122,15 @@ int64_t pitch_of(int64_t I) { return (I + 127) / 128 * 128; }
 
 // Bytes of a launch's parts of the workspace.
 struct MoeWorkspace {
-    size_t reordered, half, partial;            // rows in the weights' order; one of the two numbers of h; slots' results
+    size_t reordered, h, partial;               // rows in the weights' order; h, and its exponents; slots' results
 };
 size_t whole_lines(int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; }
 size_t partial_bytes(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
     return M == 0 || down_few(M, top, I) ? 0 : whole_lines((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4);
 }
 MoeWorkspace workspace_of(int64_t M, int64_t top, int64_t K, int64_t I, int64_t N, int64_t E, bool reorder) {
-    return {reorder ? whole_lines(M * K * 2) : 0, whole_lines(M * top * pitch_of(I) * 2), partial_bytes(M, top, E, I, N)};
+    const int64_t exponents = down_few(M, top, I) ? M * top * exponents_pitch((int)(I / 16)) : 0;
+    return {reorder ? whole_lines(M * K * 2) : 0, whole_lines(M * top * pitch_of(I) * 4 + exponents), partial_bytes(M, top, E, I, N)};
 }
 
 template <int B, int KW, int G, int SLOTS>
@@ -1009,7 +1157,7 @@ arcq_status launch_down_waves(const DownArgs<OutT>& d, hipStream_t stream) {
     auto kern = down_few_kernel<B, TOKENS, WAVES, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + 256 + 512 + 256, stream, d);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((d.N + 15) / 16)), dim3(64 * WAVES), WAVES * (512 + TOKENS * 512) + kFewTables, stream, d);
     return check_launch("down_few_kernel");
 }
 
@@ -1027,7 +1175,7 @@ arcq_status launch_up_many(const UpArgs& u, int64_t items, hipStream_t stream) {
     auto kern = up_many_kernel<B, MT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu() * (MT == 1 ? 2 : 1))), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, u);
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu() * (MT == 1 ? 2 : 1))), dim3(512), 2 * kRowBytes<MT> + kListBytes, stream, u);
     return check_launch("up_many_kernel");
 }
 template <int B, int MT, typename OutT>
@@ -1035,7 +1183,7 @@ arcq_status launch_down_many(const DownArgs<OutT>& d, int64_t items, hipStream_t
     auto kern = down_many_kernel<B, MT, OutT>;
     static std::atomic<uint64_t> lds_raised{0};
     if (arcq_status st = raise_lds_limit(reinterpret_cast<const void*>(kern), lds_raised)) return st;
-    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu() * (MT == 1 ? 2 : 1))), dim3(512), 2 * kRowBytes<MT> + sizeof(Lists), stream, d);
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min<int64_t>(items, num_cu() * (MT == 1 ? 2 : 1))), dim3(512), 2 * kRowBytes<MT> + kListBytes + 2 * 2 * 8 * MT * sizeof(float), stream, d);
     return check_launch("down_many_kernel");
 }
 
@@ -1043,8 +1191,10 @@ template <int B, typename OutT>
 arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     const MoeWorkspace w = workspace_of(std::min<int64_t>(p.M, kMostTokens), p.top, p.K, p.I, p.N, p.E, p.perm != nullptr);
     uint8_t* at = static_cast<uint8_t*>(p.workspace);
-    uint16_t *reordered = reinterpret_cast<uint16_t*>(at), *high = reinterpret_cast<uint16_t*>(at + w.reordered), *low = reinterpret_cast<uint16_t*>(at + w.reordered + w.half);
-    float* partial = reinterpret_cast<float*>(at + w.reordered + 2 * w.half);
+    uint16_t* reordered = reinterpret_cast<uint16_t*>(at);
+    float *h = reinterpret_cast<float*>(at + w.reordered), *partial = reinterpret_cast<float*>(at + w.reordered + w.h);
+    // (a last launch of fewer tokens leaves room behind h: that of 64 tokens holds h and exponents of 8)
+    uint8_t* exponents = down_few(M, p.top, p.I) ? reinterpret_cast<uint8_t*>(h + M * p.top * pitch_of(p.I)) : nullptr;
     const uint16_t* x = static_cast<const uint16_t*>(p.x) + m0 * p.ldx;
     int64_t ldx = p.ldx;
     // Up to 8192 values that have to be put in order are so by up_few_kernel itself: one token of 2048 through eight of 64 18.2 us, behind a launch that does it
@@ -1059,7 +1209,7 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     const int tiles = (int)(p.I / 16);
     const Experts up = {p.up_codes, p.up_scales, p.up_tensor_scales, (p.K + p.S_up) / 2, (p.K + p.S_up) / B, (int)(2 * p.I)};
     const Experts down = {p.down_codes, p.down_scales, p.down_tensor_scales, (p.I + p.S_down) / 2, (p.I + p.S_down) / B, (int)p.N};
-    const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, high, low, (int)pitch_of(p.I), tiles, gather ? p.perm : nullptr};
+    const UpArgs u = {x, ldx, ids, p.weights + m0 * p.top, (int)M, (int)p.top, (int)p.E, (int)p.K, (int)p.I, p.activation, up, h, (int)pitch_of(p.I), exponents, tiles, gather ? p.perm : nullptr};
     if (up_few(M, p.top, p.K)) {
         const int64_t items = most * tiles;
         const int chunks = (int)((p.K + 127) / 128);
@@ -1072,7 +1222,7 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
         const int64_t groups = (tiles + 7) / 8;
         if (arcq_status st = M <= 16 ? launch_up_many<B, 1>(u, M * p.top * groups, p.stream) : launch_up_many<B, 2>(u, M * p.top * groups, p.stream)) return st;
     }
-    DownArgs<OutT> d = {high, low, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
+    DownArgs<OutT> d = {h, exponents, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
                         static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 255) / 256), 1};
     if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2>(d, p.stream) : M <= 4 ? launch_down_few<B, 4>(d, p.stream) : launch_down_few<B, 8>(d, p.stream);
     // (a last launch of fewer tokens has the runs of the first: there is room for those)
@@ -1097,7 +1247,7 @@ size_t moe_workspace_bytes(int64_t M, int64_t top, int64_t E, int64_t K, int64_t
         const int64_t experts = kRunItems / (groups * runs);        // that there may be work for
         partial = std::max(partial, partial_bytes(E <= experts ? M : std::min(M, experts / top), top, E, I, N));
     }
-    return w.reordered + 2 * w.half + partial;
+    return w.reordered + w.h + partial;
 }
 
 // Tokens go kMostTokens at a time.
