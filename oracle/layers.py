@@ -42,17 +42,23 @@ def activation(name, v):
     raise ValueError(name)
 
 
+def gelu_tail(v):
+    """|v| Phi(-|v|)"""
+    return np.abs(v) * _erfc(np.abs(v) / math.sqrt(2.0)) / 2.0
+
+
 def activation_slack(name, v):
     """What evaluating it in fp32 may be off by at a v in fp32.
     silu, gelu_tanh: v / (1 + E), E = 2^(-t log2 e): the exponent's rounding and the constant's put 1.5 |t| half steps on E (tanh's t itself has four
     roundings: 4 |t| more), the exponential, the sum, the reciprocal and the product 2 + 1 + 2 + 1; where E overflows the result is 0.
-    gelu: |v| / 2 times an erfc off by 1.5e-7 (Abramowitz and Stegun 7.1.26), whose polynomial sums terms of up to 4.5 in all with five roundings."""
+    gelu: v less a tail of |v| / 2 erfc(|v| / sqrt(2)), each of which is within half a step, and the tail's value within 20: its argument t = 1 / (1 + p z) within 3 behind the sum's
+    and z's roundings, 2 more by the reciprocal, times at most 3 (z = 0, where z's own error does not count: 9 in all), the polynomial's fit 1, its roundings 4, t 1, the
+    exponential with what is put back on it 4, the products 1."""
     v = np.asarray(v, dtype=np.float64)
     if name in ("none", "relu"):
         return np.zeros_like(v)
     if name == "gelu":
-        z = np.minimum(v * v / 2.0, 700.0)
-        return np.abs(v) / 2.0 * (1.5e-7 + (30.0 + 4.0 * z) * HALF * np.exp(-z)) + np.abs(v) * HALF
+        return gelu_tail(v) * 20.0 * HALF + np.abs(v) * HALF + 2.0 ** -126
     t = np.abs(v) if name == "silu" else 1.6 * (np.abs(v) + 0.044715 * np.abs(v) ** 3)
     out = np.abs(activation(name, v))
     return out * ((1.5 if name == "silu" else 5.5) * np.minimum(t, 200.0) + 6.0) * HALF + 2.0 ** -110
