@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/arcq.h"
 #include "gemm_epilogue.h"
 
@@ -19,6 +21,10 @@ struct Epilogue {
     int64_t ldr;
     int activation;
 };
+
+// y of a kernel.  Where there may be a residual that is y, its memory is read through another pointer than it is written through.
+template <typename OutT, typename Ep>
+using OutputOf = std::conditional_t<std::is_same<Ep, NoEpilogue>::value, OutT* __restrict__, OutT*>;
 
 constexpr float kLog2e = 1.44269504088896340736f;
 

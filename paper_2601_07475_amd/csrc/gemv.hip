@@ -53,7 +53,7 @@ constexpr int kWhole = 8192;                    // WHOLE: most values of the row
 template <int B, int ROWS, int NT, int WAVES, int X, typename OutT, typename Ep>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(ROWS == 4 || WAVES == 16 ? 4 : 2, 4))) void gemv_kernel(
     const uint16_t* __restrict__ x, int64_t ldx, int M, int K, const int32_t* __restrict__ perm, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutT* __restrict__ y, int64_t ldy, int tiles_n, uint32_t stride, uint32_t splits, Ep ep) {
+    const uint8_t* __restrict__ w_scales, int N, int64_t cpitch, int64_t spitch, float alpha, OutputOf<OutT, Ep> y, int64_t ldy, int tiles_n, uint32_t stride, uint32_t splits, Ep ep) {
     constexpr int MT = (ROWS + 15) / 16, THREADS = 64 * WAVES, PIECES = kWhole / 8 / THREADS;
     static_assert(X == SLICE || MT == 1, "WHOLE: up to 16 rows");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];

@@ -56,7 +56,7 @@ __device__ __forceinline__ void split_codes(const int8v& a, int8v& large, int8v&
 template <int MT, int NT, int WAVES, typename OutT, typename Ep>
 __global__ __launch_bounds__(WAVES * 64) void mx8_stream_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, uint32_t tiles_n, uint32_t tiles_m, int splits, Ep ep) {
+    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutputOf<OutT, Ep> y, int64_t ldy, uint32_t tiles_n, uint32_t tiles_m, int splits, Ep ep) {
     // the partial tiles of BATCH weight tiles fit the static LDS limit at a time
     constexpr int BATCH = WAVES * MT * NT > 64 ? (NT + 1) / 2 : NT;
     __shared__ float red[WAVES][MT * BATCH][4][64];
@@ -218,7 +218,7 @@ __device__ __forceinline__ float16v mfma_w4a8(const uint4& w, const int8v& a, co
 template <int WM, int WN, int GM, int GN, int NS, typename OutT, typename Ep>
 __global__ __launch_bounds__(64 * GM * GN) void mx8_tile_kernel(
     const uint8_t* __restrict__ a_codes, const uint8_t* __restrict__ a_scales, const uint8_t* __restrict__ w_codes,
-    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutT* __restrict__ y, int64_t ldy, int tiles_m, int tiles_n,
+    const uint8_t* __restrict__ w_scales, int M, int N, int nb, int nbw, OutputOf<OutT, Ep> y, int64_t ldy, int tiles_m, int tiles_n,
     int group_rows, int splits, int64_t split_stride, Ep ep) {
     using C = Mx8Tile<WM, WN, GM, GN, NS>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
