@@ -149,7 +149,7 @@ __global__ __launch_bounds__(1024) void route_token_kernel(RouteArgs a, int team
 
 // 16 tokens by 16 experts, one of `splits` runs of K, in four waves.  Lane (i, q) brings k = 32 c + 8 q .. + 7 of token i and of expert i: the s-th of
 // these of the four lane groups are a step of the matrix instruction.
-__global__ __launch_bounds__(256) void scores_kernel(RouteArgs a, uint32_t tiles_e, uint32_t tiles_m) {
+__global__ __launch_bounds__(256) void scores_kernel(RouteArgs a, uint32_t tiles_e) {
     __shared__ double part[4][256];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     const uint32_t tile = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x % (uint32_t)a.splits;
@@ -260,7 +260,7 @@ arcq_status launch_moe_route(const void* x, int64_t M, int64_t K, int64_t ldx, c
             continue;
         }
         const unsigned tiles_e = (unsigned)((E + 15) / 16), tiles_m = (unsigned)((rows + 15) / 16);
-        hipLaunchKernelGGL(scores_kernel, dim3(tiles_e * tiles_m * (unsigned)splits), dim3(256), 0, stream, a, tiles_e, tiles_m);
+        hipLaunchKernelGGL(scores_kernel, dim3(tiles_e * tiles_m * (unsigned)splits), dim3(256), 0, stream, a, tiles_e);
         if (arcq_status st = check_launch("scores_kernel")) return st;
         const arcq_status st = E <= 64    ? launch_choose<1>(a, stream)
                                : E <= 128 ? launch_choose<2>(a, stream)
