@@ -4,7 +4,7 @@
 // x fp16, G over U the 2 I rows of an expert's first operand, D its second; NVFP4 (B = 16) or MXFP4 (B = 32).
 //
 // Bound by reading the chosen experts' weights once (3 K I weights each, 9/16 or 17/32 byte a weight).  Tokens are rows of v_mfma_f32_16x16x32_f16's tile, so
-// up to 16 (8 behind the activation) cost what one does.  Two launches, because every column of h depends on all of x and every column of y on all of h; what
+// up to 16 (4 behind the activation) cost what one does.  Two launches, because every column of h depends on all of x and every column of y on all of h; what
 // a launch that waits for another costs by itself, start, choices and the first trip to memory, is 5 to 6 us, and with few bytes that is most of the time.
 //
 // Every workgroup finds out by itself which tokens choose an expert: no kernel in front, and none that waits for the host.  An expert that a token
@@ -469,14 +469,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     }
 }
 
-// Up to 8 tokens: 16 columns of y a workgroup.  The reduction runs over all chosen experts' channels one after the other, in equal shares for the waves, G
+// Up to 4 tokens: 16 columns of y a workgroup.  The reduction runs over all chosen experts' channels one after the other, in equal shares for the waves, G
 // chunks at a time; a wave adds what it has of an expert to its own sums of all tokens, and the waves' sums are added in their order at the end.
 // Rows of h reach a wave's registers through a slice of LDS of its own, so that a chunk on its way takes TOKENS / 2 registers of 16 bytes and not four.  A row
 // of h has one unit, by the exponents that came with it: looking for the largest values of a chunk on its arrival instead took 2 to 10 % of a call.
 constexpr int kFewTables = 256 + 512 + 256 + 256;      // bytes of its tables in LDS
 template <int B, int TOKENS, int WAVES, typename OutT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(4, 4))) void down_few_kernel(DownArgs<OutT> a) {
-    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2, G = TOKENS < 8 ? 4 : B == 16 ? 3 : 2;      // (as registers allow)
+    constexpr int THREADS = 64 * WAVES, LOADS = TOKENS / 2, G = 4;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     float(&sums)[WAVES][8][16] = *reinterpret_cast<float(*)[WAVES][8][16]>(lds);
     int* ids_of = reinterpret_cast<int*>(lds + sizeof(sums));
@@ -763,7 +763,8 @@ constexpr int kRowBytes = kStage * MT * 4096;   // of a buffer
 // Which row a thread copies pieces of, and which of a chunk's pieces of 16 bytes: rows of fp32 have 32, so that half a wave has all of a row's.
 template <typename T, int MT>
 __device__ __forceinline__ int copied_row() {
-    return std::is_same<T, float>::value ? (int)threadIdx.x / (64 / MT) : (int)(threadIdx.x >> 4) & (16 * MT - 1);
+    if (std::is_same<T, float>::value) return MT == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : (int)threadIdx.x / (64 / MT);
+    return (int)(threadIdx.x >> 4) & (16 * MT - 1);
 }
 
 template <int B, int MT, typename T, typename Take, typename Store>
@@ -1089,18 +1090,21 @@ __global__ __launch_bounds__(256) void join_kernel(DownArgs<OutT> a, uint32_t pa
     store_out(a.y + m * a.ldy + n, sum);
 }
 
-// Whether a launch's tokens go as rows of one tile: up to the activation wherever 16 rows and LDS take them, behind it up to 8 tokens.  Measured, us of a call, and with
-// the tokens gathered instead there:       up_few_kernel                   down_few_kernel
-//   1 x 4096 x 14336, two of eight             51    60                        51    60
-//   4 x 4096 x 1792, eight of 128              84    95                        85    91    (8 tokens 153, 149; 16 tokens 229, 229)
-//   13 x 5120 x 1392, four of 30               93   107                        (more than 8 tokens)
-//   1 x 2048 x 1024, eight of 64                                               18    27
+// Whether a launch's tokens go as rows of one tile: up to the activation wherever 16 rows and LDS take them, behind it up to 4 tokens.  Measured, us of a call, and with
+// the tokens gathered instead in front of the activation, and behind it:
+//                                            1 token        4 tokens          5 tokens          8 tokens          16 tokens
+//   2048 x 1024, eight of 64, MXFP4        18.7  28  29      41   43   40      50    -   45      64   73   56       69   72
+//   4096 x 14336, two of eight, NVFP4      52.7  59  60     142  176  148     160    -  153     193  219  175      182  204
+//   4096 x 1792, eight of 128, MXFP4       31.9  44  44      87   99   90     110    -  107     165  175  152      239  240
+//   5120 x 1392, four of 30, NVFP4, fp32   23.6  58  33      62   76   63      68    -   69      79   90   79      110  110
 size_t up_few_lds(int64_t M, int64_t K) { return sizeof(UpFewLds) + (size_t)M * (size_t)((K + 127) / 128 * 256 + 16); }
 bool up_few(int64_t M, int64_t top, int64_t K) { return M <= 16 && M * top <= 256 && K >= 256 && up_few_lds(M, K) <= kMaxLdsBytes; }
-bool down_few(int64_t M, int64_t top, int64_t I) { return M <= 8 && M * top <= 64 && I >= 128; }
+bool down_few(int64_t M, int64_t I) { return M <= 4 && I >= 128; }
 
-// Waves that split K in up_few_kernel: as many as have four chunks each.  And how many chunks go together, so that few are asked for in vain where a wave's are
-// not a multiple of that.  (13 x 5120 x 1392, four of 30: 5 chunks a wave go as five in 93 us, as four and one of four in 97.)
+// Waves that split K in up_few_kernel: as many as have four chunks each.  Measured, us of a call, and with half and with twice as many: K = 2048, eight of 64, one token
+// 18.3, 19.7, 18.9, four 40.6, 40.9, 44.0; K = 4096, two of eight, one token with eight waves 52.4, with four 56.2, four tokens 143, 151; K = 1024, eight of 64, four tokens with
+// two waves 31.4, with four 32.7.  And how many chunks go together, so that few are asked for in vain where a wave's are not a multiple of that.  (13 x 5120 x 1392, four
+// of 30: 5 chunks a wave go as five in 93 us, as four and one of four in 97.)
 int waves_of(int chunks) { return chunks >= 32 ? 8 : chunks >= 16 ? 4 : 2; }
 int group_of(int chunks, int waves) {
     const int most = (chunks + waves - 1) / waves;
@@ -1126,10 +1130,10 @@ struct MoeWorkspace {
 };
 size_t whole_lines(int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; }
 size_t partial_bytes(int64_t M, int64_t top, int64_t E, int64_t I, int64_t N) {
-    return M == 0 || down_few(M, top, I) ? 0 : whole_lines((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4);
+    return M == 0 || down_few(M, I) ? 0 : whole_lines((int64_t)down_splits(M, top, E, I, N) * M * top * N * 4);
 }
 MoeWorkspace workspace_of(int64_t M, int64_t top, int64_t K, int64_t I, int64_t N, int64_t E, bool reorder) {
-    const int64_t exponents = down_few(M, top, I) ? M * top * exponents_pitch((int)(I / 16)) : 0;
+    const int64_t exponents = down_few(M, I) ? M * top * exponents_pitch((int)(I / 16)) : 0;
     return {reorder ? whole_lines(M * K * 2) : 0, whole_lines(M * top * pitch_of(I) * 4 + exponents), partial_bytes(M, top, E, I, N)};
 }
 
@@ -1162,7 +1166,7 @@ arcq_status launch_down_waves(const DownArgs<OutT>& d, hipStream_t stream) {
 }
 
 // 16 waves a workgroup, one on a compute unit; where a last round of those would leave a quarter of the compute units' time idle, 8, of which two fit.
-// (5120 features, 1392 channels, four of 30, us of a call with 8 and with 16: one token 24, 27; four 61, 66; eight 79, 84.)
+// (5120 features, 1392 channels, four of 30, us of a call with 8 and with 16: one token 24, 27; four 61, 66.)
 template <int B, int TOKENS, typename OutT>
 arcq_status launch_down_few(const DownArgs<OutT>& d, hipStream_t stream) {
     const int64_t tiles = (d.N + 15) / 16, cus = num_cu(), rounds = (tiles + cus - 1) / cus;
@@ -1193,8 +1197,8 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     uint8_t* at = static_cast<uint8_t*>(p.workspace);
     uint16_t* reordered = reinterpret_cast<uint16_t*>(at);
     float *h = reinterpret_cast<float*>(at + w.reordered), *partial = reinterpret_cast<float*>(at + w.reordered + w.h);
-    // (a last launch of fewer tokens leaves room behind h: that of 64 tokens holds h and exponents of 8)
-    uint8_t* exponents = down_few(M, p.top, p.I) ? reinterpret_cast<uint8_t*>(h + M * p.top * pitch_of(p.I)) : nullptr;
+    // (a last launch of fewer tokens leaves room behind h: that of 64 tokens holds h and exponents of 4)
+    uint8_t* exponents = down_few(M, p.I) ? reinterpret_cast<uint8_t*>(h + M * p.top * pitch_of(p.I)) : nullptr;
     const uint16_t* x = static_cast<const uint16_t*>(p.x) + m0 * p.ldx;
     int64_t ldx = p.ldx;
     // Up to 8192 values that have to be put in order are so by up_few_kernel itself: one token of 2048 through eight of 64 18.2 us, behind a launch that does it
@@ -1224,7 +1228,7 @@ arcq_status launch_tokens(const MoeArgs& p, int64_t m0, int64_t M) {
     }
     DownArgs<OutT> d = {h, exponents, ids, (int)M, (int)p.top, (int)p.E, (int)p.I, (int)pitch_of(p.I), (int)p.N, down, static_cast<const OutT*>(p.residual) + (p.residual ? m0 * p.ldr : 0), p.ldr,
                         static_cast<OutT*>(p.y) + m0 * p.ldy, p.ldy, partial, (int)((p.N + 255) / 256), 1};
-    if (down_few(M, p.top, p.I)) return M <= 2 ? launch_down_few<B, 2>(d, p.stream) : M <= 4 ? launch_down_few<B, 4>(d, p.stream) : launch_down_few<B, 8>(d, p.stream);
+    if (down_few(M, p.I)) return M <= 2 ? launch_down_few<B, 2>(d, p.stream) : launch_down_few<B, 4>(d, p.stream);
     // (a last launch of fewer tokens has the runs of the first: there is room for those)
     d.splits = down_splits(std::min<int64_t>(p.M, kMostTokens), p.top, p.E, p.I, p.N);
     const int64_t items = M * p.top * d.splits * d.groups;

@@ -12,7 +12,7 @@ from test_gpu_epilogue import ACT, assert_within
 from test_gpu_experts import call, choices, random_experts
 from test_gpu_parity import dev, say
 
-# tokens as rows of one tile, two, four and eight of them, with sixteen waves a workgroup and with eight; gathered, 8 and 16 rows at a time, from less than a chunk to several
+# tokens as rows of one tile, two and four of them, with sixteen waves a workgroup and with eight; gathered, 8 and 16 rows at a time, from less than a chunk to several
 # runs of the channels between
 KINDS = [(1, 256, 2), (2, 1120, 2), (3, 288, 1), (4, 2080, 2), (5, 416, 2), (8, 544, 2), (8, 1312, 1), (3, 64, 1), (7, 96, 2), (5, 2080, 16), (8, 160, 9), (12, 96, 2), (20, 2080, 2), (40, 288, 2),
          (70, 1056, 1)]

@@ -47,7 +47,7 @@ def test_experts(top, E, K, I, N, reorder):
     for m in range(1, 65):
         # h of every slot in 32 bits, and results of every run, as the launch has them, where they are added up by a launch of their own
         groups, runs = (N + 255) // 256 * min(E, m * top), 0
-        if m > 8 or m * top > 64 or I < 128:
+        if m > 4 or I < 128:
             runs = max(1, min(512 // groups, (I + 127) // 128 // 8, 8))
         assert got[m - 1] >= 4 * m * top * ((I + 127) // 128 * 128) + 4 * runs * m * top * N + 2 * m * K * reorder
         call = lambda ws, bytes_: B.lib().arcq_moe(FAKE, m, K, K, FAKE if reorder else None, FAKE, FAKE, top, E, FAKE, FAKE, FAKE, I, 0, FAKE, FAKE, FAKE, N, 0, 4,  # noqa: E731
