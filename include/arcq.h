@@ -390,7 +390,9 @@ arcq_status arcq_mx_gemv_epilogue(const void* x, int64_t M, int64_t K, int64_t l
  *   l[m, e] = sum_k x[m, k] router[e, k];   s[m, .] = softmax over the experts, or 1 / (1 + exp(-l)) each with ARCQ_MOE_SIGMOID
  *   ids[m, 0 .. top_k - 1]: the experts with the largest s[m, e] + bias[e], largest first, equal ones by ascending index;
  *   weights[m, j] = s[m, ids[m, j]], without the bias; with ARCQ_MOE_RENORMALIZE divided by the sum of the top_k.
- * Experts are ranked by values in 64 bits (of exact products; without a bias by l, which orders them as s does).
+ * Experts are ranked by values in 64 bits (of exact products; without a bias by l, which orders them as s does): values that differ by less than the roundings of a sum in
+ * 64 bits may fall either way.  The router has no bias of its own on l, and experts are chosen among all.  Scores that are 0 in 64 bits for all of the top_k have no shares:
+ * their renormalized weights are NaN.
  * x       fp16 [M, K], pitch ldx, K % 8 == 0, 16-byte aligned, ldx % 8 == 0;  router  fp16 [E, K], pitch ldr, the same
  * bias    fp32 [E], 4-byte aligned, or NULL: none
  * 1 <= top_k <= E <= ARCQ_MOE_MAX_EXPERTS, top_k <= ARCQ_MOE_MAX_TOP_K

@@ -121,8 +121,8 @@ struct Operands<Epilogue<OutT>> {
 // the accumulator registers, four activations would fill the instruction cache); the residual on the way out, where a wave's loads and stores are
 // whole lines.  A fragment row's residual is asked for before the one before it is worked on.
 // lds_wave: epilogue_lds_bytes(WN) bytes, as in store_fragment_rows_f16_via_lds.
-// Measured: 4096 x 8192 over K = 28672 with a residual in fp16 1.20 to 1.24 ms, the product alone 1.21 to 1.24 (1.28 where every row asked for its own and looked for the edge
-// value by value); 333 x 27648 over 5120 with SiLU 93 us, alone 90 to 97; 777 x 6147 over 4352 with everything, fp32, 65 us, alone 54 (one
+// Measured: 4096 x 8192 over K = 28672 with a residual in fp16 1.20 to 1.26 ms, the product alone 1.21 to 1.24 (1.28 where every row asked for its own and looked for the edge
+// value by value); 333 x 27648 over 5120 with SiLU 93 us, alone 90 to 97; 777 x 6147 over 4352 with everything, fp32, 66 us, alone 54 (one
 // round of tiles, all at their ends at the same time).
 template <int WM, int WN, typename OutT, bool INSIDE>
 struct TileEnd {

@@ -18,12 +18,13 @@
 //
 // No atomics on results, and every sum in an order that the sizes and choices fix: the same inputs give the same bits.
 //
-// Measured (us of a call whose weights are not in cache, TB/s of the chosen experts' weights, where a plain read reaches 6.2, and us of the two products alone):
-//   one token, eight of 64, 2048 x 1024, MXFP4              17   1.6     9 +   9
-//   one token, two of eight, 4096 x 14336, NVFP4            51   3.9    24 +  18 (weights in part cached)
-//   four tokens, eight of 128, 4096 x 1792, MXFP4           84   3.5    49 +  36
-//   13 tokens, four of 30, 5120 x 1392, NVFP4, fp32 y       89   2.8    54 +  34, reordering 2 to 4, joining 4
-//   64 tokens, two of eight, 4096 x 14336, MXFP4           201   3.7   118 + 102, joining 4
+// Measured: us of a call whose inputs and weights change from call to call, TB/s of the chosen experts' weights (a plain read reaches 6.2); and the durations that a trace of
+// calls with the same inputs gives of the products' kernels, which overlap at their ends and find part of their weights in caches: they do not add up to the call.
+//   one token, eight of 64, 2048 x 1024, MXFP4              17.8   1.5     8.8    9.6
+//   one token, two of eight, 4096 x 14336, NVFP4            50.6   3.9    24     19
+//   four tokens, eight of 128, 4096 x 1792, MXFP4           86     3.4    49     38
+//   13 tokens, four of 30, 5120 x 1392, NVFP4, fp32 y       88 to 98      54     36, reordering and joining 3 to 5 each
+//   64 tokens, two of eight, 4096 x 14336, MXFP4           208     3.6   118    114, joining 5
 #include "epilogue.h"
 #include "internal.h"
 #include "lds_dma.h"

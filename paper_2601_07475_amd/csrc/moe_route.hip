@@ -1,12 +1,13 @@
 // The router of a mixture of experts: scores of all experts for a token, its best ones and their weights.
 //   l[m, e] = sum_k x[m, k] r[e, k];   s = softmax(l) or 1 / (1 + exp(-l));   best by s (+ bias);   weights: their s, or their shares of those
-// Which experts are best is decided by sums in 64 bits of exact products, so near ties fall as the definition has it and not as an order of fp32 sums does.
+// Which experts are best is decided by sums in 64 bits of exact products: near ties fall as the definition has it down to the roundings of such a sum, whose order differs
+// between the kernels, and not as an order of fp32 sums does.
 //
 // One launch where a workgroup a token gets through the router's weights quickly; otherwise scores_kernel, on v_mfma_f64_16x16x4_f64, leaves sums of runs of K
 // in the workspace and choose_kernel adds them up in their order.  Bound by two launches for a few tokens, by the 64-bit matrix rate for many (2 M K E of
 // 78 * 10^12 a second).
-// Measured, us a call: 1 x 4096, two of eight 5.9 (one launch: a trip to memory for x and the weights, the sums of 16 waves, two choices one after the other);
-// 64 x 8192, eight of 256 15.7 (a workgroup a token, which reads all 4 MB of the weights for each, 119).
+// Measured, us a call: 1 x 4096, two of eight 5.9 to 6.2 (one launch: a trip to memory for x and the weights, the sums of 16 waves, two choices one after the other);
+// 64 x 8192, eight of 256 15.3 (a workgroup a token, which reads all 4 MB of the weights for each, 119).
 #include "internal.h"
 
 #include <algorithm>
